@@ -357,6 +357,91 @@ int kvr_continue_batched_rope(const kvr_desc *desc, const kvr_rope *rope, const 
                               void *out, void *ws, size_t ws_bytes, void *stream);
 
 /*
+ * One step of N readers that share a cached prefix and each have cached rows of
+ * their own (the paper's N readers of one document, once they have begun their
+ * answers): kvr_continue_batched serves their first turn, this every later one.
+ *   Qs [n][S][Hq][d], Ks/Vs [n][S][Hkv][d]: S new tokens of each reader.
+ *   kcache/vcache: the shared prefix, rows [0, L_prefix) are read (NULL when
+ *   L_prefix == 0).
+ *   ktail/vtail [n][n_kv_heads][tail_capacity][d]: the readers' own rows.
+ *   tail_len: DEVICE int32[n], own rows that reader r has cached.  They are read
+ *   when the work runs: a captured graph serves every step of a decode.
+ *   Token i of reader r sees the prefix, own rows [0, tail_len[r]) and new
+ *   tokens 0 .. i, never another reader's rows; out [n][S][Hq][d].
+ *   append != 0 also writes the new rows into own rows [tail_len[r],
+ *   tail_len[r] + S) (tail_len itself is the caller's to advance); append == 0
+ *   leaves the tails untouched (drafted tokens; needs no tail at all when
+ *   tail_capacity == 0).
+ *   A reader with tail_len[r] < 0 takes no part (an empty slot of the batch), and
+ *   neither does one whose rows do not fit (tail_len[r] > tail_capacity, or with
+ *   append tail_len[r] + S > tail_capacity): its rows of out and of the tails are
+ *   left as they were.
+ *   rope == NULL: Qs and Ks are rotated already.  Otherwise they arrive unrotated
+ *   and token i of reader r is rotated at position pos0 + tail_len[r] + i; the
+ *   caches hold rotated keys.  pos0 is L_prefix for a whole prefix, and the number
+ *   of positions that it stands for when rows were evicted from it.  Needs
+ *   rope->n_pos >= pos0 + tail_capacity (+ S when append == 0).
+ *   ws: kvr_workspace_bytes_shared(desc, L_prefix, n, S, tail_capacity) bytes.
+ * Limits: n S n_q_heads, L_prefix and tail_capacity below 2^31 (KVR_ERR_SHAPE).
+ * A masked place never reaches a result: not own rows behind a reader's length, nor
+ * a later new token's key or value, whatever they hold.
+ */
+int kvr_continue_shared(const kvr_desc *desc, const kvr_rope *rope, const void *Qs, const void *Ks, const void *Vs,
+                        int32_t n, int32_t S, const void *kcache, const void *vcache, int64_t L_prefix,
+                        int64_t pos0, void *ktail, void *vtail, int64_t tail_capacity, const int32_t *tail_len,
+                        int32_t append, void *out, void *ws, size_t ws_bytes, void *stream);
+
+/* Workspace bytes of kvr_continue_shared: non-decreasing in L_prefix and
+ * tail_capacity; (size_t)-1 for invalid arguments. */
+size_t kvr_workspace_bytes_shared(const kvr_desc *desc, int64_t L_prefix, int32_t n, int32_t S, int64_t tail_capacity);
+
+/*
+ * The attention weight that each cached row receives, accumulated:
+ *   weight[g][j] += sum over i < S and the query heads h of kv head g of
+ *                   softmax_j(scale * q_ih . k_j),  token i seeing keys 0 .. L_prefix + i
+ *   Qs [S][Hq][d], Ks [S][Hkv][d] as in kvr_continue (rotated already, by
+ *   kvr_rope_apply, where the cache holds rotated keys); kcache rows
+ *   [0, L_prefix) are read, rows behind them are not.  After a prefill of L tokens the last
+ *   W of them weigh its cache with L_prefix = L - W, S = W and their rows.
+ *   weight: device float [n_kv_heads][capacity], rows [0, L_prefix + S) added to
+ *   (new token i is row L_prefix + i), the others untouched.  Needs
+ *   L_prefix + S <= capacity (KVR_ERR_CAPACITY).
+ *   ws: kvr_workspace_bytes_weigh(desc, L_prefix, S) bytes.
+ * Scores, softmax and sums in fp32 for every element type.
+ * Limits: S n_q_heads / n_kv_heads and L_prefix + S below 2^31 (KVR_ERR_SHAPE).
+ */
+int kvr_cache_weigh(const kvr_desc *desc, const void *Qs, const void *Ks, const void *kcache, int64_t L_prefix,
+                    int64_t S, float *weight, void *ws, size_t ws_bytes, void *stream);
+
+/* Workspace bytes of kvr_cache_weigh: non-decreasing in L_prefix; (size_t)-1 for
+ * invalid arguments. */
+size_t kvr_workspace_bytes_weigh(const kvr_desc *desc, int64_t L_prefix, int64_t S);
+
+/*
+ * Eviction by accumulated weight: a smaller cache of n_keep of the rows [0, L), kv
+ * head by kv head: the first n_first rows, the last n_last, and of those between
+ * the ones with the largest weight, the lower row where weights are equal (a weight
+ * that is not a number counts as the largest).  The kept rows stay in order.
+ *   kcache/vcache, weight [n_kv_heads][capacity]: read.
+ *   kout/vout [n_kv_heads][capacity_out][d]: rows [0, n_keep) are written, exact
+ *   copies; a cache of n_keep rows for every entry point whose caller places the
+ *   following tokens itself (their positions go on from L, not from n_keep).
+ *   weight_out [n_kv_heads][capacity_out]: the kept rows' weights; NULL: not wanted.
+ *   index int32 [n_kv_heads][n_keep]: the rows they were; NULL: not wanted.
+ *   Needs n_first + n_last <= n_keep <= L (KVR_ERR_SHAPE), L <= capacity and
+ *   n_keep <= capacity_out (KVR_ERR_CAPACITY).  No output may overlap another
+ *   buffer of the call (KVR_ERR_SHAPE).  n_keep == 0 is a no-op.
+ *   weight, weight_out and index need 4-byte alignment.
+ *   ws: kvr_workspace_bytes_evict(desc, L) bytes.
+ */
+int kvr_cache_evict(const kvr_desc *desc, const void *kcache, const void *vcache, int64_t L, const float *weight,
+                    int64_t n_first, int64_t n_last, int64_t n_keep, void *kout, void *vout, int64_t capacity_out,
+                    float *weight_out, int32_t *index, void *ws, size_t ws_bytes, void *stream);
+
+/* Workspace bytes of kvr_cache_evict, for any n_keep <= L; (size_t)-1 for invalid arguments. */
+size_t kvr_workspace_bytes_evict(const kvr_desc *desc, int64_t L);
+
+/*
  * Workspace bytes of kvr_continue_rope (n <= 1, total_S = S) and
  * kvr_continue_batched_rope (n >= 2, total_S = cu[n]): the plain
  * continuation's workspace plus room for the rotated rows.  Non-decreasing in

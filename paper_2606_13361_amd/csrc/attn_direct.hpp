@@ -1,0 +1,321 @@
+// attn_direct.hpp -- attention tiles whose K and V rows go from memory straight
+// to the registers that the matrix instructions read: no LDS and no barrier in
+// the key loop.  Shared by shared.hip (attention of many readers) and weigh.hip
+// (accumulated attention weight).
+//
+// Notation of one wave and one stage of KEYS keys; a tile is 16 query rows:
+//   S^T[key][row]  = K Q^T      A = K: lane (i, g) = (lane % 16, lane / 16) holds 16
+//                               consecutive bytes of key i's row (of every 64)
+//   O^T[d][row]   += V^T P^T    B = P^T: the score accumulator itself.  It leaves lane
+//                               (i, g) with row i and keys 4 g + e of each 16-key part,
+//                               and the k-slots of a product only have to name the same
+//                               key in A and B.
+// A = V^T wants NT = D / 16 operands of one head-dim index and the lane's keys.
+// Operand t of lane i is given head-dim index NT i + t, so a lane loads NT
+// consecutive elements of each of its keys' V rows (16 lanes read a whole row)
+// and, in 16-bit types, transposes them in registers: 4 byte permutes for each
+// operand of 8 keys.  The output comes out alike: lane (row, g), operand t,
+// component c is head-dim index NT (4 g + c) + t.
+//
+// Rows come through a buffer resource that ends with the last valid one: a lane
+// past it reads zeros and touches no memory, so ragged ends need no address of
+// their own, and their scores are masked by the key's index.
+#pragma once
+
+#include <type_traits>
+
+#include "attn_common.hpp"
+
+namespace kvr {
+namespace dev {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Rows [0, n) of stride_b bytes from `base`, of which row_b are read: the resource
+// that ends with row n - 1 (n <= 0: an empty one).  n * stride_b stays below 2^31:
+// a stage has at most 32 rows, and a row of all kv heads at most 2 MB.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_rsrc(uint64_t base, int n, uint32_t stride_b, uint32_t row_b) {
+    const uint32_t bytes = n > 0 ? (uint32_t)(n - 1) * stride_b + row_b : 0u;
+    return __builtin_amdgcn_make_buffer_rsrc((void *)(uintptr_t)base, 0, bytes, 0x00020000);
+}
+
+// Maximum and sum over the four lanes of a query row (lanes i, i + 16, i + 32, i + 48;
+// the same bits in each)
+__device__ __forceinline__ float quad_max(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return pair_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// 16-bit elements (E: Bf16 or F16): stages of 32 keys, two 16-key parts
+template <class E, int D>
+struct Op16 {
+    static constexpr int DIM = D, KEYS = 32, NS = 8, NT = D / 16, NK = D / 32, ROWB = D * 2, ELT = 2;
+    struct Q {
+        u32x4 f[NK];
+    };
+    typedef uint32_t vrow __attribute__((ext_vector_type(NT / 2)));
+    struct K {
+        u32x4 f[2][NK];
+    };
+    struct V {
+        vrow r[8];
+    };
+    // the lane's key of score e
+    __device__ static __forceinline__ int key_of(int e, int g) { return 16 * (e >> 2) + 4 * g + (e & 3); }
+
+    __device__ static __forceinline__ void load_q(Q &q, const void *row, int g) {
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks) q.f[ks] = *(const u32x4 *)((const unsigned char *)row + 64 * ks + 16 * g);
+    }
+    // cs: the table row of the position
+    __device__ static __forceinline__ void rotate_q(Q &q, const float *cs, int g) {
+#pragma unroll
+        for (int ks = 0; ks < NK / 2; ++ks) rope_rot8<E>(q.f[ks], q.f[ks + NK / 2], cs + 2 * (32 * ks + 8 * g));
+    }
+    __device__ static __forceinline__ void load_k(K &k, __amdgpu_buffer_rsrc_t r, uint32_t stride_b, int i, int g) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int ks = 0; ks < NK; ++ks)
+                k.f[h][ks] = buf_load16(r, (uint32_t)(16 * h + i) * stride_b + 16 * g + 64 * ks);
+    }
+    __device__ static __forceinline__ void load_v(V &v, __amdgpu_buffer_rsrc_t r, uint32_t stride_b, int i, int g) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t off = (uint32_t)key_of(e, g) * stride_b + 2 * NT * i;
+            if constexpr (NT == 8) v.r[e] = buf_load16(r, off);
+            else v.r[e] = __builtin_amdgcn_raw_buffer_load_b64(r, (int)off, 0, 0);
+        }
+    }
+    // new key rows: position of key c of the stage is that of table row cs + c * D
+    __device__ static __forceinline__ void rotate_k(K &k, const float *cs, int n, int i, int g) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int c = min(16 * h + i, n - 1);      // a row past the last is masked: any table row
+#pragma unroll
+            for (int ks = 0; ks < NK / 2; ++ks)
+                rope_rot8<E>(k.f[h][ks], k.f[h][ks + NK / 2], cs + c * D + 2 * (32 * ks + 8 * g));
+        }
+    }
+    // rows [0, n) of the stage into consecutive rows of a cache
+    __device__ static __forceinline__ void store(const K &k, const V &v, unsigned char *kd, unsigned char *vd, int n,
+                                                 int i, int g) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (16 * h + i < n)
+#pragma unroll
+                for (int ks = 0; ks < NK; ++ks)
+                    *(u32x4 *)(kd + (16 * h + i) * ROWB + 64 * ks + 16 * g) = k.f[h][ks];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (key_of(e, g) < n) *(vrow *)(vd + key_of(e, g) * ROWB + 2 * NT * i) = v.r[e];
+    }
+    __device__ static __forceinline__ void scores(const K &k, const Q &q, float (&s)[NS]) {
+        f32x4 a[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) a[h] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) a[h] = mfma(k.f[h][ks], q.f[ks], a[h]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = a[e >> 2][e & 3];
+    }
+    // Weights as the second product's operand: the element type, rounded to nearest
+    // even.  Each weight is off by half a step at most, as the values it multiplies
+    // are by themselves; the row's sum is taken from the unrounded ones.
+    struct P {
+        u32x4 f;
+    };
+    __device__ static __forceinline__ void weights(P &w, const float (&p)[NS]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w.f[j] = E::pack2(p[2 * j], p[2 * j + 1]);
+    }
+    // whether every value of the stage is a number (the exponent's bits are not all set)
+    __device__ static __forceinline__ bool finite(const V &v) {
+        constexpr uint32_t ex = std::is_same<E, F16>::value ? 0x7c00u : 0x7f80u;
+        bool ok = true;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int j = 0; j < NT / 2; ++j)
+                ok = ok && (v.r[e][j] & ex) != ex && (v.r[e][j] >> 16 & ex) != ex;
+        return ok;
+    }
+    // o[rt][t] += V^T P^T of every tile
+    template <int RT>
+    __device__ static __forceinline__ void accumulate(const V &v, const P (&w)[RT], f32x4 (&o)[RT][NT]) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            u32x4 a;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)      // elements t of keys 2j (low half) and 2j + 1 (high half)
+                a[j] = __builtin_amdgcn_perm(v.r[2 * j + 1][t / 2], v.r[2 * j][t / 2],
+                                             (t & 1) ? 0x07060302u : 0x05040100u);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) o[rt][t] = mfma(a, w[rt].f, o[rt][t]);
+        }
+    }
+    // the same of key c alone (zeros in the place of the others), for the rows that see it
+    template <int RT>
+    __device__ static __forceinline__ void accumulate_key(const V &v, const P (&w)[RT], f32x4 (&o)[RT][NT], int c,
+                                                          const bool (&sees)[RT], int g) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            u32x4 a;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t keep = key_of(2 * j, g) == c ? 0xffffu : key_of(2 * j + 1, g) == c ? 0xffff0000u : 0u;
+                a[j] = keep & __builtin_amdgcn_perm(v.r[2 * j + 1][t / 2], v.r[2 * j][t / 2],
+                                                    (t & 1) ? 0x07060302u : 0x05040100u);
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const f32x4 x = mfma(a, w[rt].f, o[rt][t]);
+                o[rt][t] = sees[rt] ? x : o[rt][t];
+            }
+        }
+    }
+    __device__ static __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+        if constexpr (std::is_same<E, F16>::value)
+            return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c,
+                                                          0, 0, 0);
+        else
+            return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+    }
+    // four consecutive outputs
+    __device__ static __forceinline__ void put4(void *row, int d, float a, float b, float c, float e) {
+        u32x2 v;
+        v[0] = E::pack2(a, b);
+        v[1] = E::pack2(c, e);
+        *(u32x2 *)((uint16_t *)row + d) = v;
+    }
+};
+
+// fp32: stages of 16 keys, one element for each lane of an operand
+template <int D>
+struct Op32 {
+    static constexpr int DIM = D, KEYS = 16, NS = 4, NT = D / 16, NK = D / 16, ROWB = D * 4, ELT = 4;
+    struct Q {
+        f32x4 f[NK];
+    };
+    struct K {
+        f32x4 f[NK];
+    };
+    struct V {
+        f32x4 r[4][NT / 4];
+    };
+    struct P {
+        float f[4];
+    };
+    __device__ static __forceinline__ int key_of(int e, int g) { return 4 * g + e; }
+
+    __device__ static __forceinline__ f32x4 load(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+        return __builtin_bit_cast(f32x4, buf_load16(r, off));
+    }
+    __device__ static __forceinline__ void load_q(Q &q, const void *row, int g) {
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks) q.f[ks] = *(const f32x4 *)((const unsigned char *)row + 64 * ks + 16 * g);
+    }
+    __device__ static __forceinline__ void turn(f32x4 &a, f32x4 &b, const float *cs) {
+        const f32x4 c01 = *(const f32x4 *)cs, c23 = *(const f32x4 *)(cs + 4);
+        float x[4], y[4];
+        rope_rot(a[0], b[0], c01[0], c01[1], x[0], y[0]);
+        rope_rot(a[1], b[1], c01[2], c01[3], x[1], y[1]);
+        rope_rot(a[2], b[2], c23[0], c23[1], x[2], y[2]);
+        rope_rot(a[3], b[3], c23[2], c23[3], x[3], y[3]);
+        a = (f32x4){x[0], x[1], x[2], x[3]};
+        b = (f32x4){y[0], y[1], y[2], y[3]};
+    }
+    __device__ static __forceinline__ void rotate_q(Q &q, const float *cs, int g) {
+#pragma unroll
+        for (int ks = 0; ks < NK / 2; ++ks) turn(q.f[ks], q.f[ks + NK / 2], cs + 2 * (16 * ks + 4 * g));
+    }
+    __device__ static __forceinline__ void load_k(K &k, __amdgpu_buffer_rsrc_t r, uint32_t stride_b, int i, int g) {
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks) k.f[ks] = load(r, (uint32_t)i * stride_b + 16 * g + 64 * ks);
+    }
+    __device__ static __forceinline__ void load_v(V &v, __amdgpu_buffer_rsrc_t r, uint32_t stride_b, int i, int g) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int j = 0; j < NT / 4; ++j)
+                v.r[e][j] = load(r, (uint32_t)key_of(e, g) * stride_b + 4 * NT * i + 16 * j);
+    }
+    __device__ static __forceinline__ void rotate_k(K &k, const float *cs, int n, int i, int g) {
+        const int c = min(i, n - 1);
+#pragma unroll
+        for (int ks = 0; ks < NK / 2; ++ks) turn(k.f[ks], k.f[ks + NK / 2], cs + c * D + 2 * (16 * ks + 4 * g));
+    }
+    __device__ static __forceinline__ void store(const K &k, const V &v, unsigned char *kd, unsigned char *vd, int n,
+                                                 int i, int g) {
+        if (i < n)
+#pragma unroll
+            for (int ks = 0; ks < NK; ++ks) *(f32x4 *)(kd + i * ROWB + 64 * ks + 16 * g) = k.f[ks];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (key_of(e, g) < n)
+#pragma unroll
+                for (int j = 0; j < NT / 4; ++j)
+                    *(f32x4 *)(vd + key_of(e, g) * ROWB + 4 * NT * i + 16 * j) = v.r[e][j];
+    }
+    // four chains of sums, joined: a chain is NK long instead of D
+    __device__ static __forceinline__ void scores(const K &k, const Q &q, float (&s)[NS]) {
+        f32x4 a[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) a[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                a[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.f[ks][c], q.f[ks][c], a[c], 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] = (a[0][e] + a[1][e]) + (a[2][e] + a[3][e]);
+    }
+    __device__ static __forceinline__ void weights(P &w, const float (&p)[NS]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w.f[e] = p[e];
+    }
+    __device__ static __forceinline__ bool finite(const V &v) {
+        bool ok = true;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int d = 0; d < NT; ++d) ok = ok && (__float_as_uint(v.r[e][d / 4][d % 4]) & 0x7f800000u) != 0x7f800000u;
+        return ok;
+    }
+    template <int RT>
+    __device__ static __forceinline__ void accumulate_key(const V &v, const P (&w)[RT], f32x4 (&o)[RT][NT], int c,
+                                                          const bool (&sees)[RT], int g) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const float a = key_of(e, g) == c ? v.r[e][t / 4][t % 4] : 0.f;
+                    const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x4f32(a, w[rt].f[e], o[rt][t], 0, 0, 0);
+                    o[rt][t] = sees[rt] ? x : o[rt][t];
+                }
+    }
+    template <int RT>
+    __device__ static __forceinline__ void accumulate(const V &v, const P (&w)[RT], f32x4 (&o)[RT][NT]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+                    o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.r[e][t / 4][t % 4], w[rt].f[e], o[rt][t], 0, 0, 0);
+    }
+    __device__ static __forceinline__ void put4(void *row, int d, float a, float b, float c, float e) {
+        *(f32x4 *)((float *)row + d) = (f32x4){a, b, c, e};
+    }
+};
+
+}  // namespace dev
+}  // namespace kvr

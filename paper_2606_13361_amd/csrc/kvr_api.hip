@@ -11,54 +11,14 @@
 #include "kvr_internal.hpp"
 
 namespace kvr {
+
 namespace {
-
-constexpr int64_t kMaxTokens = (int64_t)1 << 30;   // rows of Q per call; keeps int32 row math safe
-constexpr int64_t kMaxKeys = (int64_t)1 << 40;
-// Split heuristic for the continuation: aim for this many workgroups on the
-// 256-CU part (two per CU for both kernels), never split the prefix below
-// this many keys per workgroup.
-constexpr int64_t kTargetWorkgroupsStaged = 512;
-constexpr int64_t kTargetWorkgroupsCont = 256;   // split-K-in-workgroup kernel: one per CU (155 KB of LDS)
-constexpr int64_t kMinSplitKeys = 256;
-// longest key range per workgroup for which the row-split continuation is used
-constexpr int64_t kRowsSplitMaxKeys = 640;
-// Many readers on the two-group kernel (one 128 KB workgroup per CU): tiles
-// past the last full round of workgroups are split over the keys, into at
-// most this many splits of at least kReaderMinSplitTiles key tiles each.
-// Costs in units of one whole workgroup, whose time is about kReaderTileUs per
-// key tile: a split workgroup takes 1/ns of it plus kReaderSplitFixed (its own
-// query rows, first tiles and epilogue); a split launch adds the merge launch,
-// kReaderMergeCost, and the fp32 partials written and read back at about
-// kPartialBytesPerUs.
-constexpr int64_t kCus = 256;
-// fp32: 32-row tiles from this many on
-constexpr int64_t kF32WideTiles = 2 * kCus;
-constexpr int64_t kReaderMaxSplits = 16;
-constexpr int64_t kReaderMinSplitTiles = 4;
-constexpr double kReaderSplitFixed = 0.07;
-constexpr double kReaderMergeCost = 0.04;
-constexpr double kReaderTileUs = 2.0;
-// A long continuation on the same kernel: fixed time of a split workgroup and of
-// the merge launch, as its split count is chosen by
-constexpr double kLongSplitFixedUs = 6.0;
-constexpr double kLongMergeUs = 5.0;
-constexpr double kPartialBytesPerUs = 5.0e6;
-
 // bf16 and fp16 share the 16-bit MFMA path; f16() picks the element format
 bool is16(const kvr_desc *d) { return d->dtype == KVR_BF16 || d->dtype == KVR_F16; }
 bool f16(const kvr_desc *d) { return d->dtype == KVR_F16; }
 
-// Continuations of at most kContMaxRows query rows per kv head (decode steps,
-// short suffixes) at bf16 / head_dim 128 use the kernel whose waves split the keys.
-bool use_cont(const kvr_desc *d, int64_t S) {
-    return is16(d) && d->head_dim == 128 && (int64_t)(d->n_q_heads / d->n_kv_heads) * S <= kContMaxRows;
-}
-
-// Prefill and many readers at bf16 / head_dim 128 use the two-group kernel.
-bool use_pp(const kvr_desc *d) { return is16(d) && d->head_dim == 128; }
-
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+}  // namespace
 
 int check_desc(const kvr_desc *d) {
     if (!d) return KVR_ERR_NULL;
@@ -75,6 +35,54 @@ int check_desc(const kvr_desc *d) {
 float eff_scale(const kvr_desc *d) { return d->scale > 0.f ? d->scale : 1.f / sqrtf((float)d->head_dim); }
 
 int elt_bytes(const kvr_desc *d) { return is16(d) ? 2 : 4; }
+
+// RoPE table argument of a call that rotates positions [0, n_pos_needed)
+int check_rope(const kvr_rope *r, int64_t n_pos_needed) {
+    if (!r || !r->cos_sin) return KVR_ERR_NULL;
+    if (r->n_pos < 0 || r->n_pos < n_pos_needed) return KVR_ERR_POSITION;
+    if (!aligned16(r->cos_sin)) return KVR_ERR_ALIGN;
+    return KVR_OK;
+}
+
+namespace {
+
+// Split heuristic for the continuation: aim for this many workgroups on the
+// 256-CU part (two per CU for both kernels), never split the prefix below
+// this many keys per workgroup.
+constexpr int64_t kTargetWorkgroupsStaged = 512;
+constexpr int64_t kTargetWorkgroupsCont = 256;   // split-K-in-workgroup kernel: one per CU (155 KB of LDS)
+constexpr int64_t kMinSplitKeys = 256;
+// longest key range per workgroup for which the row-split continuation is used
+constexpr int64_t kRowsSplitMaxKeys = 640;
+// Many readers on the two-group kernel (one 128 KB workgroup per CU): tiles
+// past the last full round of workgroups are split over the keys, into at
+// most this many splits of at least kReaderMinSplitTiles key tiles each.
+// Costs in units of one whole workgroup, whose time is about kReaderTileUs per
+// key tile: a split workgroup takes 1/ns of it plus kReaderSplitFixed (its own
+// query rows, first tiles and epilogue); a split launch adds the merge launch,
+// kReaderMergeCost, and the fp32 partials written and read back at about
+// kPartialBytesPerUs.
+// fp32: 32-row tiles from this many on
+constexpr int64_t kF32WideTiles = 2 * kCus;
+constexpr int64_t kReaderMaxSplits = 16;
+constexpr int64_t kReaderMinSplitTiles = 4;
+constexpr double kReaderSplitFixed = 0.07;
+constexpr double kReaderMergeCost = 0.04;
+constexpr double kReaderTileUs = 2.0;
+// A long continuation on the same kernel: fixed time of a split workgroup and of
+// the merge launch, as its split count is chosen by
+constexpr double kLongSplitFixedUs = 6.0;
+constexpr double kLongMergeUs = 5.0;
+constexpr double kPartialBytesPerUs = 5.0e6;
+
+// Continuations of at most kContMaxRows query rows per kv head (decode steps,
+// short suffixes) at bf16 / head_dim 128 use the kernel whose waves split the keys.
+bool use_cont(const kvr_desc *d, int64_t S) {
+    return is16(d) && d->head_dim == 128 && (int64_t)(d->n_q_heads / d->n_kv_heads) * S <= kContMaxRows;
+}
+
+// Prefill and many readers at bf16 / head_dim 128 use the two-group kernel.
+bool use_pp(const kvr_desc *d) { return is16(d) && d->head_dim == 128; }
 
 // Query rows per workgroup for a call of `rows` query rows per kv head.  fp32: 32
 // rows read each key once for two column tiles, 16 give twice the workgroups;
@@ -329,14 +337,6 @@ void fill_common(AttnParams &p, const kvr_desc *d) {
     p.new_tok_stride = (int64_t)d->n_kv_heads * d->head_dim;
     p.new_head_stride = d->head_dim;
     p.q_tok_stride = (int64_t)d->n_q_heads * d->head_dim;
-}
-
-// RoPE table argument of a call that rotates positions [0, n_pos_needed)
-int check_rope(const kvr_rope *r, int64_t n_pos_needed) {
-    if (!r || !r->cos_sin) return KVR_ERR_NULL;
-    if (r->n_pos < 0 || r->n_pos < n_pos_needed) return KVR_ERR_POSITION;
-    if (!aligned16(r->cos_sin)) return KVR_ERR_ALIGN;
-    return KVR_OK;
 }
 
 size_t align256(size_t b) { return (b + 255) / 256 * 256; }

@@ -1,0 +1,267 @@
+// readers_api.hip -- host side of kvr_continue_shared, kvr_cache_weigh and
+// kvr_cache_evict: argument validation (before any HIP call), work planning and
+// workspaces, as kvr_api.hip does for the other entry points.
+#include <string.h>
+
+#include "kvr.h"
+#include "kvr_internal.hpp"
+
+namespace kvr {
+namespace {
+
+constexpr int64_t kMaxRows = 0x7fffffff;   // cached rows and query rows of a call: 32-bit on the device
+constexpr int kWaves = 4;                  // of a workgroup
+
+bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// keys of a stage (attn_direct.hpp)
+int64_t stage_keys(const kvr_desc *d) { return d->dtype == KVR_F32 ? 16 : 32; }
+
+// 16-row tiles that a wave holds for `rows` query rows
+int row_tiles(int64_t rows, int most) {
+    const int rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    return rt < most ? rt : most;
+}
+
+// ---- shared
+constexpr int64_t kMinSplitKeys = 256;
+constexpr int64_t kMaxOwnSplits = 16;
+
+struct SharedPlan {
+    int rp, ro;
+    int64_t p_tiles, t_tiles, np, nt, chunk, rows, octs_p, octs_o;
+    size_t ws_bytes;
+};
+
+// Row tiles, key splits and grid of a call: a pure function of the shape, its
+// workspace non-decreasing in L_prefix and tail_capacity.
+bool plan_shared(const kvr_desc *d, int64_t L, int64_t n, int64_t S, int64_t tcap, SharedPlan *out) {
+    SharedPlan s;
+    memset(&s, 0, sizeof s);
+    const int64_t G = d->n_q_heads / d->n_kv_heads;
+    if (n > kMaxRows || S > kMaxTokens || L > kMaxRows || tcap > kMaxRows) return false;
+    if (n > 0 && S > kMaxRows / n / d->n_q_heads) return false;
+    s.rows = n * S * d->n_q_heads;
+    if (s.rows > 0) {
+        const int most = d->dtype == KVR_F32 ? 2 : 4;
+        s.rp = row_tiles(n * S * G, most);
+        s.ro = row_tiles(S * G, most);
+        s.p_tiles = ceil_div(n * S * G, 16 * s.rp);
+        s.t_tiles = ceil_div(S * G, 16 * s.ro);
+        int64_t want = 0;
+        if (L > 0) {
+            const int64_t base = s.p_tiles * d->n_kv_heads;
+            const int64_t step = kWaves * stage_keys(d);
+            want = ceil_div(kCus, base);
+            const int64_t by_keys = ceil_div(L, kMinSplitKeys);
+            if (want > by_keys) want = by_keys;
+            s.chunk = ceil_div(ceil_div(L, want), step) * step;
+            s.np = ceil_div(L, s.chunk);
+        }
+        const int64_t own = n * s.t_tiles * d->n_kv_heads;
+        s.nt = ceil_div(kCus, own);
+        const int64_t by_cap = ceil_div(tcap, kMinSplitKeys);
+        if (s.nt > by_cap) s.nt = by_cap;
+        if (s.nt > kMaxOwnSplits) s.nt = kMaxOwnSplits;
+        if (s.nt < 1) s.nt = 1;
+        s.octs_p = ceil_div(s.np * d->n_kv_heads, 8) * s.p_tiles;
+        s.octs_o = ceil_div(own * s.nt, 8);
+        if ((s.octs_p + s.octs_o) * 8 > kMaxRows) return false;
+        s.ws_bytes = (size_t)(want + s.nt) * (size_t)s.rows * (d->head_dim + 2) * sizeof(float);
+    }
+    *out = s;
+    return true;
+}
+
+// ---- weigh
+struct WeighPlan {
+    int rt;
+    int64_t nsplit, chunk, grid;
+    size_t ws_bytes;
+};
+
+bool plan_weigh(const kvr_desc *d, int64_t L, int64_t S, WeighPlan *out) {
+    WeighPlan w;
+    memset(&w, 0, sizeof w);
+    const int64_t G = d->n_q_heads / d->n_kv_heads;
+    if (L > kMaxRows || S > kMaxRows / G || L + S > kMaxRows) return false;
+    if (S > 0) {
+        const int64_t rows = S * G;
+        w.rt = row_tiles(rows, 4);
+        const int64_t base = ceil_div(rows, 16 * w.rt) * d->n_kv_heads;
+        const int64_t stages = ceil_div(L, stage_keys(d)) + ceil_div(S, stage_keys(d));
+        int64_t want = ceil_div(2 * kCus, base);
+        const int64_t most = ceil_div(stages, 2 * kWaves);
+        if (want > most) want = most;
+        w.chunk = ceil_div(ceil_div(stages, want), kWaves) * kWaves;
+        w.nsplit = ceil_div(stages, w.chunk);
+        w.grid = base * w.nsplit;
+        if (w.grid > kMaxRows) return false;
+        w.ws_bytes = (size_t)want * d->n_kv_heads * rows * 2 * sizeof(float);
+    }
+    *out = w;
+    return true;
+}
+
+// ---- evict
+bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && na && nb && x < y + nb && y < x + na;
+}
+
+int to_status(hipError_t e) { return e == hipSuccess ? KVR_OK : KVR_ERR_DEVICE; }
+
+}  // namespace
+}  // namespace kvr
+
+using namespace kvr;
+
+extern "C" {
+
+size_t kvr_workspace_bytes_shared(const kvr_desc *desc, int64_t L_prefix, int32_t n, int32_t S, int64_t tail_capacity) {
+    SharedPlan s;
+    if (check_desc(desc) != KVR_OK || L_prefix < 0 || n < 0 || S < 0 || tail_capacity < 0) return (size_t)-1;
+    return plan_shared(desc, L_prefix, n, S, tail_capacity, &s) ? s.ws_bytes : (size_t)-1;
+}
+
+int kvr_continue_shared(const kvr_desc *desc, const kvr_rope *rope, const void *Qs, const void *Ks, const void *Vs,
+                        int32_t n, int32_t S, const void *kcache, const void *vcache, int64_t L_prefix, int64_t pos0,
+                        void *ktail, void *vtail, int64_t tail_capacity, const int32_t *tail_len, int32_t append,
+                        void *out, void *ws, size_t ws_bytes, void *stream) {
+    int st = check_desc(desc);
+    if (st) return st;
+    if (n < 0 || S < 0 || L_prefix < 0 || tail_capacity < 0) return KVR_ERR_SHAPE;
+    SharedPlan plan;
+    if (!plan_shared(desc, L_prefix, n, S, tail_capacity, &plan)) return KVR_ERR_SHAPE;
+    if (L_prefix > desc->capacity) return KVR_ERR_CAPACITY;
+    if (append && S > tail_capacity) return KVR_ERR_CAPACITY;
+    if (plan.rows == 0) return KVR_OK;
+    if (!Qs || !Ks || !Vs || !out || !tail_len) return KVR_ERR_NULL;
+    if (L_prefix > 0 && (!kcache || !vcache)) return KVR_ERR_NULL;
+    if (tail_capacity > 0 && (!ktail || !vtail)) return KVR_ERR_NULL;
+    if (rope) {
+        if (pos0 < 0 || pos0 > kMaxKeys) return KVR_ERR_POSITION;
+        if ((st = check_rope(rope, pos0 + tail_capacity + (append ? 0 : S)))) return st;
+    }
+    const void *const ptrs[] = {Qs, Ks, Vs, out, kcache, vcache, ktail, vtail, ws};
+    for (const void *p : ptrs)
+        if (!aligned(p, 16)) return KVR_ERR_ALIGN;
+    if (!aligned(tail_len, 4)) return KVR_ERR_ALIGN;
+    if (!ws || ws_bytes < plan.ws_bytes) return KVR_ERR_WORKSPACE;
+
+    SharedParams p;
+    memset(&p, 0, sizeof p);
+    p.q = Qs; p.kn = Ks; p.vn = Vs; p.kc = kcache; p.vc = vcache; p.kt = ktail; p.vt = vtail;
+    p.len = tail_len;
+    p.out = out;
+    p.ws = (float *)ws;
+    p.rope = rope ? rope->cos_sin : nullptr;
+    p.cap = desc->capacity;
+    p.tcap = tail_capacity;
+    p.L = L_prefix;
+    p.pos0 = pos0;
+    p.chunk = plan.chunk;
+    p.rows = plan.rows;
+    p.scale_log2 = eff_scale(desc) * 1.4426950408889634f;
+    p.n = n;
+    p.S = S;
+    p.n_q_heads = desc->n_q_heads;
+    p.n_kv_heads = desc->n_kv_heads;
+    p.group = desc->n_q_heads / desc->n_kv_heads;
+    p.append = append ? 1 : 0;
+    p.np = (int32_t)plan.np;
+    p.nt = (int32_t)plan.nt;
+    p.nrec = p.np + p.nt;
+    p.p_tiles = (int32_t)plan.p_tiles;
+    p.t_tiles = (int32_t)plan.t_tiles;
+    p.oct_all = (uint32_t)(plan.octs_p + plan.octs_o);
+    p.own_share = (((uint64_t)plan.octs_o << 32) + p.oct_all - 1) / p.oct_all;
+    return to_status(launch_shared(p, desc->head_dim, desc->dtype, plan.rp, plan.ro, (hipStream_t)stream));
+}
+
+size_t kvr_workspace_bytes_weigh(const kvr_desc *desc, int64_t L_prefix, int64_t S) {
+    WeighPlan w;
+    if (check_desc(desc) != KVR_OK || L_prefix < 0 || S < 0) return (size_t)-1;
+    return plan_weigh(desc, L_prefix, S, &w) ? w.ws_bytes : (size_t)-1;
+}
+
+int kvr_cache_weigh(const kvr_desc *desc, const void *Qs, const void *Ks, const void *kcache, int64_t L_prefix,
+                    int64_t S, float *weight, void *ws, size_t ws_bytes, void *stream) {
+    const int st = check_desc(desc);
+    if (st) return st;
+    if (L_prefix < 0 || S < 0) return KVR_ERR_SHAPE;
+    WeighPlan plan;
+    if (!plan_weigh(desc, L_prefix, S, &plan)) return KVR_ERR_SHAPE;
+    if (L_prefix + S > desc->capacity) return KVR_ERR_CAPACITY;
+    if (S == 0) return KVR_OK;
+    if (!Qs || !Ks || !weight || (L_prefix > 0 && !kcache)) return KVR_ERR_NULL;
+    if (!aligned(Qs, 16) || !aligned(Ks, 16) || !aligned(kcache, 16) || !aligned(weight, 4) || !aligned(ws, 16))
+        return KVR_ERR_ALIGN;
+    if (!ws || ws_bytes < plan.ws_bytes) return KVR_ERR_WORKSPACE;
+
+    WeighParams p;
+    memset(&p, 0, sizeof p);
+    p.q = Qs; p.kn = Ks; p.kc = kcache;
+    p.weight = weight;
+    p.ws = (float2 *)ws;
+    p.cap = desc->capacity;
+    p.L = L_prefix;
+    p.S = (int32_t)S;
+    p.n_q_heads = desc->n_q_heads;
+    p.n_kv_heads = desc->n_kv_heads;
+    p.group = desc->n_q_heads / desc->n_kv_heads;
+    p.nsplit = (int32_t)plan.nsplit;
+    p.chunk = (int32_t)plan.chunk;
+    p.scale_log2 = eff_scale(desc) * 1.4426950408889634f;
+    return to_status(launch_weigh(p, desc->head_dim, desc->dtype, plan.rt, (hipStream_t)stream));
+}
+
+size_t kvr_workspace_bytes_evict(const kvr_desc *desc, int64_t L) {
+    if (check_desc(desc) != KVR_OK || L < 0 || L > kMaxRows) return (size_t)-1;
+    return (size_t)desc->n_kv_heads * (size_t)L * sizeof(int32_t);
+}
+
+int kvr_cache_evict(const kvr_desc *desc, const void *kcache, const void *vcache, int64_t L, const float *weight,
+                    int64_t n_first, int64_t n_last, int64_t n_keep, void *kout, void *vout, int64_t capacity_out,
+                    float *weight_out, int32_t *index, void *ws, size_t ws_bytes, void *stream) {
+    const int st = check_desc(desc);
+    if (st) return st;
+    if (L < 0 || L > kMaxRows || n_first < 0 || n_last < 0 || n_keep < 0 || n_keep > L) return KVR_ERR_SHAPE;
+    if (n_first > n_keep || n_last > n_keep - n_first) return KVR_ERR_SHAPE;
+    if (capacity_out < 0 || capacity_out > kMaxKeys) return KVR_ERR_SHAPE;
+    if (L > desc->capacity || n_keep > capacity_out) return KVR_ERR_CAPACITY;
+    if (n_keep == 0) return KVR_OK;
+    if (!kcache || !vcache || !weight || !kout || !vout) return KVR_ERR_NULL;
+    const void *const ptrs[] = {kcache, vcache, kout, vout, ws};
+    for (const void *p : ptrs)
+        if (!aligned(p, 16)) return KVR_ERR_ALIGN;
+    if (!aligned(weight, 4) || !aligned(weight_out, 4) || !aligned(index, 4)) return KVR_ERR_ALIGN;
+    if (!ws || ws_bytes < kvr_workspace_bytes_evict(desc, L)) return KVR_ERR_WORKSPACE;
+    // rows move without an order: no output may share memory with anything else of the call
+    const size_t hkv = (size_t)desc->n_kv_heads, row = (size_t)desc->head_dim * elt_bytes(desc);
+    const struct { const void *p; size_t n; bool out; } buf[] = {
+        {kcache, hkv * (size_t)desc->capacity * row, false}, {vcache, hkv * (size_t)desc->capacity * row, false},
+        {weight, hkv * (size_t)desc->capacity * 4, false},   {kout, hkv * (size_t)capacity_out * row, true},
+        {vout, hkv * (size_t)capacity_out * row, true},      {weight_out, hkv * (size_t)capacity_out * 4, true},
+        {index, hkv * (size_t)n_keep * 4, true},             {ws, hkv * (size_t)n_keep * 4, true}};
+    for (size_t a = 0; a < sizeof buf / sizeof buf[0]; ++a)
+        for (size_t b = 0; b < a; ++b)
+            if ((buf[a].out || buf[b].out) && overlap(buf[a].p, buf[a].n, buf[b].p, buf[b].n)) return KVR_ERR_SHAPE;
+
+    EvictParams p;
+    memset(&p, 0, sizeof p);
+    p.kc = kcache; p.vc = vcache; p.weight = weight;
+    p.ko = kout; p.vo = vout; p.weight_out = weight_out; p.index = index;
+    p.list = (int32_t *)ws;
+    p.cap = desc->capacity;
+    p.cap_out = capacity_out;
+    p.L = (int32_t)L;
+    p.n_first = (int32_t)n_first;
+    p.n_last = (int32_t)n_last;
+    p.n_keep = (int32_t)n_keep;
+    p.n_kv_heads = desc->n_kv_heads;
+    p.row_chunks = desc->head_dim * elt_bytes(desc) / 16;
+    return to_status(launch_evict(p, (hipStream_t)stream));
+}
+
+}  // extern "C"

@@ -28,7 +28,9 @@ EXPORTS = ("kvr_prefill", "kvr_continue", "kvr_continue_append", "kvr_continue_n
            "kvr_q8_bytes", "kvr_quantize_cache", "kvr_continue_q8",
            "kvr_artifact_bytes", "kvr_artifact_save", "kvr_artifact_load",
            "kvr_rope_table", "kvr_rope_apply", "kvr_prefill_rope", "kvr_continue_rope",
-           "kvr_continue_batched_rope", "kvr_workspace_bytes_rope")
+           "kvr_continue_batched_rope", "kvr_workspace_bytes_rope",
+           "kvr_continue_shared", "kvr_workspace_bytes_shared", "kvr_cache_weigh", "kvr_workspace_bytes_weigh",
+           "kvr_cache_evict", "kvr_workspace_bytes_evict")
 
 _TORCH_DTYPE = {KVR_BF16: torch.bfloat16, KVR_F32: torch.float32, KVR_F16: torch.float16}
 
@@ -92,6 +94,16 @@ def load():
                                               P, P, I64, P, P, SZ, P]
     lib.kvr_workspace_bytes_rope.argtypes = [D, I64, I64, ctypes.c_int32]
     lib.kvr_workspace_bytes_rope.restype = SZ
+    I32 = ctypes.c_int32
+    lib.kvr_continue_shared.argtypes = [D, R, P, P, P, I32, I32, P, P, I64, I64, P, P, I64, P, I32, P, P, SZ, P]
+    lib.kvr_workspace_bytes_shared.argtypes = [D, I64, I32, I32, I64]
+    lib.kvr_workspace_bytes_shared.restype = SZ
+    lib.kvr_cache_weigh.argtypes = [D, P, P, P, I64, I64, P, P, SZ, P]
+    lib.kvr_workspace_bytes_weigh.argtypes = [D, I64, I64]
+    lib.kvr_workspace_bytes_weigh.restype = SZ
+    lib.kvr_cache_evict.argtypes = [D, P, P, I64, P, I64, I64, I64, P, P, I64, P, P, P, SZ, P]
+    lib.kvr_workspace_bytes_evict.argtypes = [D, I64]
+    lib.kvr_workspace_bytes_evict.restype = SZ
     lib.kvr_strerror.argtypes = [ctypes.c_int]
     lib.kvr_strerror.restype = ctypes.c_char_p
     lib.kvr_abi_version.argtypes = []
@@ -100,7 +112,8 @@ def load():
               lib.kvr_cache_append,
               lib.kvr_abi_version, lib.kvr_quantize_cache, lib.kvr_continue_q8, lib.kvr_artifact_save,
               lib.kvr_artifact_load, lib.kvr_rope_table, lib.kvr_rope_apply, lib.kvr_prefill_rope,
-              lib.kvr_continue_rope, lib.kvr_continue_batched_rope):
+              lib.kvr_continue_rope, lib.kvr_continue_batched_rope, lib.kvr_continue_shared,
+              lib.kvr_cache_weigh, lib.kvr_cache_evict):
         f.restype = ctypes.c_int
     _lib = lib
     return lib
@@ -453,3 +466,129 @@ def kvr_continue_batched_rope(desc, rope, Qs, Ks, Vs, cu_seqlens, kcache, vcache
     _raise(load().kvr_continue_batched_rope(ctypes.byref(desc), _rope(rope, desc), q, k, v, arr, n, kc, vc,
                                             int(L_prefix), o, wp, wn, _stream(stream)),
            "kvr_continue_batched_rope")
+
+
+# ---------------------------------------------------------------- many readers, later turns
+def _check_typed(t, name, dtype, shape):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s GPU tensor" % (name, dtype))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    return t.data_ptr()
+
+
+def _launch(call, where, stream, first, *others):
+    """call(stream handle) with the tensors' device current; they all have to be on one."""
+    dev = first.device
+    for t in others:
+        if t is not None and t.device != dev:
+            raise ValueError("%s: tensors on %s and %s" % (where, dev, t.device))
+    if isinstance(stream, torch.cuda.Stream) and stream.device != dev:
+        raise ValueError("%s: tensors on %s, the stream is of %s" % (where, dev, stream.device))
+    if dev.index == torch.cuda.current_device():
+        _raise(call(_stream(stream)), where)
+    else:
+        with torch.cuda.device(dev):
+            _raise(call(_stream(stream)), where)
+
+
+def _bytes(nb):
+    if nb == _SIZE_ERR:
+        raise ValueError("invalid layer descriptor or sizes")
+    return nb
+
+
+def kvr_workspace_bytes_shared(desc, L_prefix, n, S, tail_capacity):
+    return _bytes(load().kvr_workspace_bytes_shared(ctypes.byref(desc), int(L_prefix), int(n), int(S),
+                                                    int(tail_capacity)))
+
+
+def workspace_for_shared(desc, L_prefix, n, S, tail_capacity, device="cuda"):
+    """Allocate (with torch) the workspace of kvr_continue_shared."""
+    return torch.empty(kvr_workspace_bytes_shared(desc, L_prefix, n, S, tail_capacity), dtype=torch.uint8, device=device)
+
+
+def kvr_continue_shared(desc, Qs, Ks, Vs, kcache, vcache, L_prefix, ktail, vtail, tail_len, out, ws, rope=None,
+                        pos0=None, append=False, stream=None):
+    """One step of n readers of a shared prefix, each with cached rows of its own.
+
+    Qs, out [n, S, n_q_heads, head_dim]; Ks, Vs [n, S, n_kv_heads, head_dim];
+    ktail, vtail [n, n_kv_heads, tail_capacity, head_dim] (None: the readers have no
+    rows); tail_len: int32 GPU tensor [n].  rope: a RopeTable that rotates the rows
+    at pos0 + tail_len[r] + i (pos0: L_prefix by default)."""
+    Hq, Hkv, d = desc.n_q_heads, desc.n_kv_heads, desc.head_dim
+    if not isinstance(Qs, torch.Tensor) or Qs.dim() != 4:
+        raise ValueError("Qs must be a tensor [n, S, n_q_heads, head_dim]")
+    n, S = Qs.shape[0], Qs.shape[1]
+    q = _check(Qs, "Qs", desc, (n, S, Hq, d))
+    k = _check(Ks, "Ks", desc, (n, S, Hkv, d))
+    v = _check(Vs, "Vs", desc, (n, S, Hkv, d))
+    o = _check(out, "out", desc, (n, S, Hq, d))
+    kc, vc = _cache_ptrs(desc, kcache, vcache, L_prefix > 0)
+    cap, kt, vt = 0, None, None
+    if ktail is not None or vtail is not None:
+        if not isinstance(ktail, torch.Tensor) or ktail.dim() != 4:
+            raise ValueError("ktail must be a tensor [n, n_kv_heads, tail_capacity, head_dim]")
+        cap = ktail.shape[2]
+        kt = _check(ktail, "ktail", desc, (n, Hkv, cap, d))
+        vt = _check(vtail, "vtail", desc, (n, Hkv, cap, d))
+    ln = _check_typed(tail_len, "tail_len", torch.int32, (n,))
+    wp, wn = _workspace(ws)
+    rp = None if rope is None else _rope(rope, desc)
+    at = int(L_prefix if pos0 is None else pos0)
+    _launch(lambda s: load().kvr_continue_shared(ctypes.byref(desc), rp, q, k, v, n, S, kc, vc, int(L_prefix), at, kt,
+                                                 vt, cap, ln, 1 if append else 0, o, wp, wn, s),
+            "kvr_continue_shared", stream, Qs, Ks, Vs, out, kcache, vcache, ktail, vtail, tail_len, ws,
+            None if rope is None else rope.cos_sin)
+
+
+def kvr_workspace_bytes_weigh(desc, L_prefix, S):
+    return _bytes(load().kvr_workspace_bytes_weigh(ctypes.byref(desc), int(L_prefix), int(S)))
+
+
+def workspace_for_weigh(desc, L_prefix, S, device="cuda"):
+    """Allocate (with torch) the workspace of kvr_cache_weigh."""
+    return torch.empty(kvr_workspace_bytes_weigh(desc, L_prefix, S), dtype=torch.uint8, device=device)
+
+
+def kvr_cache_weigh(desc, Qs, Ks, kcache, L_prefix, S, weight, ws, stream=None):
+    """Add to weight [n_kv_heads, capacity] (float32) the attention weight that each row
+    receives from the S tokens at positions L_prefix.. ."""
+    Hq, Hkv, d = desc.n_q_heads, desc.n_kv_heads, desc.head_dim
+    q = _check(Qs, "Qs", desc, (S, Hq, d))
+    k = _check(Ks, "Ks", desc, (S, Hkv, d))
+    kc = _check(kcache, "kcache", desc, (Hkv, desc.capacity, d)) if L_prefix > 0 or kcache is not None else None
+    w = _check_typed(weight, "weight", torch.float32, (Hkv, desc.capacity))
+    wp, wn = _workspace(ws)
+    _launch(lambda s: load().kvr_cache_weigh(ctypes.byref(desc), q, k, kc, int(L_prefix), int(S), w, wp, wn, s),
+            "kvr_cache_weigh", stream, Qs, Ks, kcache, weight, ws)
+
+
+def kvr_workspace_bytes_evict(desc, L):
+    return _bytes(load().kvr_workspace_bytes_evict(ctypes.byref(desc), int(L)))
+
+
+def workspace_for_evict(desc, L, device="cuda"):
+    """Allocate (with torch) the workspace of kvr_cache_evict."""
+    return torch.empty(kvr_workspace_bytes_evict(desc, L), dtype=torch.uint8, device=device)
+
+
+def kvr_cache_evict(desc, kcache, vcache, L, weight, n_keep, kout, vout, n_first=0, n_last=0, weight_out=None,
+                    index=None, ws=None, stream=None):
+    """Copy the n_keep rows of [0, L) with the most weight (the first n_first and the last
+    n_last always) into kout, vout [n_kv_heads, capacity_out, head_dim]; weight_out
+    [n_kv_heads, capacity_out] and index (int32 [n_kv_heads, n_keep]) are optional."""
+    Hkv, d = desc.n_kv_heads, desc.head_dim
+    kc, vc = _cache_ptrs(desc, kcache, vcache, True)
+    w = _check_typed(weight, "weight", torch.float32, (Hkv, desc.capacity))
+    if not isinstance(kout, torch.Tensor) or kout.dim() != 3:
+        raise ValueError("kout must be a tensor [n_kv_heads, capacity_out, head_dim]")
+    cap = kout.shape[1]
+    ko = _check(kout, "kout", desc, (Hkv, cap, d))
+    vo = _check(vout, "vout", desc, (Hkv, cap, d))
+    wo = None if weight_out is None else _check_typed(weight_out, "weight_out", torch.float32, (Hkv, cap))
+    ix = None if index is None else _check_typed(index, "index", torch.int32, (Hkv, n_keep))
+    wp, wn = _workspace(ws)
+    _launch(lambda s: load().kvr_cache_evict(ctypes.byref(desc), kc, vc, int(L), w, int(n_first), int(n_last),
+                                             int(n_keep), ko, vo, cap, wo, ix, wp, wn, s),
+            "kvr_cache_evict", stream, kcache, vcache, weight, kout, vout, weight_out, index, ws)
