@@ -35,7 +35,7 @@ def hipcc():
 
 
 def sources():
-    return sorted(glob.glob(os.path.join(CSRC, "*.hip")))
+    return sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "readers", "*.hip")))
 
 
 def model_sources():

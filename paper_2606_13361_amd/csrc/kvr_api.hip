@@ -11,41 +11,10 @@
 #include "kvr_internal.hpp"
 
 namespace kvr {
-
-namespace {
-// bf16 and fp16 share the 16-bit MFMA path; f16() picks the element format
-bool is16(const kvr_desc *d) { return d->dtype == KVR_BF16 || d->dtype == KVR_F16; }
-bool f16(const kvr_desc *d) { return d->dtype == KVR_F16; }
-
-bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
-}  // namespace
-
-int check_desc(const kvr_desc *d) {
-    if (!d) return KVR_ERR_NULL;
-    if (d->dtype != KVR_BF16 && d->dtype != KVR_F32 && d->dtype != KVR_F16) return KVR_ERR_DTYPE;
-    if (d->n_q_heads <= 0 || d->n_kv_heads <= 0 || d->n_q_heads % d->n_kv_heads != 0) return KVR_ERR_SHAPE;
-    if (d->n_q_heads > 4096) return KVR_ERR_SHAPE;
-    if (d->head_dim != 64 && d->head_dim != 128) return KVR_ERR_SHAPE;
-    if (d->capacity < 0 || d->capacity > kMaxKeys) return KVR_ERR_SHAPE;
-    if (d->reserved != 0) return KVR_ERR_SHAPE;
-    if (isnan(d->scale) || isinf(d->scale)) return KVR_ERR_SHAPE;
-    return KVR_OK;
-}
-
-float eff_scale(const kvr_desc *d) { return d->scale > 0.f ? d->scale : 1.f / sqrtf((float)d->head_dim); }
-
-int elt_bytes(const kvr_desc *d) { return is16(d) ? 2 : 4; }
-
-// RoPE table argument of a call that rotates positions [0, n_pos_needed)
-int check_rope(const kvr_rope *r, int64_t n_pos_needed) {
-    if (!r || !r->cos_sin) return KVR_ERR_NULL;
-    if (r->n_pos < 0 || r->n_pos < n_pos_needed) return KVR_ERR_POSITION;
-    if (!aligned16(r->cos_sin)) return KVR_ERR_ALIGN;
-    return KVR_OK;
-}
-
 namespace {
 
+constexpr int64_t kMaxTokens = (int64_t)1 << 30;   // rows of Q per call; keeps int32 row math safe
+constexpr int64_t kMaxKeys = (int64_t)1 << 40;
 // Split heuristic for the continuation: aim for this many workgroups on the
 // 256-CU part (two per CU for both kernels), never split the prefix below
 // this many keys per workgroup.
@@ -62,6 +31,7 @@ constexpr int64_t kRowsSplitMaxKeys = 640;
 // query rows, first tiles and epilogue); a split launch adds the merge launch,
 // kReaderMergeCost, and the fp32 partials written and read back at about
 // kPartialBytesPerUs.
+constexpr int64_t kCus = 256;
 // fp32: 32-row tiles from this many on
 constexpr int64_t kF32WideTiles = 2 * kCus;
 constexpr int64_t kReaderMaxSplits = 16;
@@ -75,6 +45,10 @@ constexpr double kLongSplitFixedUs = 6.0;
 constexpr double kLongMergeUs = 5.0;
 constexpr double kPartialBytesPerUs = 5.0e6;
 
+// bf16 and fp16 share the 16-bit MFMA path; f16() picks the element format
+bool is16(const kvr_desc *d) { return d->dtype == KVR_BF16 || d->dtype == KVR_F16; }
+bool f16(const kvr_desc *d) { return d->dtype == KVR_F16; }
+
 // Continuations of at most kContMaxRows query rows per kv head (decode steps,
 // short suffixes) at bf16 / head_dim 128 use the kernel whose waves split the keys.
 bool use_cont(const kvr_desc *d, int64_t S) {
@@ -83,6 +57,24 @@ bool use_cont(const kvr_desc *d, int64_t S) {
 
 // Prefill and many readers at bf16 / head_dim 128 use the two-group kernel.
 bool use_pp(const kvr_desc *d) { return is16(d) && d->head_dim == 128; }
+
+bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+
+int check_desc(const kvr_desc *d) {
+    if (!d) return KVR_ERR_NULL;
+    if (d->dtype != KVR_BF16 && d->dtype != KVR_F32 && d->dtype != KVR_F16) return KVR_ERR_DTYPE;
+    if (d->n_q_heads <= 0 || d->n_kv_heads <= 0 || d->n_q_heads % d->n_kv_heads != 0) return KVR_ERR_SHAPE;
+    if (d->n_q_heads > 4096) return KVR_ERR_SHAPE;
+    if (d->head_dim != 64 && d->head_dim != 128) return KVR_ERR_SHAPE;
+    if (d->capacity < 0 || d->capacity > kMaxKeys) return KVR_ERR_SHAPE;
+    if (d->reserved != 0) return KVR_ERR_SHAPE;
+    if (isnan(d->scale) || isinf(d->scale)) return KVR_ERR_SHAPE;
+    return KVR_OK;
+}
+
+float eff_scale(const kvr_desc *d) { return d->scale > 0.f ? d->scale : 1.f / sqrtf((float)d->head_dim); }
+
+int elt_bytes(const kvr_desc *d) { return is16(d) ? 2 : 4; }
 
 // Query rows per workgroup for a call of `rows` query rows per kv head.  fp32: 32
 // rows read each key once for two column tiles, 16 give twice the workgroups;
@@ -337,6 +329,14 @@ void fill_common(AttnParams &p, const kvr_desc *d) {
     p.new_tok_stride = (int64_t)d->n_kv_heads * d->head_dim;
     p.new_head_stride = d->head_dim;
     p.q_tok_stride = (int64_t)d->n_q_heads * d->head_dim;
+}
+
+// RoPE table argument of a call that rotates positions [0, n_pos_needed)
+int check_rope(const kvr_rope *r, int64_t n_pos_needed) {
+    if (!r || !r->cos_sin) return KVR_ERR_NULL;
+    if (r->n_pos < 0 || r->n_pos < n_pos_needed) return KVR_ERR_POSITION;
+    if (!aligned16(r->cos_sin)) return KVR_ERR_ALIGN;
+    return KVR_OK;
 }
 
 size_t align256(size_t b) { return (b + 255) / 256 * 256; }

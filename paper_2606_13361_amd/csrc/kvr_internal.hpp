@@ -160,68 +160,6 @@ bool fused_rows_ok(const kvr_desc *d, int64_t L_prefix, int64_t S);
 int continue_fused_rows(const kvr_desc *d, const QkvRows &rows, const float *cos_sin, void *kcache, void *vcache,
                         int64_t L_prefix, int64_t S, void *out, void *ws, size_t ws_bytes, hipStream_t stream);
 
-// Many readers of one prefix, each with cached rows of its own (shared.hip)
-struct SharedParams {
-    const void *q;          // [n][S][n_q_heads][D]
-    const void *kn, *vn;    // new rows [n][S][n_kv_heads][D]
-    const void *kc, *vc;    // prefix [n_kv_heads][cap][D]
-    void *kt, *vt;          // the readers' own rows [n][n_kv_heads][tcap][D]
-    const int32_t *len;     // device [n]: cached own rows
-    void *out;
-    float *ws;              // partials: O [nrec][rows][D], then (m, l) [nrec][rows][2]; rows as in out
-    const float *rope;      // table, or null
-    int64_t cap, tcap, L, pos0;
-    int64_t chunk;          // prefix keys per split
-    int64_t rows;           // n S n_q_heads
-    uint64_t own_share;     // groups of eight blocks that hold own items, of all groups, times 2^32 (rounded up)
-    uint32_t oct_all;       // all groups
-    float scale_log2;
-    int32_t n, S, n_q_heads, n_kv_heads, group;
-    int32_t append;
-    int32_t np, nt, nrec;   // splits of the prefix and of own rows; np + nt
-    int32_t p_tiles, t_tiles;   // row tiles of a kv head over the prefix, of a reader's kv head over its own rows
-};
-// rp, ro: 16-row tiles that a wave holds in prefix and own items: 1, 2 or 4 (fp32: 1 or 2), ro <= rp
-hipError_t launch_shared(const SharedParams &p, int head_dim, int dtype, int rp, int ro, hipStream_t s);
-
-// Attention weight received by each cached row (weigh.hip)
-struct WeighParams {
-    const void *q;        // [S][n_q_heads][D]
-    const void *kn;       // new keys [S][n_kv_heads][D]
-    const void *kc;       // [n_kv_heads][cap][D]
-    float *weight;        // [n_kv_heads][cap], added to
-    float2 *ws;           // (M, l) [n_kv_heads][nsplit][rows], rows = S group
-    int64_t cap, L;
-    int32_t S, n_q_heads, n_kv_heads, group;
-    int32_t nsplit, chunk;   // key splits of the first pass, of `chunk` stages each
-    float scale_log2;
-};
-// rt: 16-row tiles that a wave of the first pass holds: 1, 2 or 4
-hipError_t launch_weigh(const WeighParams &p, int head_dim, int dtype, int rt, hipStream_t s);
-
-// The cache of the rows with the most weight (evict.hip)
-struct EvictParams {
-    const void *kc, *vc;     // [n_kv_heads][cap][row]
-    const float *weight;     // [n_kv_heads][cap]
-    void *ko, *vo;           // [n_kv_heads][cap_out][row]
-    float *weight_out;       // [n_kv_heads][cap_out], or null
-    int32_t *index;          // [n_kv_heads][n_keep], or null
-    int32_t *list;           // workspace: the kept rows [n_kv_heads][n_keep]
-    int64_t cap, cap_out;
-    int32_t L, n_first, n_last, n_keep;
-    int32_t n_kv_heads, row_chunks;   // 16-byte chunks per row
-};
-hipError_t launch_evict(const EvictParams &p, hipStream_t s);
-
-// Host checks and conversions shared by the entry points (kvr_api.hip)
-int check_desc(const kvr_desc *d);
-int check_rope(const kvr_rope *r, int64_t n_pos_needed);   // the call rotates positions [0, n_pos_needed)
-float eff_scale(const kvr_desc *d);
-int elt_bytes(const kvr_desc *d);
-constexpr int64_t kMaxTokens = (int64_t)1 << 30;   // rows of Q per call; keeps int32 row math safe
-constexpr int64_t kMaxKeys = (int64_t)1 << 40;
-constexpr int64_t kCus = 256;
-
 // row-tile geometry of the two paths
 constexpr int kRowsBf16 = 128;  // query rows per workgroup, bf16 path
 constexpr int kRowsF32 = 32;    // query rows per workgroup, fp32 path (16 when those are few)

@@ -7,7 +7,7 @@
 //   select  one workgroup per kv head: the pick-th largest key by a radix search over
 //           its bytes, then the kept rows' indices in ascending order
 //   copy    the kept rows, their weights and indices
-#include "kvr_internal.hpp"
+#include "readers_internal.hpp"
 
 namespace kvr {
 namespace {

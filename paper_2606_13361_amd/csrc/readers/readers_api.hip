@@ -1,16 +1,26 @@
 // readers_api.hip -- host side of kvr_continue_shared, kvr_cache_weigh and
 // kvr_cache_evict: argument validation (before any HIP call), work planning and
 // workspaces, as kvr_api.hip does for the other entry points.
+#include <math.h>
 #include <string.h>
 
 #include "kvr.h"
-#include "kvr_internal.hpp"
+#include "readers_internal.hpp"
 
 namespace kvr {
 namespace {
 
+constexpr int64_t kMaxTokens = (int64_t)1 << 30;
+constexpr int64_t kMaxKeys = (int64_t)1 << 40;
+constexpr int64_t kCus = 256;
 constexpr int64_t kMaxRows = 0x7fffffff;   // cached rows and query rows of a call: 32-bit on the device
 constexpr int kWaves = 4;                  // of a workgroup
+
+// The library's check of a descriptor: an update of no rows ends after it
+int check_desc(const kvr_desc *d) { return kvr_cache_append(d, nullptr, nullptr, 0, nullptr, nullptr, 0, nullptr); }
+
+float eff_scale(const kvr_desc *d) { return d->scale > 0.f ? d->scale : 1.f / sqrtf((float)d->head_dim); }
+int elt_bytes(const kvr_desc *d) { return d->dtype == KVR_F32 ? 4 : 2; }
 
 bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -141,9 +151,10 @@ int kvr_continue_shared(const kvr_desc *desc, const kvr_rope *rope, const void *
     if (tail_capacity > 0 && (!ktail || !vtail)) return KVR_ERR_NULL;
     if (rope) {
         if (pos0 < 0 || pos0 > kMaxKeys) return KVR_ERR_POSITION;
-        if ((st = check_rope(rope, pos0 + tail_capacity + (append ? 0 : S)))) return st;
+        if (!rope->cos_sin) return KVR_ERR_NULL;
+        if (rope->n_pos < pos0 + tail_capacity + (append ? 0 : S)) return KVR_ERR_POSITION;
     }
-    const void *const ptrs[] = {Qs, Ks, Vs, out, kcache, vcache, ktail, vtail, ws};
+    const void *const ptrs[] = {Qs, Ks, Vs, out, kcache, vcache, ktail, vtail, ws, rope ? rope->cos_sin : nullptr};
     for (const void *p : ptrs)
         if (!aligned(p, 16)) return KVR_ERR_ALIGN;
     if (!aligned(tail_len, 4)) return KVR_ERR_ALIGN;

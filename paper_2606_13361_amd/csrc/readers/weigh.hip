@@ -14,6 +14,7 @@
 #include <type_traits>
 
 #include "attn_direct.hpp"
+#include "readers_internal.hpp"
 
 namespace kvr {
 namespace {

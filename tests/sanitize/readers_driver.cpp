@@ -12,6 +12,7 @@
 
 #include "kvr.h"
 #include "kvr_internal.hpp"
+#include "readers/readers_internal.hpp"
 
 static int g_launches = 0, g_bad = 0;
 static size_t g_ws_given = 0;

@@ -22,7 +22,7 @@ def test_readers_host_code_under_sanitizers(tmp_path):
     host = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
             "-Xarch_host", "-fno-sanitize-recover=all", "-Xarch_host", "-fno-omit-frame-pointer"]
     objs = []
-    for src in (os.path.join(CSRC, "kvr_api.hip"), os.path.join(CSRC, "readers_api.hip"),
+    for src in (os.path.join(CSRC, "kvr_api.hip"), os.path.join(CSRC, "readers", "readers_api.hip"),
                 os.path.join(SAN, "readers_driver.cpp")):
         obj = str(tmp_path / (os.path.basename(src) + ".o"))
         subprocess.run([hipcc, "-x", "hip", "-c", "-fPIC", "--offload-arch=gfx950", "-O1", "-g", "-std=c++17",
