@@ -432,7 +432,8 @@ size_t kvr_workspace_bytes_weigh(const kvr_desc *desc, int64_t L_prefix, int64_t
  *   n_keep <= capacity_out (KVR_ERR_CAPACITY).  No output may overlap another
  *   buffer of the call (KVR_ERR_SHAPE).  n_keep == 0 is a no-op.
  *   weight, weight_out and index need 4-byte alignment.
- *   ws: kvr_workspace_bytes_evict(desc, L) bytes.
+ *   ws: kvr_workspace_bytes_evict(desc, L) bytes (may be NULL when that is 0: up to
+ *   32768 rows).
  */
 int kvr_cache_evict(const kvr_desc *desc, const void *kcache, const void *vcache, int64_t L, const float *weight,
                     int64_t n_first, int64_t n_last, int64_t n_keep, void *kout, void *vout, int64_t capacity_out,

@@ -76,25 +76,31 @@ struct Op16 {
 #pragma unroll
         for (int ks = 0; ks < NK / 2; ++ks) rope_rot8<E>(q.f[ks], q.f[ks + NK / 2], cs + 2 * (32 * ks + 8 * g));
     }
+    // PARTS = 1: a stage of at most 16 rows, the other part zeros
+    template <int PARTS = 2>
     __device__ static __forceinline__ void load_k(K &k, __amdgpu_buffer_rsrc_t r, uint32_t stride_b, int i, int g) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int ks = 0; ks < NK; ++ks)
-                k.f[h][ks] = buf_load16(r, (uint32_t)(16 * h + i) * stride_b + 16 * g + 64 * ks);
+                k.f[h][ks] = h < PARTS ? buf_load16(r, (uint32_t)(16 * h + i) * stride_b + 16 * g + 64 * ks)
+                                       : (u32x4){0u, 0u, 0u, 0u};
     }
+    template <int PARTS = 2>
     __device__ static __forceinline__ void load_v(V &v, __amdgpu_buffer_rsrc_t r, uint32_t stride_b, int i, int g) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const uint32_t off = (uint32_t)key_of(e, g) * stride_b + 2 * NT * i;
-            if constexpr (NT == 8) v.r[e] = buf_load16(r, off);
+            if (e >= 4 * PARTS) v.r[e] = vrow(0);
+            else if constexpr (NT == 8) v.r[e] = buf_load16(r, off);
             else v.r[e] = __builtin_amdgcn_raw_buffer_load_b64(r, (int)off, 0, 0);
         }
     }
     // new key rows: position of key c of the stage is that of table row cs + c * D
+    template <int PARTS = 2>
     __device__ static __forceinline__ void rotate_k(K &k, const float *cs, int n, int i, int g) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < PARTS; ++h) {
             const int c = min(16 * h + i, n - 1);      // a row past the last is masked: any table row
 #pragma unroll
             for (int ks = 0; ks < NK / 2; ++ks)
@@ -102,16 +108,17 @@ struct Op16 {
         }
     }
     // rows [0, n) of the stage into consecutive rows of a cache
+    template <int PARTS = 2>
     __device__ static __forceinline__ void store(const K &k, const V &v, unsigned char *kd, unsigned char *vd, int n,
                                                  int i, int g) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < PARTS; ++h)
             if (16 * h + i < n)
 #pragma unroll
                 for (int ks = 0; ks < NK; ++ks)
                     *(u32x4 *)(kd + (16 * h + i) * ROWB + 64 * ks + 16 * g) = k.f[h][ks];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < 4 * PARTS; ++e)
             if (key_of(e, g) < n) *(vrow *)(vd + key_of(e, g) * ROWB + 2 * NT * i) = v.r[e];
     }
     __device__ static __forceinline__ void scores(const K &k, const Q &q, float (&s)[NS]) {
@@ -137,25 +144,41 @@ struct Op16 {
     }
     // whether every value of the stage is a number (the exponent's bits are not all set)
     __device__ static __forceinline__ bool finite(const V &v) {
+        bool ok = true;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ok = ok && finite_words(v.r[e]);
+        return ok;
+    }
+    template <class W>
+    __device__ static __forceinline__ bool finite_words(const W &w) {
         constexpr uint32_t ex = std::is_same<E, F16>::value ? 0x7c00u : 0x7f80u;
         bool ok = true;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-#pragma unroll
-            for (int j = 0; j < NT / 2; ++j)
-                ok = ok && (v.r[e][j] & ex) != ex && (v.r[e][j] >> 16 & ex) != ex;
+        for (int j = 0; j < (int)(sizeof(W) / 4); ++j) ok = ok && (w[j] & ex) != ex && (w[j] >> 16 & ex) != ex;
         return ok;
+    }
+    // an operand of eight keys with zeros in the place of every key but c
+    __device__ static __forceinline__ u32x4 only_key(u32x4 a, int c, int g) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            a[j] &= key_of(2 * j, g) == c ? 0xffffu : key_of(2 * j + 1, g) == c ? 0xffff0000u : 0u;
+        return a;
+    }
+    __device__ static __forceinline__ void rotate8(u32x4 &lo, u32x4 &hi, const float *cs) { rope_rot8<E>(lo, hi, cs); }
+    // operand t of V^T: elements t of keys 2j (low half) and 2j + 1 (high half)
+    __device__ static __forceinline__ u32x4 column(const V &v, int t) {
+        u32x4 a;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            a[j] = __builtin_amdgcn_perm(v.r[2 * j + 1][t / 2], v.r[2 * j][t / 2], (t & 1) ? 0x07060302u : 0x05040100u);
+        return a;
     }
     // o[rt][t] += V^T P^T of every tile
     template <int RT>
     __device__ static __forceinline__ void accumulate(const V &v, const P (&w)[RT], f32x4 (&o)[RT][NT]) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            u32x4 a;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)      // elements t of keys 2j (low half) and 2j + 1 (high half)
-                a[j] = __builtin_amdgcn_perm(v.r[2 * j + 1][t / 2], v.r[2 * j][t / 2],
-                                             (t & 1) ? 0x07060302u : 0x05040100u);
+            const u32x4 a = column(v, t);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) o[rt][t] = mfma(a, w[rt].f, o[rt][t]);
         }
@@ -166,13 +189,7 @@ struct Op16 {
                                                           const bool (&sees)[RT], int g) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            u32x4 a;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t keep = key_of(2 * j, g) == c ? 0xffffu : key_of(2 * j + 1, g) == c ? 0xffff0000u : 0u;
-                a[j] = keep & __builtin_amdgcn_perm(v.r[2 * j + 1][t / 2], v.r[2 * j][t / 2],
-                                                    (t & 1) ? 0x07060302u : 0x05040100u);
-            }
+            const u32x4 a = only_key(column(v, t), c, g);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 const f32x4 x = mfma(a, w[rt].f, o[rt][t]);
@@ -235,10 +252,12 @@ struct Op32 {
 #pragma unroll
         for (int ks = 0; ks < NK / 2; ++ks) turn(q.f[ks], q.f[ks + NK / 2], cs + 2 * (16 * ks + 4 * g));
     }
+    template <int PARTS = 1>
     __device__ static __forceinline__ void load_k(K &k, __amdgpu_buffer_rsrc_t r, uint32_t stride_b, int i, int g) {
 #pragma unroll
         for (int ks = 0; ks < NK; ++ks) k.f[ks] = load(r, (uint32_t)i * stride_b + 16 * g + 64 * ks);
     }
+    template <int PARTS = 1>
     __device__ static __forceinline__ void load_v(V &v, __amdgpu_buffer_rsrc_t r, uint32_t stride_b, int i, int g) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -246,11 +265,13 @@ struct Op32 {
             for (int j = 0; j < NT / 4; ++j)
                 v.r[e][j] = load(r, (uint32_t)key_of(e, g) * stride_b + 4 * NT * i + 16 * j);
     }
+    template <int PARTS = 1>
     __device__ static __forceinline__ void rotate_k(K &k, const float *cs, int n, int i, int g) {
         const int c = min(i, n - 1);
 #pragma unroll
         for (int ks = 0; ks < NK / 2; ++ks) turn(k.f[ks], k.f[ks + NK / 2], cs + c * D + 2 * (16 * ks + 4 * g));
     }
+    template <int PARTS = 1>
     __device__ static __forceinline__ void store(const K &k, const V &v, unsigned char *kd, unsigned char *vd, int n,
                                                  int i, int g) {
         if (i < n)

@@ -27,18 +27,15 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // keys of a stage (attn_direct.hpp)
 int64_t stage_keys(const kvr_desc *d) { return d->dtype == KVR_F32 ? 16 : 32; }
 
-// 16-row tiles that a wave holds for `rows` query rows
-int row_tiles(int64_t rows, int most) {
-    const int rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    return rt < most ? rt : most;
-}
+// query rows of a workgroup (readers_internal.hpp)
+int64_t way_rows(int way) { return way > kByRows ? 64 * (way - kByRows) : 16 * way; }
 
 // ---- shared
 constexpr int64_t kMinSplitKeys = 256;
 constexpr int64_t kMaxOwnSplits = 16;
 
 struct SharedPlan {
-    int rp, ro;
+    int pw, ow;
     int64_t p_tiles, t_tiles, np, nt, chunk, rows, octs_p, octs_o;
     size_t ws_bytes;
 };
@@ -53,11 +50,12 @@ bool plan_shared(const kvr_desc *d, int64_t L, int64_t n, int64_t S, int64_t tca
     if (n > 0 && S > kMaxRows / n / d->n_q_heads) return false;
     s.rows = n * S * d->n_q_heads;
     if (s.rows > 0) {
-        const int most = d->dtype == KVR_F32 ? 2 : 4;
-        s.rp = row_tiles(n * S * G, most);
-        s.ro = row_tiles(S * G, most);
-        s.p_tiles = ceil_div(n * S * G, 16 * s.rp);
-        s.t_tiles = ceil_div(S * G, 16 * s.ro);
+        const int64_t rows_p = n * S * G, rows_o = S * G;
+        const bool f32 = d->dtype == KVR_F32;
+        s.pw = rows_p <= 16 ? 1 : f32 ? 2 : kByRows + (rows_p <= 64 ? 1 : 2);
+        s.ow = rows_o <= 16 ? 1 : f32 ? 2 : kByRows + 1;
+        s.p_tiles = ceil_div(rows_p, way_rows(s.pw));
+        s.t_tiles = ceil_div(rows_o, way_rows(s.ow));
         int64_t want = 0;
         if (L > 0) {
             const int64_t base = s.p_tiles * d->n_kv_heads;
@@ -85,7 +83,7 @@ bool plan_shared(const kvr_desc *d, int64_t L, int64_t n, int64_t S, int64_t tca
 
 // ---- weigh
 struct WeighPlan {
-    int rt;
+    int way, held;
     int64_t nsplit, chunk, grid;
     size_t ws_bytes;
 };
@@ -97,8 +95,8 @@ bool plan_weigh(const kvr_desc *d, int64_t L, int64_t S, WeighPlan *out) {
     if (L > kMaxRows || S > kMaxRows / G || L + S > kMaxRows) return false;
     if (S > 0) {
         const int64_t rows = S * G;
-        w.rt = row_tiles(rows, 4);
-        const int64_t base = ceil_div(rows, 16 * w.rt) * d->n_kv_heads;
+        w.way = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 || d->dtype == KVR_F32 ? 4 : kByRows + (rows <= 128 ? 2 : 4);
+        const int64_t base = ceil_div(rows, way_rows(w.way)) * d->n_kv_heads;
         const int64_t stages = ceil_div(L, stage_keys(d)) + ceil_div(S, stage_keys(d));
         int64_t want = ceil_div(2 * kCus, base);
         const int64_t most = ceil_div(stages, 2 * kWaves);
@@ -106,6 +104,8 @@ bool plan_weigh(const kvr_desc *d, int64_t L, int64_t S, WeighPlan *out) {
         w.chunk = ceil_div(ceil_div(stages, want), kWaves) * kWaves;
         w.nsplit = ceil_div(stages, w.chunk);
         w.grid = base * w.nsplit;
+        // second pass: keys held in registers serve every row, as long as the workgroups fill the part
+        w.held = ceil_div(stages, kWaves * 2) * d->n_kv_heads >= 2 * kCus ? 2 : 1;
         if (w.grid > kMaxRows) return false;
         w.ws_bytes = (size_t)want * d->n_kv_heads * rows * 2 * sizeof(float);
     }
@@ -114,6 +114,8 @@ bool plan_weigh(const kvr_desc *d, int64_t L, int64_t S, WeighPlan *out) {
 }
 
 // ---- evict
+constexpr int64_t kRowsPerPart = 16;   // at least, of a workgroup that searches on its own
+
 bool overlap(const void *a, size_t na, const void *b, size_t nb) {
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
     return a && b && na && nb && x < y + nb && y < x + na;
@@ -187,7 +189,7 @@ int kvr_continue_shared(const kvr_desc *desc, const kvr_rope *rope, const void *
     p.t_tiles = (int32_t)plan.t_tiles;
     p.oct_all = (uint32_t)(plan.octs_p + plan.octs_o);
     p.own_share = (((uint64_t)plan.octs_o << 32) + p.oct_all - 1) / p.oct_all;
-    return to_status(launch_shared(p, desc->head_dim, desc->dtype, plan.rp, plan.ro, (hipStream_t)stream));
+    return to_status(launch_shared(p, desc->head_dim, desc->dtype, plan.pw, plan.ow, (hipStream_t)stream));
 }
 
 size_t kvr_workspace_bytes_weigh(const kvr_desc *desc, int64_t L_prefix, int64_t S) {
@@ -224,12 +226,12 @@ int kvr_cache_weigh(const kvr_desc *desc, const void *Qs, const void *Ks, const 
     p.nsplit = (int32_t)plan.nsplit;
     p.chunk = (int32_t)plan.chunk;
     p.scale_log2 = eff_scale(desc) * 1.4426950408889634f;
-    return to_status(launch_weigh(p, desc->head_dim, desc->dtype, plan.rt, (hipStream_t)stream));
+    return to_status(launch_weigh(p, desc->head_dim, desc->dtype, plan.way, plan.held, (hipStream_t)stream));
 }
 
 size_t kvr_workspace_bytes_evict(const kvr_desc *desc, int64_t L) {
     if (check_desc(desc) != KVR_OK || L < 0 || L > kMaxRows) return (size_t)-1;
-    return (size_t)desc->n_kv_heads * (size_t)L * sizeof(int32_t);
+    return L <= kHeldRows ? 0 : (size_t)desc->n_kv_heads * (size_t)L * sizeof(int32_t);
 }
 
 int kvr_cache_evict(const kvr_desc *desc, const void *kcache, const void *vcache, int64_t L, const float *weight,
@@ -247,14 +249,15 @@ int kvr_cache_evict(const kvr_desc *desc, const void *kcache, const void *vcache
     for (const void *p : ptrs)
         if (!aligned(p, 16)) return KVR_ERR_ALIGN;
     if (!aligned(weight, 4) || !aligned(weight_out, 4) || !aligned(index, 4)) return KVR_ERR_ALIGN;
-    if (!ws || ws_bytes < kvr_workspace_bytes_evict(desc, L)) return KVR_ERR_WORKSPACE;
+    const size_t need = kvr_workspace_bytes_evict(desc, L);
+    if (need && (!ws || ws_bytes < need)) return KVR_ERR_WORKSPACE;
     // rows move without an order: no output may share memory with anything else of the call
     const size_t hkv = (size_t)desc->n_kv_heads, row = (size_t)desc->head_dim * elt_bytes(desc);
     const struct { const void *p; size_t n; bool out; } buf[] = {
         {kcache, hkv * (size_t)desc->capacity * row, false}, {vcache, hkv * (size_t)desc->capacity * row, false},
         {weight, hkv * (size_t)desc->capacity * 4, false},   {kout, hkv * (size_t)capacity_out * row, true},
         {vout, hkv * (size_t)capacity_out * row, true},      {weight_out, hkv * (size_t)capacity_out * 4, true},
-        {index, hkv * (size_t)n_keep * 4, true},             {ws, hkv * (size_t)n_keep * 4, true}};
+        {index, hkv * (size_t)n_keep * 4, true},             {ws, need, true}};
     for (size_t a = 0; a < sizeof buf / sizeof buf[0]; ++a)
         for (size_t b = 0; b < a; ++b)
             if ((buf[a].out || buf[b].out) && overlap(buf[a].p, buf[a].n, buf[b].p, buf[b].n)) return KVR_ERR_SHAPE;
@@ -272,6 +275,10 @@ int kvr_cache_evict(const kvr_desc *desc, const void *kcache, const void *vcache
     p.n_keep = (int32_t)n_keep;
     p.n_kv_heads = desc->n_kv_heads;
     p.row_chunks = desc->head_dim * elt_bytes(desc) / 16;
+    while ((1 << p.chunk_bits) < p.row_chunks) ++p.chunk_bits;
+    // workgroups of a kv head: all compute units, unless that leaves one too few rows
+    const int64_t parts = ceil_div(n_keep, kRowsPerPart), most = kCus / desc->n_kv_heads;
+    p.parts = (int32_t)(parts < most ? parts : most > 1 ? most : 1);
     return to_status(launch_evict(p, (hipStream_t)stream));
 }
 

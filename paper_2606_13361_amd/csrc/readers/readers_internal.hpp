@@ -31,8 +31,11 @@ struct SharedParams {
     int32_t np, nt, nrec;   // splits of the prefix and of own rows; np + nt
     int32_t p_tiles, t_tiles;   // row tiles of a kv head over the prefix, of a reader's kv head over its own rows
 };
-// rp, ro: 16-row tiles that a wave holds in prefix and own items: 1, 2 or 4 (fp32: 1 or 2), ro <= rp
-hipError_t launch_shared(const SharedParams &p, int head_dim, int dtype, int rp, int ro, hipStream_t s);
+// pw, ow: the ways of prefix and own items, ow <= pw.  1, 2: the four waves share 16 or 32
+// query rows and split the keys (2: fp32 only); kByRows + 1, + 2: each wave has 16 or 32
+// rows of its own (16-bit only; own items: + 1)
+constexpr int kByRows = 10;
+hipError_t launch_shared(const SharedParams &p, int head_dim, int dtype, int pw, int ow, hipStream_t s);
 
 // Attention weight received by each cached row (weigh.hip)
 struct WeighParams {
@@ -46,8 +49,10 @@ struct WeighParams {
     int32_t nsplit, chunk;   // key splits of the first pass, of `chunk` stages each
     float scale_log2;
 };
-// rt: 16-row tiles that a wave of the first pass holds: 1, 2 or 4
-hipError_t launch_weigh(const WeighParams &p, int head_dim, int dtype, int rt, hipStream_t s);
+// way of the first pass: 1, 2, 4: the four waves share that many 16-row tiles and split the
+// keys; kByRows + 2, + 4: each wave has that many of its own (16-bit only).  held: key stages
+// that a wave of the second pass holds, 1 or 2
+hipError_t launch_weigh(const WeighParams &p, int head_dim, int dtype, int way, int held, hipStream_t s);
 
 // The cache of the rows with the most weight (evict.hip)
 struct EvictParams {
@@ -56,11 +61,14 @@ struct EvictParams {
     void *ko, *vo;           // [n_kv_heads][cap_out][row]
     float *weight_out;       // [n_kv_heads][cap_out], or null
     int32_t *index;          // [n_kv_heads][n_keep], or null
-    int32_t *list;           // workspace: the kept rows [n_kv_heads][n_keep]
+    int32_t *list;           // L > kHeldRows: workspace, the kept rows [n_kv_heads][n_keep]
     int64_t cap, cap_out;
     int32_t L, n_first, n_last, n_keep;
-    int32_t n_kv_heads, row_chunks;   // 16-byte chunks per row
+    int32_t n_kv_heads;
+    int32_t parts;                    // L <= kHeldRows: workgroups per kv head
+    int32_t row_chunks, chunk_bits;   // 16-byte chunks per row, 2^chunk_bits
 };
+constexpr int64_t kHeldRows = 32768;   // longest cache whose weights a workgroup holds in registers
 hipError_t launch_evict(const EvictParams &p, hipStream_t s);
 
 }  // namespace kvr

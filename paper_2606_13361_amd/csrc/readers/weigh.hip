@@ -4,16 +4,20 @@
 //   weight[g][j] += sum_(i, h of g) 2^(c q_ih . k_j - M_ih) / l_ih,   c = scale log2(e)
 //
 // A row's normalizer (M, l) covers all its keys, so there are two passes over the
-// keys, both matrix products of K and Q^T (attn_direct.hpp: K straight to registers):
-//   stats  a wave holds 16 RT query rows and walks its share of the keys; each lane
-//          keeps the running maximum and sum of its own keys, joined at the end
-//   sums   a wave holds 64 keys and walks all query rows of its kv head; the weights
+// keys, both matrix products of K and Q^T:
+//   stats  a wave holds 16 RT query rows and walks keys; each lane keeps the running
+//          reference and sum of its own keys, joined at the end.  Up to 64 rows of a kv
+//          head (and fp32): the four waves hold the same rows and split the keys, K
+//          straight from memory (attn_direct.hpp).  More: each wave has rows of its own
+//          and the four share the keys' stages in LDS (attn_ring.hpp).
+//   sums   a wave holds HELD stages of keys and walks all query rows of its kv head,
+//          which the four waves share in LDS (fp32: straight from memory); the weights
 //          of its keys add up in registers and are added to the buffer once
 // Every sum has a fixed order and every buffer element one writer: results are
 // reproducible bit for bit.
 #include <type_traits>
 
-#include "attn_direct.hpp"
+#include "attn_ring.hpp"
 #include "readers_internal.hpp"
 
 namespace kvr {
@@ -59,6 +63,28 @@ __device__ __forceinline__ void mask(float (&s)[OP::NS], int lim, int g) {
         if (OP::key_of(e, g) > lim) s[e] = -INFINITY;
 }
 
+constexpr float kSlack = 60.f;
+
+// A stage's scores into the lane's running reference and sum
+template <class OP>
+__device__ __forceinline__ void add_scores(const float (&s)[OP::NS], float c2, float &m, float &l) {
+    float mx = s[0];
+#pragma unroll
+    for (int e = 1; e < OP::NS; ++e) mx = fmaxf(mx, s[e]);
+    mx *= c2;
+    // The sum's reference need not be the maximum, only near enough: 2^31 terms of up to
+    // 2^kSlack stay below the type's largest value, and nothing is rounded differently for it
+    if (__ballot(mx > m + kSlack)) {
+        const float mn = fmaxf(m, mx);
+        l *= __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < OP::NS; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c2, -m));
+    l += sum;
+}
+
 // block: (row tile, split, kv head), kv head fastest.  A split's key range is p.chunk
 // stages; the last one ends with the new rows.
 template <class OP, int RT>
@@ -98,14 +124,7 @@ __global__ __launch_bounds__(256) void weigh_stats_kernel(const WeighParams p) {
             float s[OP::NS];
             OP::scores(kk, q[rt], s);
             if (nw || n < OP::KEYS) mask<OP>(s, nw ? min(n - 1, tok[rt] - c0) : n - 1, g);
-            float mx = s[0];
-#pragma unroll
-            for (int e = 1; e < OP::NS; ++e) mx = fmaxf(mx, s[e]);
-            const float mn = fmaxf(m[rt], mx * c2);
-            l[rt] *= __builtin_amdgcn_exp2f(m[rt] - mn);
-            m[rt] = mn;
-#pragma unroll
-            for (int e = 0; e < OP::NS; ++e) l[rt] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c2, -mn));
+            add_scores<OP>(s, c2, m[rt], l[rt]);
         }
     };
     int t = t0 + wave;
@@ -140,65 +159,117 @@ __global__ __launch_bounds__(256) void weigh_stats_kernel(const WeighParams p) {
     }
 }
 
-constexpr int ROWS_AT_ONCE = 1024;      // normalizers held in LDS
-constexpr int HELD = 2;                 // stages of keys that a wave holds
-
-template <class OP>
-__global__ __launch_bounds__(256) void weigh_sum_kernel(const WeighParams p) {
-    __shared__ float2 norm[ROWS_AT_ONCE];
+// The same with rows of its own for every wave (64 RT a workgroup) and the stages' K
+// rows shared in LDS
+template <class OP, class RG, int RT>
+__global__ __launch_bounds__(256) void weigh_stats_rows_kernel(const WeighParams p) {
+    constexpr int SLOTS = 3;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[SLOTS * RG::HALF];
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int hd = blockIdx.x % p.n_kv_heads;
+    uint32_t b = blockIdx.x;
+    const int hd = b % p.n_kv_heads;
+    b /= p.n_kv_heads;
+    const int split = b % p.nsplit, tile = b / p.nsplit;
     const int G = p.group, rows = p.S * G;
-    const Keys<OP> keys(p, hd);
-    const int n_all = keys.n_pre + (p.S + OP::KEYS - 1) / OP::KEYS;
-    const int t0 = ((int)(blockIdx.x / p.n_kv_heads) * WAVES + wave) * HELD;
-    const float c2 = p.scale_log2;
-    typename OP::K k[HELD];
-    float acc[HELD][OP::NS];
+    typename OP::Q q[RT];
+    float m[RT], l[RT];
+    int tok[RT];
 #pragma unroll
-    for (int h = 0; h < HELD; ++h) {
-        keys.load(k[h], t0 + h, t0 + h < n_all ? keys.count(t0 + h) : 0, i, g);
-#pragma unroll
-        for (int e = 0; e < OP::NS; ++e) acc[h][e] = 0.f;
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = min(((tile * WAVES + wave) * RT + rt) * 16 + i, rows - 1);
+        tok[rt] = r / G;
+        OP::load_q(q[rt], (const unsigned char *)p.q + ((int64_t)tok[rt] * p.n_q_heads + hd * G + (r - tok[rt] * G)) * OP::ROWB, g);
+        m[rt] = -1e30f;
+        l[rt] = 0.f;
     }
-    for (int r0 = 0; r0 < rows; r0 += ROWS_AT_ONCE) {
-        const int nr = min(rows - r0, ROWS_AT_ONCE);
-        if (r0) __syncthreads();
-        for (int r = threadIdx.x; r < nr; r += 256) {
-            const float2 *src = p.ws + (int64_t)hd * p.nsplit * rows + r0 + r;
-            float M = -1e30f, sum = 0.f;
-            for (int s = 0; s < p.nsplit; ++s) {
-                const float2 v = src[(int64_t)s * rows];
-                const float mn = fmaxf(M, v.x);
-                sum = sum * __builtin_amdgcn_exp2f(M - mn) + v.y * __builtin_amdgcn_exp2f(v.x - mn);
+    const Keys<OP> keys(p, hd);
+    const int last_tok = (min((tile + 1) * WAVES * RT * 16, rows) - 1) / G;      // beyond it no new row is seen
+    const int n_all = keys.n_pre + last_tok / OP::KEYS + 1;
+    const int t0 = split * p.chunk;
+    const int t1 = split == p.nsplit - 1 ? n_all : min(t0 + p.chunk, n_all);
+    const uint32_t ka = RG::row_at(i, g);
+    const float c2 = p.scale_log2;
+    auto load = [&](int t, int slot) {
+        const uint64_t first = (uint64_t)keys.first(t);
+        if (keys.is_new(t)) RG::load(keys.kn + first * keys.new_b, keys.new_b, keys.count(t), lds + slot * RG::HALF, wave, lane);
+        else RG::load(keys.kc + first * OP::ROWB, OP::ROWB, keys.count(t), lds + slot * RG::HALF, wave, lane);
+    };
+    if (t0 < t1) load(t0, 0);
+    if (t0 + 1 < t1) load(t0 + 1, 1);
+    int slot = 0;
+    for (int t = t0; t < t1; ++t) {
+        if (t + 1 < t1) wait_vmcnt<RG::LOADS>();
+        else wait_vmcnt<0>();
+        barrier_lds();      // the stage has landed, the slot of the one before is free
+        if (t + 2 < t1) load(t + 2, slot == 0 ? 2 : slot - 1);
+        const unsigned char *st = lds + slot * RG::HALF;
+        const int n = keys.count(t);
+        const bool nw = keys.is_new(t);
+        const int c0 = (int)keys.first(t);
+        typename OP::K k;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int ks = 0; ks < OP::NK; ++ks) k.f[h][ks] = RG::row_frag(st, ka, h, ks);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float s[OP::NS];
+            OP::scores(k, q[rt], s);
+            if (nw || n < OP::KEYS) mask<OP>(s, nw ? min(n - 1, tok[rt] - c0) : n - 1, g);
+            add_scores<OP>(s, c2, m[rt], l[rt]);
+        }
+        slot = slot == SLOTS - 1 ? 0 : slot + 1;
+    }
+    // the four lanes of a row
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const float M = quad_max(m[rt]);
+        const float sum = quad_sum(l[rt] * __builtin_amdgcn_exp2f(m[rt] - M));
+        const int row = ((tile * WAVES + wave) * RT + rt) * 16 + i;
+        if (g == 0 && row < rows) p.ws[((int64_t)hd * p.nsplit + split) * rows + row] = make_float2(M, sum);
+    }
+}
+
+constexpr int ROWS_AT_ONCE = 1024;      // normalizers held in LDS
+
+// norm[r] = M + log2(l) of rows r0 .. r0 + nr - 1 of a kv head, joined from its splits by
+// eight lanes a row: a weight is one 2^x.  Rounding that exponent is an error of the size
+// that the score has already.  Rows up to `padded` get weight 0.
+__device__ __forceinline__ void join_norms(const WeighParams &p, float *norm, int hd, int rows, int r0, int nr, int padded) {
+    constexpr int AT_ONCE = 4;
+    for (int x = threadIdx.x; x < padded * 8; x += 256) {
+        const int r = x >> 3;
+        const float2 *src = p.ws + (int64_t)hd * p.nsplit * rows + r0 + min(r, nr - 1);
+        float M = -1e30f, sum = 0.f;
+        for (int s0 = x & 7; s0 < p.nsplit; s0 += 8 * AT_ONCE) {
+            float2 v[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                v[u] = src[(int64_t)min(s0 + 8 * u, p.nsplit - 1) * rows];
+                if (s0 + 8 * u >= p.nsplit) v[u] = make_float2(-1e30f, 0.f);
+            }
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const float mn = fmaxf(M, v[u].x);
+                sum = sum * __builtin_amdgcn_exp2f(M - mn) + v[u].y * __builtin_amdgcn_exp2f(v[u].x - mn);
                 M = mn;
             }
-            norm[r] = make_float2(M, 1.f / sum);
         }
-        __syncthreads();
-        for (int rr = 0; rr < nr; rr += 16) {
-            const int r = rr + i;
-            const bool valid = r < nr;
-            const int at = r0 + min(r, nr - 1);
-            const int tok = at / G;
-            typename OP::Q q;
-            OP::load_q(q, (const unsigned char *)p.q + ((int64_t)tok * p.n_q_heads + hd * G + (at - tok * G)) * OP::ROWB, g);
-            const float2 nm = norm[min(r, nr - 1)];
 #pragma unroll
-            for (int h = 0; h < HELD; ++h) {
-                float s[OP::NS];
-                OP::scores(k[h], q, s);
-                const int t = t0 + h;
-                if (keys.is_new(t)) mask<OP>(s, tok - (int)keys.first(t), g);
-#pragma unroll
-                for (int e = 0; e < OP::NS; ++e) {
-                    const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c2, -nm.x)) * nm.y;
-                    acc[h][e] += valid ? w : 0.f;
-                }
-            }
+        for (int d = 1; d < 8; d <<= 1) {
+            const float M2 = __shfl_xor(M, d), sum2 = __shfl_xor(sum, d), mn = fmaxf(M, M2);
+            sum = sum * __builtin_amdgcn_exp2f(M - mn) + sum2 * __builtin_amdgcn_exp2f(M2 - mn);
+            M = mn;
         }
+        if ((x & 7) == 0) norm[r] = r < nr ? M + __builtin_amdgcn_logf(sum) : INFINITY;
     }
+}
+
+// The weights of a wave's keys, summed over the lanes of a key's 16 rows, into the buffer
+template <class OP, int HELD>
+__device__ __forceinline__ void add_to_buffer(const WeighParams &p, const Keys<OP> &keys, float (&acc)[HELD][OP::NS], int hd,
+                                              int t0, int n_all, int i, int g) {
 #pragma unroll
     for (int h = 0; h < HELD; ++h) {
         const int t = t0 + h;
@@ -215,28 +286,175 @@ __global__ __launch_bounds__(256) void weigh_sum_kernel(const WeighParams p) {
     }
 }
 
+// block: (group of WAVES x HELD stages, kv head), kv head fastest.  The query rows go
+// through LDS in stages of 32.
+template <class OP, class RG, int HELD>
+__global__ __launch_bounds__(256) void weigh_sum_rows_kernel(const WeighParams p) {
+    constexpr int SLOTS = 3, ROWS = 32;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[SLOTS * RG::HALF];
+    __shared__ float norm[ROWS_AT_ONCE];
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hd = blockIdx.x % p.n_kv_heads;
+    const int G = p.group, rows = p.S * G;
+    const Keys<OP> keys(p, hd);
+    const int n_all = keys.n_pre + (p.S + OP::KEYS - 1) / OP::KEYS;
+    const int t0 = ((int)(blockIdx.x / p.n_kv_heads) * WAVES + wave) * HELD;
+    const float c2 = p.scale_log2;
+    const uint32_t qa = RG::row_at(i, g);
+    const uint64_t q0 = (uint64_t)(uintptr_t)p.q + (uint64_t)hd * G * OP::ROWB;
+    typename OP::K k[HELD];
+    float acc[HELD][OP::NS];
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) {
+        keys.load(k[h], t0 + h, t0 + h < n_all ? keys.count(t0 + h) : 0, i, g);
+#pragma unroll
+        for (int e = 0; e < OP::NS; ++e) acc[h][e] = 0.f;
+    }
+    // this wave's quarter of query rows r .. r + 31 (past the last: it again)
+    auto load = [&](int r, int slot) {
+#pragma unroll
+        for (int x = 0; x < RG::LOADS; ++x) {
+            const int at = (wave * RG::LOADS + x) * 1024;
+            const int row = at / OP::ROWB + lane / RG::CH;
+            const int rr = min(r + row, rows - 1), tok = rr / G;
+            const uint64_t src = q0 + ((uint64_t)tok * p.n_q_heads + (rr - tok * G)) * OP::ROWB +
+                                 16u * (uint32_t)((lane & (RG::CH - 1)) ^ RG::swz(row));
+            dma16((const void *)(uintptr_t)src, lds + slot * RG::HALF + at);
+        }
+    };
+    for (int r0 = 0; r0 < rows; r0 += ROWS_AT_ONCE) {
+        const int nr = min(rows - r0, ROWS_AT_ONCE), padded = (nr + ROWS - 1) / ROWS * ROWS;
+        if (r0) barrier_lds();
+        join_norms(p, norm, hd, rows, r0, nr, padded);
+        load(r0, 0);
+        if (ROWS < padded) load(r0 + ROWS, 1);
+        int slot = 0;
+        for (int rr = 0; rr < padded; rr += ROWS) {
+            if (rr + ROWS < padded) wait_vmcnt<RG::LOADS>();
+            else wait_vmcnt<0>();
+            barrier_lds();
+            if (rr + 2 * ROWS < padded) load(r0 + rr + 2 * ROWS, slot == 0 ? 2 : slot - 1);
+            const unsigned char *st = lds + slot * RG::HALF;
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                typename OP::Q q;
+#pragma unroll
+                for (int ks = 0; ks < OP::NK; ++ks) q.f[ks] = RG::row_frag(st, qa, part, ks);
+                const float nm = norm[rr + 16 * part + i];
+                const int tok = keys.is_new(t0 + HELD - 1) ? (r0 + rr + 16 * part + i) / G : 0;
+#pragma unroll
+                for (int h = 0; h < HELD; ++h) {
+                    float s[OP::NS];
+                    OP::scores(k[h], q, s);
+                    const int t = t0 + h;
+                    if (keys.is_new(t)) mask<OP>(s, tok - (int)keys.first(t), g);
+#pragma unroll
+                    for (int e = 0; e < OP::NS; ++e) acc[h][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c2, -nm));
+                }
+            }
+            slot = slot == SLOTS - 1 ? 0 : slot + 1;
+        }
+    }
+    add_to_buffer<OP, HELD>(p, keys, acc, hd, t0, n_all, i, g);
+}
+
+// The same with the query rows straight from memory
+template <class OP, int HELD>
+__global__ __launch_bounds__(256) void weigh_sum_kernel(const WeighParams p) {
+    __shared__ float norm[ROWS_AT_ONCE];
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hd = blockIdx.x % p.n_kv_heads;
+    const int G = p.group, rows = p.S * G;
+    const Keys<OP> keys(p, hd);
+    const int n_all = keys.n_pre + (p.S + OP::KEYS - 1) / OP::KEYS;
+    const int t0 = ((int)(blockIdx.x / p.n_kv_heads) * WAVES + wave) * HELD;
+    const float c2 = p.scale_log2;
+    typename OP::K k[HELD];
+    float acc[HELD][OP::NS];
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) {
+        keys.load(k[h], t0 + h, t0 + h < n_all ? keys.count(t0 + h) : 0, i, g);
+#pragma unroll
+        for (int e = 0; e < OP::NS; ++e) acc[h][e] = 0.f;
+    }
+    // row r0 + i of the kv head is head `rem` of token `tok`; 16 rows on: (t16, r16) further
+    const int t16 = 16 / G, r16 = 16 - t16 * G;
+    for (int r0 = 0; r0 < rows; r0 += ROWS_AT_ONCE) {
+        const int nr = min(rows - r0, ROWS_AT_ONCE), padded = (nr + 15) & ~15;
+        if (r0) __syncthreads();
+        join_norms(p, norm, hd, rows, r0, nr, padded);
+        int tok = (r0 + i) / G, rem = (r0 + i) - tok * G;
+        typename OP::Q q, next;
+        auto load = [&](typename OP::Q &to) {      // (rows past the last: any row)
+            const int t = min(tok, p.S - 1);
+            OP::load_q(to, (const unsigned char *)p.q + ((int64_t)t * p.n_q_heads + hd * G + rem) * OP::ROWB, g);
+        };
+        load(q);
+        __syncthreads();
+        for (int rr = 0; rr < padded; rr += 16) {
+            const int at = tok;
+            tok += t16;
+            rem += r16;
+            if (rem >= G) {
+                rem -= G;
+                ++tok;
+            }
+            load(next);
+            const float nm = norm[rr + i];
+#pragma unroll
+            for (int h = 0; h < HELD; ++h) {
+                float s[OP::NS];
+                OP::scores(k[h], q, s);
+                const int t = t0 + h;
+                if (keys.is_new(t)) mask<OP>(s, at - (int)keys.first(t), g);
+#pragma unroll
+                for (int e = 0; e < OP::NS; ++e) acc[h][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c2, -nm));
+            }
+            q = next;
+        }
+    }
+    add_to_buffer<OP, HELD>(p, keys, acc, hd, t0, n_all, i, g);
+}
+
+template <class E, int D>
+struct Op : Op16<E, D> {
+    using Ring = Ring16<E, D>;
+};
+
 template <class OP>
-hipError_t launch_op(const WeighParams &p, int rt, hipStream_t s) {
-    const int rows = p.S * p.group;
-    const unsigned tiles = (unsigned)((rows + 16 * rt - 1) / (16 * rt));
-    const dim3 grid(tiles * p.nsplit * p.n_kv_heads);
-    if (rt == 1) hipLaunchKernelGGL((weigh_stats_kernel<OP, 1>), grid, dim3(256), 0, s, p);
-    else if (rt == 2) hipLaunchKernelGGL((weigh_stats_kernel<OP, 2>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((weigh_stats_kernel<OP, 4>), grid, dim3(256), 0, s, p);
+hipError_t launch_op(const WeighParams &p, int way, int held, hipStream_t s) {
+    const int rows = p.S * p.group, per = way > kByRows ? 64 * (way - kByRows) : 16 * way;
+    const dim3 grid((unsigned)((rows + per - 1) / per) * p.nsplit * p.n_kv_heads), block(256);
+    if (way == 1) hipLaunchKernelGGL((weigh_stats_kernel<OP, 1>), grid, block, 0, s, p);
+    else if (way == 2) hipLaunchKernelGGL((weigh_stats_kernel<OP, 2>), grid, block, 0, s, p);
+    else if (way == 4) hipLaunchKernelGGL((weigh_stats_kernel<OP, 4>), grid, block, 0, s, p);
+    else if constexpr (OP::ELT == 2) {
+        if (way == kByRows + 2) hipLaunchKernelGGL((weigh_stats_rows_kernel<OP, typename OP::Ring, 2>), grid, block, 0, s, p);
+        else hipLaunchKernelGGL((weigh_stats_rows_kernel<OP, typename OP::Ring, 4>), grid, block, 0, s, p);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t stages = (p.L + OP::KEYS - 1) / OP::KEYS + (p.S + OP::KEYS - 1) / OP::KEYS;
-    const unsigned wgs = (unsigned)((stages + WAVES * HELD - 1) / (WAVES * HELD));
-    hipLaunchKernelGGL(weigh_sum_kernel<OP>, dim3(wgs * p.n_kv_heads), dim3(256), 0, s, p);
+    const dim3 wgs((unsigned)((stages + WAVES * held - 1) / (WAVES * held) * p.n_kv_heads));
+    if constexpr (OP::ELT == 2) {
+        using RG = typename OP::Ring;
+        if (held == 2) hipLaunchKernelGGL((weigh_sum_rows_kernel<OP, RG, 2>), wgs, block, 0, s, p);
+        else hipLaunchKernelGGL((weigh_sum_rows_kernel<OP, RG, 1>), wgs, block, 0, s, p);
+    } else {
+        if (held == 2) hipLaunchKernelGGL((weigh_sum_kernel<OP, 2>), wgs, block, 0, s, p);
+        else hipLaunchKernelGGL((weigh_sum_kernel<OP, 1>), wgs, block, 0, s, p);
+    }
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_weigh(const WeighParams &p, int head_dim, int dtype, int rt, hipStream_t s) {
-    if (dtype == KVR_F32) return head_dim == 128 ? launch_op<Op32<128>>(p, rt, s) : launch_op<Op32<64>>(p, rt, s);
-    if (dtype == KVR_F16) return head_dim == 128 ? launch_op<Op16<F16, 128>>(p, rt, s) : launch_op<Op16<F16, 64>>(p, rt, s);
-    return head_dim == 128 ? launch_op<Op16<Bf16, 128>>(p, rt, s) : launch_op<Op16<Bf16, 64>>(p, rt, s);
+hipError_t launch_weigh(const WeighParams &p, int head_dim, int dtype, int way, int held, hipStream_t s) {
+    if (dtype == KVR_F32) return head_dim == 128 ? launch_op<Op32<128>>(p, way, held, s) : launch_op<Op32<64>>(p, way, held, s);
+    if (dtype == KVR_F16) return head_dim == 128 ? launch_op<Op<F16, 128>>(p, way, held, s) : launch_op<Op<F16, 64>>(p, way, held, s);
+    return head_dim == 128 ? launch_op<Op<Bf16, 128>>(p, way, held, s) : launch_op<Op<Bf16, 64>>(p, way, held, s);
 }
 
 }  // namespace kvr

@@ -34,11 +34,13 @@ hipError_t launch_rope_table(float *, int, double, int64_t, hipStream_t) { retur
 
 // The grid's blocks, decoded as the kernel decodes them, name every prefix item and
 // every own item exactly once; splits cover the prefix; records fit the workspace.
-hipError_t launch_shared(const SharedParams &p, int head_dim, int dtype, int rp, int ro, hipStream_t) {
+hipError_t launch_shared(const SharedParams &p, int head_dim, int dtype, int pw, int ow, hipStream_t) {
     ++g_launches;
     const int64_t G = p.group, rows_p = (int64_t)p.n * p.S * G, rows_o = (int64_t)p.S * G;
-    if (ro > rp || (dtype == KVR_F32 && rp > 2)) BAD("row tiles %d %d", rp, ro);
-    if (p.p_tiles != (rows_p + 16 * rp - 1) / (16 * rp) || p.t_tiles != (rows_o + 16 * ro - 1) / (16 * ro)) BAD("tiles");
+    const bool f32 = dtype == KVR_F32;
+    const int64_t tp = pw > kByRows ? 64 * (pw - kByRows) : 16 * pw, to = ow > kByRows ? 64 * (ow - kByRows) : 16 * ow;
+    if (ow > pw || (f32 ? pw > 2 : pw == 2 || ow == 2 || pw > kByRows + 2 || ow > kByRows + 1)) BAD("ways %d %d", pw, ow);
+    if (p.p_tiles != (rows_p + tp - 1) / tp || p.t_tiles != (rows_o + to - 1) / to) BAD("tiles");
     if (p.rows != (int64_t)p.n * p.S * p.n_q_heads || p.rows > 0x7fffffff) BAD("rows");
     if (p.nrec != p.np + p.nt || p.nt < 1) BAD("records");
     if ((p.L == 0) != (p.np == 0)) BAD("no split of a prefix");
@@ -68,19 +70,24 @@ hipError_t launch_shared(const SharedParams &p, int head_dim, int dtype, int rp,
     }
     return hipErrorUnknown;
 }
-hipError_t launch_weigh(const WeighParams &p, int, int dtype, int rt, hipStream_t) {
+hipError_t launch_weigh(const WeighParams &p, int, int dtype, int way, int held, hipStream_t) {
     ++g_launches;
     const int64_t keys = dtype == KVR_F32 ? 16 : 32;
     const int64_t stages = (p.L + keys - 1) / keys + (p.S + keys - 1) / keys, rows = (int64_t)p.S * p.group;
     if ((int64_t)p.nsplit * p.chunk < stages || (int64_t)(p.nsplit - 1) * p.chunk >= stages) BAD("weigh splits");
     if ((size_t)p.nsplit * p.n_kv_heads * rows * 8 > g_ws_given) BAD("weigh workspace");
-    if ((rows + 16 * rt - 1) / (16 * rt) * p.nsplit * p.n_kv_heads > 0x7fffffff) BAD("weigh grid");
+    const int64_t per = way > kByRows ? 64 * (way - kByRows) : 16 * way;
+    if ((rows + per - 1) / per * p.nsplit * p.n_kv_heads > 0x7fffffff) BAD("weigh grid");
+    const bool direct = way == 1 || way == 2 || way == 4, ring = dtype != KVR_F32 && (way == kByRows + 2 || way == kByRows + 4);
+    if ((!direct && !ring) || (held != 1 && held != 2)) BAD("weigh way %d %d", way, held);
     return hipErrorUnknown;
 }
 hipError_t launch_evict(const EvictParams &p, hipStream_t) {
     ++g_launches;
     if (p.n_first + p.n_last > p.n_keep || p.n_keep > p.L || p.L > p.cap || p.n_keep > p.cap_out) BAD("evict rows");
-    if ((size_t)p.n_kv_heads * p.n_keep * 4 > g_ws_given) BAD("evict workspace");
+    if (p.L > kHeldRows && (size_t)p.n_kv_heads * p.n_keep * 4 > g_ws_given) BAD("evict workspace");
+    if (p.L <= kHeldRows && (p.parts < 1 || (int64_t)p.parts * p.n_kv_heads > 0x7fffffff)) BAD("evict grid");
+    if (p.row_chunks != 1 << p.chunk_bits) BAD("evict chunks");
     return hipErrorUnknown;
 }
 }  // namespace kvr

@@ -115,14 +115,24 @@ def test_weigh_no_work(lib):
     (dict(kc=None), "NULL"), (dict(vc=None), "NULL"), (dict(w=None), "NULL"), (dict(ko=None), "NULL"), (dict(vo=None), "NULL"),
     (dict(kc=FAR + 8), "ALIGN"), (dict(ko=FAR + 8), "ALIGN"), (dict(w=FAR + 2), "ALIGN"), (dict(ix=FAR + 1), "ALIGN"),
     (dict(wo=FAR + 1), "ALIGN"), (dict(ws=FAR + 4), "ALIGN"),
-    (dict(ws=None), "WORKSPACE"), (dict(wsb=100 * 8 * 4 - 1), "WORKSPACE"),
     # outputs over inputs or each other
     (dict(ko=FAR), "SHAPE"), (dict(vo=FAR + 4096 * 8 * 256 - 16), "SHAPE"), (dict(ko=2 * FAR - 16), "SHAPE"),
-    (dict(vo=4 * FAR), "SHAPE"), (dict(wo=3 * FAR), "SHAPE"), (dict(ix=3 * FAR + 16), "SHAPE"), (dict(ix=8 * FAR), "SHAPE"),
-    (dict(ws=4 * FAR), "SHAPE"),
+    (dict(vo=4 * FAR), "SHAPE"), (dict(wo=3 * FAR), "SHAPE"), (dict(ix=3 * FAR + 16), "SHAPE"),
 ])
 def test_evict_refusals(lib, kw, code):
     assert evict(lib, **kw) == getattr(kvr, "KVR_ERR_" + code)
+
+
+def test_evict_workspace_of_long_caches(lib):
+    d = desc(capacity=70000)
+    need = 70000 * 8 * 4
+    assert kvr.kvr_workspace_bytes_evict(d, 70000) == need
+    assert kvr.kvr_workspace_bytes_evict(d, 32768) == 0
+    long = lambda **kw: evict(lib, d, L=70000, **kw)
+    assert long(ws=None) == kvr.KVR_ERR_WORKSPACE
+    assert long(wsb=need - 1) == kvr.KVR_ERR_WORKSPACE
+    assert long(wsb=need, ix=8 * FAR) == kvr.KVR_ERR_SHAPE        # an output in the workspace
+    assert long(wsb=need, ws=4 * FAR) == kvr.KVR_ERR_SHAPE
 
 
 def test_evict_no_work(lib):
@@ -131,7 +141,6 @@ def test_evict_no_work(lib):
 
 def test_workspace_sizes(lib):
     d = desc()
-    assert kvr.kvr_workspace_bytes_evict(d, 100) == 8 * 100 * 4
     assert kvr.kvr_workspace_bytes_shared(d, 100, 0, 1, 10) == 0
     assert kvr.kvr_workspace_bytes_weigh(d, 100, 0) == 0
     for n, S in ((1, 1), (9, 1), (64, 2), (3, 40)):
