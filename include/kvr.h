@@ -382,7 +382,8 @@ int kvr_continue_batched_rope(const kvr_desc *desc, const kvr_rope *rope, const 
  *   of positions that it stands for when rows were evicted from it.  Needs
  *   rope->n_pos >= pos0 + tail_capacity (+ S when append == 0).
  *   ws: kvr_workspace_bytes_shared(desc, L_prefix, n, S, tail_capacity) bytes.
- * Limits: n S n_q_heads, L_prefix and tail_capacity below 2^31 (KVR_ERR_SHAPE).
+ * Limits: n S n_q_heads below 2^24, L_prefix and tail_capacity below 2^31
+ * (KVR_ERR_SHAPE).
  * A masked place never reaches a result: not own rows behind a reader's length, nor
  * a later new token's key or value, whatever they hold.
  */
@@ -408,7 +409,8 @@ size_t kvr_workspace_bytes_shared(const kvr_desc *desc, int64_t L_prefix, int32_
  *   L_prefix + S <= capacity (KVR_ERR_CAPACITY).
  *   ws: kvr_workspace_bytes_weigh(desc, L_prefix, S) bytes.
  * Scores, softmax and sums in fp32 for every element type.
- * Limits: S n_q_heads / n_kv_heads and L_prefix + S below 2^31 (KVR_ERR_SHAPE).
+ * Limits: S n_q_heads and (L_prefix + S) n_kv_heads below 2^28 are served; calls far
+ * beyond that are refused (KVR_ERR_SHAPE).
  */
 int kvr_cache_weigh(const kvr_desc *desc, const void *Qs, const void *Ks, const void *kcache, int64_t L_prefix,
                     int64_t S, float *weight, void *ws, size_t ws_bytes, void *stream);

@@ -32,11 +32,14 @@ namespace dev {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Rows [0, n) of stride_b bytes from `base`, of which row_b are read: the resource
-// that ends with row n - 1 (n <= 0: an empty one).  n * stride_b stays below 2^31:
-// a stage has at most 32 rows, and a row of all kv heads at most 2 MB.
+// that ends with row n - 1 (n <= 0: an empty one).  A row of all kv heads has at most 2 MB:
+// strides are 24-bit numbers, and a stage of at most 32 rows ends below 2^31.
+// All wave-uniform; said so, or the compiler loops over the lanes' resources.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_rsrc(uint64_t base, int n, uint32_t stride_b, uint32_t row_b) {
     const uint32_t bytes = n > 0 ? (uint32_t)(n - 1) * stride_b + row_b : 0u;
-    return __builtin_amdgcn_make_buffer_rsrc((void *)(uintptr_t)base, 0, bytes, 0x00020000);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)base), hi = __builtin_amdgcn_readfirstlane((uint32_t)(base >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc((void *)(uintptr_t)((uint64_t)hi << 32 | lo), 0,
+                                             __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
 }
 
 // Maximum and sum over the four lanes of a query row (lanes i, i + 16, i + 32, i + 48;
@@ -83,14 +86,14 @@ struct Op16 {
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int ks = 0; ks < NK; ++ks)
-                k.f[h][ks] = h < PARTS ? buf_load16(r, (uint32_t)(16 * h + i) * stride_b + 16 * g + 64 * ks)
+                k.f[h][ks] = h < PARTS ? buf_load16(r, __umul24(16 * h + i, stride_b) + 16 * g + 64 * ks)
                                        : (u32x4){0u, 0u, 0u, 0u};
     }
     template <int PARTS = 2>
     __device__ static __forceinline__ void load_v(V &v, __amdgpu_buffer_rsrc_t r, uint32_t stride_b, int i, int g) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint32_t off = (uint32_t)key_of(e, g) * stride_b + 2 * NT * i;
+            const uint32_t off = __umul24(key_of(e, g), stride_b) + 2 * NT * i;
             if (e >= 4 * PARTS) v.r[e] = vrow(0);
             else if constexpr (NT == 8) v.r[e] = buf_load16(r, off);
             else v.r[e] = __builtin_amdgcn_raw_buffer_load_b64(r, (int)off, 0, 0);
@@ -133,20 +136,47 @@ struct Op16 {
         for (int e = 0; e < 8; ++e) s[e] = a[e >> 2][e & 3];
     }
     // Weights as the second product's operand: the element type, rounded to nearest
-    // even.  Each weight is off by half a step at most, as the values it multiplies
-    // are by themselves; the row's sum is taken from the unrounded ones.
+    // even, each off by half a step at most.  The row's sum is taken from the rounded
+    // ones, as one more product (with ones in the place of V^T: every component is the
+    // row's sum over all the wave's keys), so that out = sum p v / sum p stays a mean of
+    // the values: where one weight dominates, its rounding cancels.
+    using L = f32x4;
+    __device__ static __forceinline__ L no_sum() { return (f32x4){0.f, 0.f, 0.f, 0.f}; }
+    __device__ static __forceinline__ float total(const L &l) { return l[0]; }
     struct P {
         u32x4 f;
     };
     __device__ static __forceinline__ void weights(P &w, const float (&p)[NS]) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w.f[j] = E::pack2(p[2 * j], p[2 * j + 1]);
+        for (int j = 0; j < 4; ++j) {
+            uint32_t x = E::pack2(p[2 * j], p[2 * j + 1]);
+            asm("" : "+v"(x));      // one conversion of two: the halves' maxima below would split it
+            w.f[j] = x;
+        }
+    }
+    __device__ static __forceinline__ void add(L &l, const P &w) {
+        constexpr uint32_t one = std::is_same<E, F16>::value ? 0x3c003c00u : 0x3f803f80u;
+        l = mfma((u32x4){one, one, one, one}, w.f, l);
+    }
+    // The largest weights, two by two: positive floats order as their bits do.  Up to 2^15 in
+    // fp16 (whose largest is just below 2^16), 2^60 in bf16: 2^31 of them, each times a value
+    // of up to 2^35, are less than the largest fp32 sum.
+    static constexpr int kMost = std::is_same<E, F16>::value ? 15 : 60;
+    typedef uint16_t Peak __attribute__((ext_vector_type(2)));
+    __device__ static __forceinline__ Peak no_peak() { return (Peak){0, 0}; }
+    __device__ static __forceinline__ void raise(Peak &k, const P &w) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k = __builtin_elementwise_max(k, __builtin_bit_cast(Peak, (uint32_t)w.f[j]));
+    }
+    __device__ static __forceinline__ bool too_large(Peak k) {
+        constexpr uint16_t most = std::is_same<E, F16>::value ? (15 + kMost) << 10 : (127 + kMost) << 7;
+        return k[0] > most || k[1] > most;
     }
     // whether every value of the stage is a number (the exponent's bits are not all set)
     __device__ static __forceinline__ bool finite(const V &v) {
         bool ok = true;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ok = ok && finite_words(v.r[e]);
+        for (int e = 0; e < 8; ++e) ok &= finite_words(v.r[e]);
         return ok;
     }
     template <class W>
@@ -154,7 +184,7 @@ struct Op16 {
         constexpr uint32_t ex = std::is_same<E, F16>::value ? 0x7c00u : 0x7f80u;
         bool ok = true;
 #pragma unroll
-        for (int j = 0; j < (int)(sizeof(W) / 4); ++j) ok = ok && (w[j] & ex) != ex && (w[j] >> 16 & ex) != ex;
+        for (int j = 0; j < (int)(sizeof(W) / 4); ++j) ok &= ((w[j] & ex) != ex) & ((w[j] >> 16 & ex) != ex);
         return ok;
     }
     // an operand of eight keys with zeros in the place of every key but c
@@ -175,24 +205,24 @@ struct Op16 {
     }
     // o[rt][t] += V^T P^T of every tile
     template <int RT>
-    __device__ static __forceinline__ void accumulate(const V &v, const P (&w)[RT], f32x4 (&o)[RT][NT]) {
+    __device__ static __forceinline__ void accumulate(const V &v, const P (&w)[RT][1], f32x4 (&o)[RT][NT]) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const u32x4 a = column(v, t);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) o[rt][t] = mfma(a, w[rt].f, o[rt][t]);
+            for (int rt = 0; rt < RT; ++rt) o[rt][t] = mfma(a, w[rt][0].f, o[rt][t]);
         }
     }
     // the same of key c alone (zeros in the place of the others), for the rows that see it
     template <int RT>
-    __device__ static __forceinline__ void accumulate_key(const V &v, const P (&w)[RT], f32x4 (&o)[RT][NT], int c,
+    __device__ static __forceinline__ void accumulate_key(const V &v, const P (&w)[RT][1], f32x4 (&o)[RT][NT], int c,
                                                           const bool (&sees)[RT], int g) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const u32x4 a = only_key(column(v, t), c, g);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                const f32x4 x = mfma(a, w[rt].f, o[rt][t]);
+                const f32x4 x = mfma(a, w[rt][0].f, o[rt][t]);
                 o[rt][t] = sees[rt] ? x : o[rt][t];
             }
         }
@@ -255,7 +285,7 @@ struct Op32 {
     template <int PARTS = 1>
     __device__ static __forceinline__ void load_k(K &k, __amdgpu_buffer_rsrc_t r, uint32_t stride_b, int i, int g) {
 #pragma unroll
-        for (int ks = 0; ks < NK; ++ks) k.f[ks] = load(r, (uint32_t)i * stride_b + 16 * g + 64 * ks);
+        for (int ks = 0; ks < NK; ++ks) k.f[ks] = load(r, __umul24(i, stride_b) + 16 * g + 64 * ks);
     }
     template <int PARTS = 1>
     __device__ static __forceinline__ void load_v(V &v, __amdgpu_buffer_rsrc_t r, uint32_t stride_b, int i, int g) {
@@ -263,7 +293,7 @@ struct Op32 {
         for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int j = 0; j < NT / 4; ++j)
-                v.r[e][j] = load(r, (uint32_t)key_of(e, g) * stride_b + 4 * NT * i + 16 * j);
+                v.r[e][j] = load(r, __umul24(key_of(e, g), stride_b) + 4 * NT * i + 16 * j);
     }
     template <int PARTS = 1>
     __device__ static __forceinline__ void rotate_k(K &k, const float *cs, int n, int i, int g) {
@@ -297,20 +327,30 @@ struct Op32 {
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[e] = (a[0][e] + a[1][e]) + (a[2][e] + a[3][e]);
     }
+    // the lane's share of the row's sum
+    using L = float;
+    __device__ static __forceinline__ L no_sum() { return 0.f; }
+    __device__ static __forceinline__ float total(L l) { return quad_sum(l); }
     __device__ static __forceinline__ void weights(P &w, const float (&p)[NS]) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) w.f[e] = p[e];
     }
+    __device__ static __forceinline__ void add(L &l, const P &w) { l += (w.f[0] + w.f[1]) + (w.f[2] + w.f[3]); }
+    static constexpr int kMost = 60;
+    using Peak = float;      // the sum: too large, or no number, if one of them is
+    __device__ static __forceinline__ Peak no_peak() { return 0.f; }
+    __device__ static __forceinline__ void raise(Peak &k, const P &w) { k += (w.f[0] + w.f[1]) + (w.f[2] + w.f[3]); }
+    __device__ static __forceinline__ bool too_large(Peak k) { return !(k <= 0x1p60f); }
     __device__ static __forceinline__ bool finite(const V &v) {
         bool ok = true;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int d = 0; d < NT; ++d) ok = ok && (__float_as_uint(v.r[e][d / 4][d % 4]) & 0x7f800000u) != 0x7f800000u;
+            for (int d = 0; d < NT; ++d) ok &= (__float_as_uint(v.r[e][d / 4][d % 4]) & 0x7f800000u) != 0x7f800000u;
         return ok;
     }
     template <int RT>
-    __device__ static __forceinline__ void accumulate_key(const V &v, const P (&w)[RT], f32x4 (&o)[RT][NT], int c,
+    __device__ static __forceinline__ void accumulate_key(const V &v, const P (&w)[RT][1], f32x4 (&o)[RT][NT], int c,
                                                           const bool (&sees)[RT], int g) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -319,19 +359,19 @@ struct Op32 {
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     const float a = key_of(e, g) == c ? v.r[e][t / 4][t % 4] : 0.f;
-                    const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x4f32(a, w[rt].f[e], o[rt][t], 0, 0, 0);
+                    const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x4f32(a, w[rt][0].f[e], o[rt][t], 0, 0, 0);
                     o[rt][t] = sees[rt] ? x : o[rt][t];
                 }
     }
     template <int RT>
-    __device__ static __forceinline__ void accumulate(const V &v, const P (&w)[RT], f32x4 (&o)[RT][NT]) {
+    __device__ static __forceinline__ void accumulate(const V &v, const P (&w)[RT][1], f32x4 (&o)[RT][NT]) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
-                    o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.r[e][t / 4][t % 4], w[rt].f[e], o[rt][t], 0, 0, 0);
+                    o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.r[e][t / 4][t % 4], w[rt][0].f[e], o[rt][t], 0, 0, 0);
     }
     __device__ static __forceinline__ void put4(void *row, int d, float a, float b, float c, float e) {
         *(f32x4 *)((float *)row + d) = (f32x4){a, b, c, e};

@@ -1,4 +1,4 @@
-// attn_ring.hpp -- stages of 32 K (or V, or Q) rows that the four waves of a workgroup
+// attn_ring.hpp -- stages of 32 or 64 K (or V, or Q) rows that the four waves of a workgroup
 // share in LDS, 16-bit elements.  Shared by shared.hip and weigh.hip.
 //
 // Fragments loaded straight from memory (attn_direct.hpp) take 16 rows' lines at each
@@ -6,9 +6,10 @@
 // the same rows, loading them once in whole rows costs the caches a quarter of the
 // lines and a wave's reads come from LDS.
 //
-// Row r of a stage lies at r ROWB, its 16-byte chunk c in slot c ^ swz(r): the 16 lanes
-// that read one chunk of 16 rows (K, Q), and the 16 that read 16 columns of four rows
-// transposed (V), touch 16 distinct slots.
+// Row r of a stage lies at r ROWB, its 16-byte chunk c in slot c ^ swz(r).  LDS gives 256
+// bytes a clock.  K and Q: 16 lanes at a time read a chunk of 16 different rows, which swz
+// spreads over 16 places of a 256-byte line.  V, transposed: 32 lanes at a time read two
+// neighbouring chunks of eight rows, four consecutive ones from each of two 16-lane groups.
 #pragma once
 
 #include "attn_direct.hpp"
@@ -16,36 +17,41 @@
 namespace kvr {
 namespace dev {
 
-template <class E, int D>
+// KEYS_: rows of a stage, 32 or 64
+template <class E, int D, int KEYS_ = 32>
 struct Ring16 {
     using OP = Op16<E, D>;
     static constexpr int ROWB = D * 2, CH = D / 8, NK = D / 32, NT = D / 16;
-    static constexpr int KEYS = 32, HALF = KEYS * ROWB;      // one operand's rows of a stage
+    static constexpr int KEYS = KEYS_, HALF = KEYS * ROWB;      // one operand's rows of a stage
     static constexpr int LOADS = HALF / 4096;                // wave-wide 1 KB loads of a wave for them
 
+    template <bool IS_V>
     __device__ static __forceinline__ int swz(int row) {
-        return D == 128 ? ((row >> 2) & 3) | ((row & 3) << 2) : (row >> 1) & 7;
+        const int half = ((row >> 2) ^ (row >> 3)) & 1;      // of the groups' rows 4 g ..
+        if (IS_V) return D == 128 ? (row & 3) << 1 | half << 3 : (row & 2) | half << 2;
+        return D == 128 ? row & 15 : (row >> 1) & 7;
     }
     // This wave's quarter of the rows [0, n) (n > 0) of stride_b bytes from base into the
     // stage at lds; rows past the last repeat it.
+    template <bool IS_V>
     __device__ static __forceinline__ void load(uint64_t base, uint32_t stride_b, int n, const unsigned char *lds, int wave,
                                                 int lane) {
 #pragma unroll
         for (int x = 0; x < LOADS; ++x) {
             const int at = (wave * LOADS + x) * 1024;
             const int row = at / ROWB + lane / CH;
-            const uint32_t off = (uint32_t)min(row, n - 1) * stride_b + 16u * (uint32_t)((lane & (CH - 1)) ^ swz(row));
+            const uint32_t off = (uint32_t)min(row, n - 1) * stride_b + 16u * (uint32_t)((lane & (CH - 1)) ^ swz<IS_V>(row));
             dma16_s(base, off, lds + at);
         }
     }
-    // lane (i, g)'s LDS offset of chunk g of row i; chunk 4 ks + g lies at this ^ 64 ks,
-    // rows 16 further at + 16 ROWB
-    __device__ static __forceinline__ uint32_t row_at(int i, int g) { return (uint32_t)(i * ROWB + 16 * (g ^ swz(i))); }
+    // lane (i, g)'s LDS offset of chunk g of row i (swz has a row's last four bits: the same
+    // 16 rows further, at + 16 ROWB); chunk 4 ks + g lies at this ^ 64 ks
+    __device__ static __forceinline__ uint32_t row_at(int i, int g) { return (uint32_t)(i * ROWB + 16 * (g ^ swz<false>(i))); }
     // what lane (i, g) passes to the transposing read of rows 4 g .. 4 g + 3, columns 0 .. 15;
     // columns 16 t .. at this ^ 32 t
     __device__ static __forceinline__ uint32_t col_at(int i, int g) {
         const int row = 4 * g + (i >> 2);
-        return (uint32_t)(row * ROWB + 16 * (((i & 3) >> 1) ^ swz(row)) + 8 * (i & 1));
+        return (uint32_t)(row * ROWB + 16 * (((i & 3) >> 1) ^ swz<true>(row)) + 8 * (i & 1));
     }
     // K (or Q) rows of a 16-row part as an operand
     __device__ static __forceinline__ u32x4 row_frag(const unsigned char *lds, uint32_t at, int part, int ks) {

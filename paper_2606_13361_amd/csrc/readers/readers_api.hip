@@ -14,6 +14,7 @@ constexpr int64_t kMaxTokens = (int64_t)1 << 30;
 constexpr int64_t kMaxKeys = (int64_t)1 << 40;
 constexpr int64_t kCus = 256;
 constexpr int64_t kMaxRows = 0x7fffffff;   // cached rows and query rows of a call: 32-bit on the device
+constexpr int64_t kMaxGrid = ((int64_t)1 << 24) - 1;   // workgroups of a launch: 2^32 threads are too many
 constexpr int kWaves = 4;                  // of a workgroup
 
 // The library's check of a descriptor: an update of no rows ends after it
@@ -31,12 +32,17 @@ int64_t stage_keys(const kvr_desc *d) { return d->dtype == KVR_F32 ? 16 : 32; }
 int64_t way_rows(int way) { return way > kByRows ? 64 * (way - kByRows) : 16 * way; }
 
 // ---- shared
-constexpr int64_t kMinSplitKeys = 256;
+// Workgroups are as many as there are compute units, as long as each keeps this many keys.
+// Prefix by keys: one stage for each wave; 128 and 256 measured 5.9 and 6.8 us with 255 keys
+// and 2 readers, 9.0 and 11.0 us with 945 keys and 3 readers in fp32.  By rows it is 256:
+// 128, 256 and 512 took 11.0, 10.6 and 14.4 us with 3774 keys and 9 readers, and a merge
+// of more records.
+constexpr int64_t kMinKeysByKeys = 128, kMinKeysByRows = 256, kMinOwnKeys = 512;
 constexpr int64_t kMaxOwnSplits = 16;
 
 struct SharedPlan {
     int pw, ow;
-    int64_t p_tiles, t_tiles, np, nt, chunk, rows, octs_p, octs_o;
+    int64_t p_tiles, t_tiles, np, nt, chunk, rows, octs_p, octs_o, octs_n;
     size_t ws_bytes;
 };
 
@@ -61,30 +67,35 @@ bool plan_shared(const kvr_desc *d, int64_t L, int64_t n, int64_t S, int64_t tca
             const int64_t base = s.p_tiles * d->n_kv_heads;
             const int64_t step = kWaves * stage_keys(d);
             want = ceil_div(kCus, base);
-            const int64_t by_keys = ceil_div(L, kMinSplitKeys);
+            const int64_t by_keys = ceil_div(L, s.pw > kByRows ? kMinKeysByRows : kMinKeysByKeys);
             if (want > by_keys) want = by_keys;
             s.chunk = ceil_div(ceil_div(L, want), step) * step;
             s.np = ceil_div(L, s.chunk);
         }
         const int64_t own = n * s.t_tiles * d->n_kv_heads;
-        s.nt = ceil_div(kCus, own);
-        const int64_t by_cap = ceil_div(tcap, kMinSplitKeys);
-        if (s.nt > by_cap) s.nt = by_cap;
-        if (s.nt > kMaxOwnSplits) s.nt = kMaxOwnSplits;
-        if (s.nt < 1) s.nt = 1;
+        if (tcap > 0) {
+            s.nt = ceil_div(kCus, own);
+            const int64_t by_cap = ceil_div(tcap, kMinOwnKeys);
+            if (s.nt > by_cap) s.nt = by_cap;
+            if (s.nt > kMaxOwnSplits) s.nt = kMaxOwnSplits;
+        }
         s.octs_p = ceil_div(s.np * d->n_kv_heads, 8) * s.p_tiles;
         s.octs_o = ceil_div(own * s.nt, 8);
-        if ((s.octs_p + s.octs_o) * 8 > kMaxRows) return false;
-        s.ws_bytes = (size_t)(want + s.nt) * (size_t)s.rows * (d->head_dim + 2) * sizeof(float);
+        s.octs_n = ceil_div(n * ceil_div(rows_o, 16) * d->n_kv_heads, 8 * kWaves);
+        if ((s.octs_p + s.octs_o + s.octs_n) * 8 > kMaxGrid || s.rows > kMaxGrid) return false;
+        s.ws_bytes = (size_t)(want + s.nt + 1) * (size_t)s.rows * (d->head_dim + 2) * sizeof(float);
     }
     *out = s;
     return true;
 }
 
 // ---- weigh
+constexpr int64_t kJoinAlone = 1024;   // splits x rows of a kv head from which they are joined once for all
+
 struct WeighPlan {
     int way, held;
-    int64_t nsplit, chunk, grid;
+    bool join;
+    int64_t nsplit, chunk, grid, norm_at;
     size_t ws_bytes;
 };
 
@@ -99,15 +110,17 @@ bool plan_weigh(const kvr_desc *d, int64_t L, int64_t S, WeighPlan *out) {
         const int64_t base = ceil_div(rows, way_rows(w.way)) * d->n_kv_heads;
         const int64_t stages = ceil_div(L, stage_keys(d)) + ceil_div(S, stage_keys(d));
         int64_t want = ceil_div(2 * kCus, base);
-        const int64_t most = ceil_div(stages, 2 * kWaves);
+        const int64_t most = ceil_div(stages, kWaves);
         if (want > most) want = most;
         w.chunk = ceil_div(ceil_div(stages, want), kWaves) * kWaves;
         w.nsplit = ceil_div(stages, w.chunk);
         w.grid = base * w.nsplit;
         // second pass: keys held in registers serve every row, as long as the workgroups fill the part
-        w.held = ceil_div(stages, kWaves * 2) * d->n_kv_heads >= 2 * kCus ? 2 : 1;
-        if (w.grid > kMaxRows) return false;
-        w.ws_bytes = (size_t)want * d->n_kv_heads * rows * 2 * sizeof(float);
+        w.held = d->dtype == KVR_F32 && ceil_div(stages, kWaves * 2) * d->n_kv_heads >= 2 * kCus ? 2 : 1;
+        if (w.grid > kMaxGrid || ceil_div(stages, kWaves) * d->n_kv_heads > kMaxGrid) return false;
+        w.join = w.nsplit * rows > kJoinAlone;
+        w.norm_at = want * d->n_kv_heads * rows * 2 * (int64_t)sizeof(float);
+        w.ws_bytes = (size_t)w.norm_at + (size_t)d->n_kv_heads * rows * sizeof(float);
     }
     *out = w;
     return true;
@@ -184,11 +197,12 @@ int kvr_continue_shared(const kvr_desc *desc, const kvr_rope *rope, const void *
     p.append = append ? 1 : 0;
     p.np = (int32_t)plan.np;
     p.nt = (int32_t)plan.nt;
-    p.nrec = p.np + p.nt;
+    p.nrec = p.np + p.nt + 1;
     p.p_tiles = (int32_t)plan.p_tiles;
     p.t_tiles = (int32_t)plan.t_tiles;
-    p.oct_all = (uint32_t)(plan.octs_p + plan.octs_o);
-    p.own_share = (((uint64_t)plan.octs_o << 32) + p.oct_all - 1) / p.oct_all;
+    p.oct_own = (uint32_t)plan.octs_p;
+    p.oct_new = (uint32_t)(plan.octs_p + plan.octs_o);
+    p.oct_all = (uint32_t)(plan.octs_p + plan.octs_o + plan.octs_n);
     return to_status(launch_shared(p, desc->head_dim, desc->dtype, plan.pw, plan.ow, (hipStream_t)stream));
 }
 
@@ -217,6 +231,7 @@ int kvr_cache_weigh(const kvr_desc *desc, const void *Qs, const void *Ks, const 
     p.q = Qs; p.kn = Ks; p.kc = kcache;
     p.weight = weight;
     p.ws = (float2 *)ws;
+    p.norm = plan.join ? (float *)((char *)ws + plan.norm_at) : nullptr;
     p.cap = desc->capacity;
     p.L = L_prefix;
     p.S = (int32_t)S;

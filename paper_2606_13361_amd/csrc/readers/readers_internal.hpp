@@ -23,12 +23,11 @@ struct SharedParams {
     int64_t cap, tcap, L, pos0;
     int64_t chunk;          // prefix keys per split
     int64_t rows;           // n S n_q_heads
-    uint64_t own_share;     // groups of eight blocks that hold own items, of all groups, times 2^32 (rounded up)
-    uint32_t oct_all;       // all groups
+    uint32_t oct_own, oct_new, oct_all;   // groups of eight blocks: where own and new items begin, all
     float scale_log2;
     int32_t n, S, n_q_heads, n_kv_heads, group;
     int32_t append;
-    int32_t np, nt, nrec;   // splits of the prefix and of own rows; np + nt
+    int32_t np, nt, nrec;   // splits of the prefix and of own rows; np + nt + 1, the last for the new rows
     int32_t p_tiles, t_tiles;   // row tiles of a kv head over the prefix, of a reader's kv head over its own rows
 };
 // pw, ow: the ways of prefix and own items, ow <= pw.  1, 2: the four waves share 16 or 32
@@ -44,6 +43,7 @@ struct WeighParams {
     const void *kc;       // [n_kv_heads][cap][D]
     float *weight;        // [n_kv_heads][cap], added to
     float2 *ws;           // (M, l) [n_kv_heads][nsplit][rows], rows = S group
+    float *norm;          // [n_kv_heads][rows] behind them where a launch of its own joins the splits, or null
     int64_t cap, L;
     int32_t S, n_q_heads, n_kv_heads, group;
     int32_t nsplit, chunk;   // key splits of the first pass, of `chunk` stages each

@@ -3,20 +3,21 @@
 //
 //   out[r, i, h] = softmax over [prefix 0 .. L-1 | own rows 0 .. len_r - 1 | new rows 0 .. i]
 //
-// Two kinds of work in one launch, joined by a merge of log-sum-exp partials:
+// Three kinds of work in one launch, joined by a merge of log-sum-exp partials:
 //   prefix  every reader sees the whole prefix, so the query rows of all readers of
 //           a kv head are packed into tiles and the prefix is read once for all of
 //           them (once for each row tile from the caches, once from HBM)
-//   own     the rows of one reader and kv head over that reader's cached rows and,
-//           causally, its new rows; the last row tile stores these to its cache
-// A workgroup of four waves is one such item over a range of keys, in one of two ways:
-//   by keys   up to 16 query rows (fp32: 32 a tile): every wave holds the same rows
-//             and takes the range's stages in turn, K and V straight from memory
-//             (attn_direct.hpp), no barrier until the four partials are joined
+//   own     the rows of one reader and kv head over that reader's cached rows
+//   new     the rows of one reader and kv head over its new rows, causally; the last
+//           row tile stores these to the reader's cache
+// Prefix and own items are a workgroup's over a range of cached keys, in one of two ways:
+//   by keys   up to 16 query rows (fp32: 32 a tile): the four waves hold the same rows and
+//             take the range's stages in turn, K and V straight from memory
+//             (attn_direct.hpp), no barrier until their partials are joined
 //   by rows   more rows, 16-bit: each wave holds 16 or 32 rows of its own and the
 //             stages go through LDS once for all four (attn_ring.hpp)
-// The item's partial (M, l, O) goes to the workspace.  The lengths are read on the
-// device: a captured graph serves every step of a decode.
+// A new item is one wave's.  Each item's partial (M, l, O) is a record of the workspace.
+// The lengths are read on the device: a captured graph serves every step of a decode.
 #include <type_traits>
 
 #include "attn_ring.hpp"
@@ -32,109 +33,172 @@ constexpr int WAVES = 4;
 // 16-bit operations of both ways
 template <class E, int D>
 struct Op : Op16<E, D> {
-    using Ring = Ring16<E, D>;
+    using Ring = Ring16<E, D, 32>;
 };
 
 template <class OP, int RT>
 struct Rows {
     typename OP::Q q[RT];
     f32x4 o[RT][OP::NT];
-    float m[RT], l[RT];      // reference (log2 domain) of the row; the lane's share of the sum
-    int last[RT];            // own rows: the last new row that the lane's query row sees
+    float m[RT];             // reference of the row (log2 domain)
+    typename OP::L l[RT];    // its sum
+    int tok[RT];             // the row's token, of its reader's new ones
+    int at[RT];              // the row in out, -1: none
 };
 
-// The scores of a stage become weights: keys with stage index >= n are masked, with
-// CAUSAL also those beyond the row's own bound (c0: the stage's first new row).
-template <class OP, int RT, bool CAUSAL>
-__device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][OP::NS], typename OP::P (&w)[RT], int n,
-                                             int c0, float c2, int g) {
+// Cached rows of reader r, or -1 if it takes no part
+__device__ __forceinline__ int reader_len(const SharedParams &p, int r) {
+    const int len = p.len[r];
+    return len >= 0 && (int64_t)len + (p.append ? p.S : 0) <= p.tcap ? len : -1;
+}
+
+// The query rows of a tile: row r0 + 16 rt + i of `nrows` rows, which are the heads
+// of kv head hd for token tok0, then for the next token; past the last one it again, not
+// to be stored.  len: the cached rows of the tokens' reader, where it is one (else -1)
+template <class OP, int RT>
+__device__ __forceinline__ void take_rows(const SharedParams &p, Rows<OP, RT> &R, int hd, int tok0, int r0, int nrows, int i,
+                                          int g, int len) {
+    const int G = p.group;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        if (CAUSAL || n < OP::KEYS) {
-            const int lim = CAUSAL ? min(n - 1, R.last[rt] - c0) : n - 1;
-#pragma unroll
-            for (int e = 0; e < OP::NS; ++e)
-                if (OP::key_of(e, g) > lim) s[rt][e] = -INFINITY;
+        const int r = r0 + 16 * rt + i;
+        const int rr = min(r, nrows - 1);
+        const int tk = rr / G;
+        const int tok = tok0 + tk;
+        const int at = tok * p.n_q_heads + hd * G + (rr - tk * G);
+        OP::load_q(R.q[rt], (const unsigned char *)p.q + (int64_t)at * OP::ROWB, g);
+        if (p.rope) {
+            const int rd = tok / p.S;
+            const int64_t pos = p.pos0 + (len >= 0 ? len : max(reader_len(p, rd), 0)) + (tok - rd * p.S);
+            OP::rotate_q(R.q[rt], p.rope + pos * OP::DIM, g);
         }
-        float mx = s[rt][0];
+        R.at[rt] = r < nrows ? at : -1;
+        R.tok[rt] = tk;
+    }
+    __builtin_amdgcn_sched_barrier(0);      // the outputs' registers hold loads until here
 #pragma unroll
-        for (int e = 1; e < OP::NS; ++e) mx = fmaxf(mx, s[rt][e]);
-        mx = quad_max(mx) * c2;
-        // the reference is the running maximum: the largest weight is 2^0, which the
-        // 16-bit operand holds without rounding
-        if (__ballot(mx > R.m[rt])) {
-            const float mn = fmaxf(R.m[rt], mx);
+    for (int rt = 0; rt < RT; ++rt) {
+        R.m[rt] = -1e30f;
+        R.l[rt] = OP::no_sum();
+#pragma unroll
+        for (int t = 0; t < OP::NT; ++t) R.o[rt][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+}
+
+// The scores of a stage of n cached keys become weights 2^(c2 s - m).  NB: operands of
+// OP::KEYS keys in the stage.
+// The reference m need not be the maximum: it moves there when a weight exceeds what the
+// operand and the fp32 sums hold (OP::too_large, seen in the operands' bits, so that no
+// maximum is taken otherwise), and weights below it lose nothing, floating as they are.
+template <class OP, int RT, int NB>
+__device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][NB][OP::NS], typename OP::P (&w)[RT][NB], int n,
+                                             float c2, int g) {
+    if (n < NB * OP::KEYS) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int e = 0; e < OP::NS; ++e)
+                    if (b * OP::KEYS + OP::key_of(e, g) >= n) s[rt][b][e] = -INFINITY;
+    }
+    auto weights = [&]() {
+        typename OP::Peak peak = OP::no_peak();
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                float p[OP::NS];
+#pragma unroll
+                for (int e = 0; e < OP::NS; ++e)
+                    p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][b][e], c2, -R.m[rt]));
+                OP::weights(w[rt][b], p);
+                OP::raise(peak, w[rt][b]);
+            }
+        return OP::too_large(peak);
+    };
+    if (__ballot(weights())) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float mx = s[rt][0][0];
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int e = 0; e < OP::NS; ++e) mx = fmaxf(mx, s[rt][b][e]);
+            mx = quad_max(mx) * c2;
+            const float mn = mx > R.m[rt] + OP::kMost ? mx : R.m[rt];      // each row for itself
             const float alpha = __builtin_amdgcn_exp2f(R.m[rt] - mn);
             R.m[rt] = mn;
             R.l[rt] *= alpha;
 #pragma unroll
             for (int t = 0; t < OP::NT; ++t) R.o[rt][t] *= alpha;
         }
-        float p[OP::NS];
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < OP::NS; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][e], c2, -R.m[rt]));
-            sum += p[e];
-        }
-        R.l[rt] += sum;
-        OP::weights(w[rt], p);
+        weights();
     }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) OP::add(R.l[rt], w[rt][b]);
 }
 
-// O += P V of a stage of new rows.  A value that is no number must not reach the rows
-// before it, whose weight for it is 0: a stage that has one goes key by key, each for
-// the rows that see it.
-template <class OP, int RT>
-__device__ __forceinline__ void accumulate_new(Rows<OP, RT> &R, const typename OP::V &v,
-                                               const typename OP::P (&w)[RT], int n, int c0, int g) {
-    if (__ballot(!OP::finite(v)) == 0) {
-        OP::template accumulate<RT>(v, w, R.o);
-        return;
-    }
-    for (int c = 0; c < n; ++c) {
-        bool sees[RT];
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) sees[rt] = c0 + c <= R.last[rt];
-        OP::template accumulate_key<RT>(v, w, R.o, c, sees, g);
-    }
+// Where row `at` of record `rec` keeps O, and (M, l)
+template <class OP>
+__device__ __forceinline__ float *record_o(const SharedParams &p, int64_t rec, int at) {
+    return p.ws + (rec * p.rows + at) * OP::DIM;
+}
+template <class OP>
+__device__ __forceinline__ float2 *record_ml(const SharedParams &p, int64_t rec, int at) {
+    return (float2 *)(p.ws + (int64_t)p.nrec * p.rows * OP::DIM) + rec * p.rows + at;
 }
 
-// Stages first, first + WAVES, ... of `nkeys` consecutive cached rows at kb / vb.
-// K and V have one set of registers each: the next stage's K is asked for when the
-// scores are done, its V when the outputs are.
+// Valid rows of stage t of KEYS rows, of n rows (0 past the last stage)
+template <int KEYS>
+__device__ __forceinline__ int stage_rows(int64_t n, int t) {
+    n -= (int64_t)t * KEYS;
+    return (int)(n < 0 ? 0 : n > KEYS ? KEYS : n);
+}
+
+// ---- by keys
+// A wave's stages first, first + WAVES, ... of `nkeys` cached rows at kb / vb.  K and V have
+// one set of registers each: the next stage's K is asked for when the scores are done,
+// its V when the outputs are.  begin() asks for the first; the caller takes its rows
+// meanwhile.
 template <class OP, int RT>
-__device__ __forceinline__ void cached_keys(Rows<OP, RT> &R, uint64_t kb, uint64_t vb, int64_t nkeys, int first,
-                                            float c2, int i, int g) {
-    constexpr int KEYS = OP::KEYS;
-    const int nst = (int)((nkeys + KEYS - 1) / KEYS);
-    if (first >= nst) return;
-    auto left = [&](int t) {      // valid rows of stage t (0 past the last stage)
-        const int64_t n = nkeys - (int64_t)t * KEYS;
-        return (int)(n < 0 ? 0 : n > KEYS ? KEYS : n);
-    };
-    auto rows_of = [&](uint64_t base, int t) {
-        return row_rsrc(base + (uint64_t)t * KEYS * OP::ROWB, left(t), OP::ROWB, OP::ROWB);
-    };
+struct ByKeys {
+    static constexpr int KEYS = OP::KEYS;
+    uint64_t kb, vb;
+    int64_t nkeys;
+    int first, i, g;
     typename OP::K k;
     typename OP::V v;
-    OP::load_k(k, rows_of(kb, first), OP::ROWB, i, g);
-    OP::load_v(v, rows_of(vb, first), OP::ROWB, i, g);
-    for (int t = first; t < nst; t += WAVES) {
-        float s[RT][OP::NS];
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) OP::scores(k, R.q[rt], s[rt]);
-        __builtin_amdgcn_sched_barrier(0);
-        OP::load_k(k, rows_of(kb, t + WAVES), OP::ROWB, i, g);
-        __builtin_amdgcn_sched_barrier(0);
-        typename OP::P w[RT];
-        softmax_step<OP, RT, false>(R, s, w, left(t), 0, c2, g);
-        OP::template accumulate<RT>(v, w, R.o);
-        __builtin_amdgcn_sched_barrier(0);
-        OP::load_v(v, rows_of(vb, t + WAVES), OP::ROWB, i, g);
-        __builtin_amdgcn_sched_barrier(0);
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(uint64_t base, int t) const {
+        return row_rsrc(base + (uint64_t)t * KEYS * OP::ROWB, stage_rows<KEYS>(nkeys, t), OP::ROWB, OP::ROWB);
     }
-}
+    __device__ __forceinline__ void begin(uint64_t kb_, uint64_t vb_, int64_t nkeys_, int first_, int lane) {
+        kb = kb_; vb = vb_; nkeys = nkeys_; first = first_;
+        i = lane & 15;
+        g = lane >> 4;
+        OP::load_k(k, rows_of(kb, first), OP::ROWB, i, g);
+        OP::load_v(v, rows_of(vb, first), OP::ROWB, i, g);
+    }
+    __device__ __forceinline__ void run(Rows<OP, RT> &R, float c2) {
+        const int nst = (int)((nkeys + KEYS - 1) / KEYS);
+        for (int t = first; t < nst; t += WAVES) {
+            float s[RT][1][OP::NS];
+            typename OP::P w[RT][1];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) OP::scores(k, R.q[rt], s[rt][0]);
+            __builtin_amdgcn_sched_barrier(0);
+            OP::load_k(k, rows_of(kb, t + WAVES), OP::ROWB, i, g);
+            __builtin_amdgcn_sched_barrier(0);
+            softmax_step<OP, RT, 1>(R, s, w, stage_rows<KEYS>(nkeys, t), c2, g);
+            OP::template accumulate<RT>(v, w, R.o);
+            __builtin_amdgcn_sched_barrier(0);
+            OP::load_v(v, rows_of(vb, t + WAVES), OP::ROWB, i, g);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+};
 
 // LDS of the join of one row tile: O of every wave, component c of the lane's four in
 // row c, then (m, l)
@@ -147,14 +211,13 @@ constexpr int join_floats() {
     return obuf_floats<OP>() + 2 * WAVES * 64;
 }
 
-// The four waves' partials: every wave posts its own, then wave w joins component w
-// of each row's outputs (NT consecutive head-dim indices a lane), in wave order, and
-// stores it to record `rec` of the workspace.
+// The partials of the workgroup's waves: every wave posts its own, then joins, in wave
+// order, one component of each row's outputs (NT consecutive head-dim indices a lane) and
+// stores it to record `rec`.
 template <class OP, int RT>
-__device__ __forceinline__ void join(const SharedParams &p, Rows<OP, RT> &R, float *lds, int64_t rec,
-                                     const int (&row)[RT], int wave, int lane) {
-    constexpr int NT = OP::NT, D = OP::DIM;
-    const int g = lane >> 4;
+__device__ __forceinline__ void join(const SharedParams &p, Rows<OP, RT> &R, float *lds, int64_t rec, int wave, int lane) {
+    constexpr int NT = OP::NT;
+    const int g = lane >> 4, c = wave;
     float *ml = lds + obuf_floats<OP>();
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -165,350 +228,345 @@ __device__ __forceinline__ void join(const SharedParams &p, Rows<OP, RT> &R, flo
             for (int t = 0; t < NT; t += 4)
                 *(f32x4 *)(lds + ((wave * 4 + c) * 64 + lane) * NT + t) =
                     (f32x4){R.o[rt][t][c], R.o[rt][t + 1][c], R.o[rt][t + 2][c], R.o[rt][t + 3][c]};
-        *(float2 *)(ml + (wave * 64 + lane) * 2) = make_float2(R.m[rt], R.l[rt]);
+        *(float2 *)(ml + (wave * 64 + lane) * 2) = make_float2(R.m[rt], OP::total(R.l[rt]));
         __syncthreads();
-        float2 w[WAVES];
-        float M = -INFINITY;
-#pragma unroll
-        for (int s = 0; s < WAVES; ++s) {
-            w[s] = *(const float2 *)(ml + (s * 64 + lane) * 2);
-            M = fmaxf(M, w[s].x);
-        }
-        float l = 0.f;
+        float M = -INFINITY, l = 0.f;
         f32x4 acc[NT / 4];
 #pragma unroll
         for (int t = 0; t < NT / 4; ++t) acc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
+        for (int s = 0; s < WAVES; ++s) M = fmaxf(M, ml[(s * 64 + lane) * 2]);
+#pragma unroll
         for (int s = 0; s < WAVES; ++s) {
-            const float a = __builtin_amdgcn_exp2f(w[s].x - M);
-            l = __builtin_fmaf(a, w[s].y, l);
+            const float2 w = *(const float2 *)(ml + (s * 64 + lane) * 2);
+            const float a = __builtin_amdgcn_exp2f(w.x - M);
+            l = __builtin_fmaf(a, w.y, l);
 #pragma unroll
             for (int t = 0; t < NT / 4; ++t) {
-                const f32x4 x = *(const f32x4 *)(lds + ((s * 4 + wave) * 64 + lane) * NT + 4 * t);
+                const f32x4 x = *(const f32x4 *)(lds + ((s * 4 + c) * 64 + lane) * NT + 4 * t);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) acc[t][c] = __builtin_fmaf(a, x[c], acc[t][c]);
+                for (int e = 0; e < 4; ++e) acc[t][e] = __builtin_fmaf(a, x[e], acc[t][e]);
             }
         }
-        l = quad_sum(l);
-        if (row[rt] < 0) continue;
-        float *po = p.ws + (rec * p.rows + row[rt]) * D + NT * (4 * g + wave);
+        if (R.at[rt] < 0) continue;
+        float *po = record_o<OP>(p, rec, R.at[rt]) + NT * (4 * g + c);
 #pragma unroll
         for (int t = 0; t < NT / 4; ++t) *(f32x4 *)(po + 4 * t) = acc[t];
-        if (wave == 0 && g == 0)
-            *(float2 *)(p.ws + (int64_t)p.nrec * p.rows * D + (rec * p.rows + row[rt]) * 2) = make_float2(M, l);
-    }
-}
-
-// Cached rows of reader r, or -1 if it takes no part
-__device__ __forceinline__ int reader_len(const SharedParams &p, int r) {
-    const int len = p.len[r];
-    return len >= 0 && (int64_t)len + (p.append ? p.S : 0) <= p.tcap ? len : -1;
-}
-
-// The query rows of a tile: row r0 + 16 rt + i of `nrows` rows, which are the heads
-// of kv head g for token tok0, then for the next token
-template <class OP, int RT>
-__device__ __forceinline__ void take_rows(const SharedParams &p, Rows<OP, RT> &R, int (&row)[RT], int head_g,
-                                          int tok0, int r0, int nrows, int i, int g) {
-    const int G = p.group;
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const int r = r0 + 16 * rt + i;
-        const int rr = min(r, nrows - 1);         // rows past the last repeat it and are not stored
-        const int tk = rr / G;
-        const int tok = tok0 + tk;
-        const int at = tok * p.n_q_heads + head_g * G + (rr - tk * G);
-        OP::load_q(R.q[rt], (const unsigned char *)p.q + (int64_t)at * OP::ROWB, g);
-        if (p.rope) {
-            const int rd = tok / p.S;
-            const int64_t pos = p.pos0 + max(reader_len(p, rd), 0) + (tok - rd * p.S);
-            OP::rotate_q(R.q[rt], p.rope + pos * OP::DIM, g);
-        }
-        row[rt] = r < nrows ? at : -1;
-        R.last[rt] = tk;
-        R.m[rt] = -1e30f;
-        R.l[rt] = 0.f;
-#pragma unroll
-        for (int t = 0; t < OP::NT; ++t) R.o[rt][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        if (c == 0 && g == 0) *record_ml<OP>(p, rec, R.at[rt]) = make_float2(M, l);
     }
 }
 
 // ---- by rows
-constexpr int SLOTS = 3;      // stages in LDS: one read, one landed or landing, one asked for
-
-// One stage from LDS.  CAUSAL: new rows, the first of which is row c0.
-template <class OP, class RG, int RT, bool CAUSAL>
-__device__ __forceinline__ void row_stage(Rows<OP, RT> &R, const unsigned char *ks_, const unsigned char *vs_, uint32_t ka,
-                                          uint32_t va, int n, int c0, float c2, int g) {
-    f32x4 a[RT][2];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) a[rt][h] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int ks = 0; ks < OP::NK; ++ks)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const u32x4 k = RG::row_frag(ks_, ka, h, ks);
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) a[rt][h] = OP::mfma(k, R.q[rt].f[ks], a[rt][h]);
-        }
-    float s[RT][OP::NS];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int e = 0; e < OP::NS; ++e) s[rt][e] = a[rt][e >> 2][e & 3];
-    typename OP::P w[RT];
-    softmax_step<OP, RT, CAUSAL>(R, s, w, n, c0, c2, g);
-    if constexpr (CAUSAL) {
-        // as accumulate_new: a value that is no number reaches the rows that see it alone
-        bool ok = true;
-#pragma unroll
-        for (int t = 0; t < OP::NT; ++t) ok = ok && OP::finite_words(RG::col_frag(vs_, va, t));
-        if (__ballot(!ok)) {
-            for (int c = 0; c < n; ++c)
-#pragma unroll
-                for (int t = 0; t < OP::NT; ++t) {
-                    const u32x4 v = OP::only_key(RG::col_frag(vs_, va, t), c, g);
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        const f32x4 x = OP::mfma(v, w[rt].f, R.o[rt][t]);
-                        R.o[rt][t] = c0 + c <= R.last[rt] ? x : R.o[rt][t];
-                    }
-                }
-            return;
-        }
-    }
-#pragma unroll
-    for (int t = 0; t < OP::NT; ++t) {
-        const u32x4 v = RG::col_frag(vs_, va, t);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) R.o[rt][t] = OP::mfma(v, w[rt].f, R.o[rt][t]);
-    }
-}
-
-// All stages of `nkeys` cached rows
+// One stage from LDS
 template <class OP, class RG, int RT>
-__device__ __forceinline__ void row_cached(Rows<OP, RT> &R, uint64_t kb, uint64_t vb, int64_t nkeys, unsigned char *lds,
-                                           float c2, int wave, int lane) {
-    const int i = lane & 15, g = lane >> 4;
-    const uint32_t ka = RG::row_at(i, g), va = RG::col_at(i, g);
-    const int nst = (int)((nkeys + RG::KEYS - 1) / RG::KEYS);
-    auto count = [&](int t) { return (int)min(nkeys - (int64_t)t * RG::KEYS, (int64_t)RG::KEYS); };
-    auto load = [&](int t, int slot) {
-        const uint64_t off = (uint64_t)t * RG::KEYS * OP::ROWB;
-        unsigned char *to = lds + slot * 2 * RG::HALF;
-        RG::load(kb + off, OP::ROWB, count(t), to, wave, lane);
-        RG::load(vb + off, OP::ROWB, count(t), to + RG::HALF, wave, lane);
-    };
-    if (nst > 0) load(0, 0);
-    if (nst > 1) load(1, 1);
-    int slot = 0;
-    for (int t = 0; t < nst; ++t) {
-        // this wave's part of stage t has landed (stage t + 1 may be on its way); behind the
-        // barrier everybody's has, and nobody reads the slot of stage t - 1 any more
-        if (t + 1 < nst) wait_vmcnt<2 * RG::LOADS>();
-        else wait_vmcnt<0>();
-        barrier_lds();
-        if (t + 2 < nst) load(t + 2, slot == 0 ? 2 : slot - 1);
-        const unsigned char *st = lds + slot * 2 * RG::HALF;
-        row_stage<OP, RG, RT, false>(R, st, st + RG::HALF, ka, va, count(t), 0, c2, g);
-        slot = slot == SLOTS - 1 ? 0 : slot + 1;
+__device__ __forceinline__ void row_stage(Rows<OP, RT> &R, const unsigned char *ks_, const unsigned char *vs_, uint32_t ka,
+                                          uint32_t va, int n, float c2, int g) {
+    constexpr int NB = RG::KEYS / OP::KEYS;
+    float s[RT][NB][OP::NS];
+    typename OP::P w[RT][NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        f32x4 a[RT][2];
+#pragma unroll
+        for (int ks = 0; ks < OP::NK; ++ks)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const u32x4 k = RG::row_frag(ks_, ka, 2 * b + h, ks);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+                    a[rt][h] = OP::mfma(k, R.q[rt].f[ks], ks ? a[rt][h] : (f32x4){0.f, 0.f, 0.f, 0.f});
+            }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int e = 0; e < OP::NS; ++e) s[rt][b][e] = a[rt][e >> 2][e & 3];
     }
-    barrier_lds();
+    softmax_step<OP, RT, NB>(R, s, w, n, c2, g);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int t = 0; t < OP::NT; ++t) {
+            const u32x4 v = RG::col_frag(vs_ + b * OP::KEYS * OP::ROWB, va, t);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) R.o[rt][t] = OP::mfma(v, w[rt][b].f, R.o[rt][t]);
+        }
 }
+
+// The stages of `nkeys` cached rows at kb / vb, in SLOTS slots of LDS: one is read while the
+// others are on their way.  begin() asks for the first; the caller takes its rows
+// meanwhile, and run() first waits for all of it: loads that the compiler knows of must
+// not be on their way when the loop begins, or it waits for every load in it.
+constexpr int SLOTS = 3;
+
+template <class OP, class RG, int RT>
+struct ByRows {
+    uint64_t kb, vb;
+    int64_t nkeys;
+    unsigned char *lds;
+    int nst, wave, lane;
+    __device__ __forceinline__ void load(int t, int slot) const {
+        const uint64_t off = (uint64_t)t * RG::KEYS * OP::ROWB;
+        const int n = stage_rows<RG::KEYS>(nkeys, t);
+        unsigned char *to = lds + slot * 2 * RG::HALF;
+        RG::template load<false>(kb + off, OP::ROWB, n, to, wave, lane);
+        RG::template load<true>(vb + off, OP::ROWB, n, to + RG::HALF, wave, lane);
+    }
+    __device__ __forceinline__ void begin(uint64_t kb_, uint64_t vb_, int64_t nkeys_, unsigned char *lds_, int wave_, int lane_) {
+        kb = kb_; vb = vb_; nkeys = nkeys_; lds = lds_; wave = wave_; lane = lane_;
+        nst = (int)((nkeys + RG::KEYS - 1) / RG::KEYS);
+        for (int t = 0; t < SLOTS - 1 && t < nst; ++t) load(t, t);
+    }
+    __device__ __forceinline__ void run(Rows<OP, RT> &R, float c2) const {
+        const int i = lane & 15, g = lane >> 4;
+        const uint32_t ka = RG::row_at(i, g), va = RG::col_at(i, g);
+        wait_vmcnt<0>();
+        int slot = 0;
+        for (int t = 0; t < nst; ++t) {
+            // this wave's part of stage t has landed (the SLOTS - 2 behind it may be on their
+            // way); behind the barrier everybody's has, and nobody reads the slot of stage
+            // t - 1 any more
+            if (t + SLOTS - 2 < nst) wait_vmcnt<(SLOTS - 2) * 2 * RG::LOADS>();
+            else wait_vmcnt<0>();
+            barrier_lds();
+            if (t + SLOTS - 1 < nst) load(t + SLOTS - 1, slot == 0 ? SLOTS - 1 : slot - 1);
+            const unsigned char *st = lds + slot * 2 * RG::HALF;
+            row_stage<OP, RG, RT>(R, st, st + RG::HALF, ka, va, stage_rows<RG::KEYS>(nkeys, t), c2, g);
+            slot = slot == SLOTS - 1 ? 0 : slot + 1;
+        }
+    }
+};
 
 // The partial of the wave's own rows
 template <class OP, int RT>
-__device__ __forceinline__ void put_rows(const SharedParams &p, Rows<OP, RT> &R, int64_t rec, const int (&row)[RT], int g) {
-    constexpr int D = OP::DIM;
+__device__ __forceinline__ void put_rows(const SharedParams &p, const Rows<OP, RT> &R, int64_t rec, int g) {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const float l = quad_sum(R.l[rt]);
-        if (row[rt] < 0) continue;
-        float *po = p.ws + (rec * p.rows + row[rt]) * D + 4 * g;
+        const float l = OP::total(R.l[rt]);
+        if (R.at[rt] < 0) continue;
+        float *po = record_o<OP>(p, rec, R.at[rt]) + 4 * g;
 #pragma unroll
         for (int t = 0; t < OP::NT; ++t) *(f32x4 *)(po + 16 * t) = R.o[rt][t];
-        if (g == 0) *(float2 *)(p.ws + (int64_t)p.nrec * p.rows * D + (rec * p.rows + row[rt]) * 2) = make_float2(R.m[rt], l);
+        if (g == 0) *record_ml<OP>(p, rec, R.at[rt]) = make_float2(R.m[rt], l);
     }
 }
 
 // ---- items
 // WAY: 1 or 2: by keys, that many 16-row tiles; kByRows + 1 or 2: by rows, that many in
 // each wave
-constexpr int kTiles(int way) { return way > kByRows ? way - kByRows : way; }
-constexpr int kRowsOf(int way) { return way > kByRows ? 64 * (way - kByRows) : 16 * way; }
+constexpr int tiles_of(int way) { return way > kByRows ? way - kByRows : way; }
+constexpr int rows_of(int way) { return way > kByRows ? 64 * (way - kByRows) : 16 * way; }
 
 template <class OP, int WAY>
 constexpr int lds_bytes() {
-    return WAY > kByRows ? SLOTS * 64 * OP::ROWB : join_floats<OP>() * 4;
+    if constexpr (WAY > kByRows) return SLOTS * 2 * OP::Ring::HALF;
+    else return join_floats<OP>() * 4;
+}
+
+// Rows r0 .. of `nrows` query rows (take_rows) over `nkeys` cached rows at k / v, to record
+// `rec`
+struct Item {
+    uint64_t k, v;
+    int64_t nkeys, rec;
+    int hd, tok0, r0, nrows, len;
+};
+
+template <class OP, int WAY>
+__device__ __forceinline__ void attend(const SharedParams &p, const Item &it, unsigned char *lds, int wave, int lane) {
+    constexpr int RT = tiles_of(WAY);
+    const int i = lane & 15, g = lane >> 4;
+    Rows<OP, RT> R;
+    if constexpr (WAY > kByRows) {
+        ByRows<OP, typename OP::Ring, RT> keys;
+        keys.begin(it.k, it.v, it.nkeys, lds, wave, lane);
+        take_rows(p, R, it.hd, it.tok0, it.r0 + wave * 16 * RT, it.nrows, i, g, it.len);
+        keys.run(R, p.scale_log2);
+        put_rows<OP, RT>(p, R, it.rec, g);
+    } else {
+        ByKeys<OP, RT> keys;
+        keys.begin(it.k, it.v, it.nkeys, wave, lane);
+        take_rows(p, R, it.hd, it.tok0, it.r0, it.nrows, i, g, it.len);
+        keys.run(R, p.scale_log2);
+        join<OP, RT>(p, R, (float *)lds, it.rec, wave, lane);
+    }
 }
 
 // Prefix item (oct, in8): the (kv head, split) pairs in groups of eight, a group's row
 // tiles one after the other.  Blocks eight apart share an XCD, so the tiles that read
 // one range of prefix rows find it in one L2.
 template <class OP, int WAY>
-__device__ __forceinline__ void prefix_item(const SharedParams &p, uint32_t oct, uint32_t in8, unsigned char *lds) {
-    constexpr int RT = kTiles(WAY);
-    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+__device__ __forceinline__ void prefix_item(const SharedParams &p, uint32_t oct, uint32_t in8, unsigned char *lds, int wave,
+                                            int lane) {
     const uint32_t pair = oct / p.p_tiles * 8 + in8;
-    const int tile = (int)(oct % p.p_tiles);
-    const int split = (int)(pair / p.n_kv_heads), hd = (int)(pair % p.n_kv_heads);
+    const int split = (int)(pair / p.n_kv_heads);
     if (split >= p.np) return;
-    const int64_t kb = split * p.chunk, ke = min(kb + p.chunk, p.L);
-    const uint64_t off = ((uint64_t)hd * p.cap + kb) * OP::ROWB;
-    const uint64_t k0 = (uint64_t)(uintptr_t)p.kc + off, v0 = (uint64_t)(uintptr_t)p.vc + off;
-    Rows<OP, RT> R;
-    int row[RT];
-    if constexpr (WAY > kByRows) {
-        take_rows(p, R, row, hd, 0, tile * kRowsOf(WAY) + wave * 16 * RT, p.n * p.S * p.group, i, g);
-        row_cached<OP, typename OP::Ring, RT>(R, k0, v0, ke - kb, lds, p.scale_log2, wave, lane);
-        put_rows<OP, RT>(p, R, split, row, g);
-    } else {
-        take_rows(p, R, row, hd, 0, tile * 16 * RT, p.n * p.S * p.group, i, g);
-        cached_keys<OP, RT>(R, k0, v0, ke - kb, wave, p.scale_log2, i, g);
-        join<OP, RT>(p, R, (float *)lds, split, row, wave, lane);
-    }
+    Item it;
+    it.hd = (int)(pair % p.n_kv_heads);
+    const int64_t kb = split * p.chunk;
+    const uint64_t off = ((uint64_t)it.hd * p.cap + kb) * OP::ROWB;
+    it.k = (uint64_t)(uintptr_t)p.kc + off;
+    it.v = (uint64_t)(uintptr_t)p.vc + off;
+    it.nkeys = min(p.chunk, p.L - kb);
+    it.rec = split;
+    it.tok0 = 0;
+    it.r0 = (int)(oct % p.p_tiles) * rows_of(WAY);
+    it.nrows = p.n * p.S * p.group;
+    it.len = -1;
+    attend<OP, WAY>(p, it, lds, wave, lane);
 }
 
-// Own item b: (split, reader, row tile, kv head), kv head fastest.  The splits have equal
-// shares of the cached rows, in whole stages of four waves; the last has the new rows too.
+// Own item x: (split, reader, row tile, kv head), kv head
+// fastest.  The splits have equal shares of the cached rows, in whole stages.
 template <class OP, int WAY>
-__device__ __forceinline__ void own_item(const SharedParams &p, uint32_t b, unsigned char *lds) {
-    constexpr int RT = kTiles(WAY), KEYS = OP::KEYS;
-    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int hd = (int)(b % p.n_kv_heads);
-    b /= p.n_kv_heads;
-    const int tile = (int)(b % p.t_tiles);
-    b /= p.t_tiles;
-    const int rd = (int)(b % p.n), split = (int)(b / p.n);
+__device__ __forceinline__ void own_item(const SharedParams &p, uint32_t x, unsigned char *lds, int wave, int lane) {
+    constexpr int KEYS = OP::KEYS;
+    Item it;
+    it.hd = (int)(x % p.n_kv_heads);
+    x /= p.n_kv_heads;
+    const int tile = (int)(x % p.t_tiles);
+    x /= p.t_tiles;
+    const int rd = (int)(x % p.n), split = (int)(x / p.n);
     if (split >= p.nt) return;
+    it.len = reader_len(p, rd);
+    if (it.len < 0) return;
+    const int chunk = ((it.len + p.nt - 1) / p.nt + KEYS - 1) / KEYS * KEYS;
+    const int64_t kb = min((int64_t)split * chunk, (int64_t)it.len);
+    it.nkeys = min((int64_t)chunk, it.len - kb);
+    const uint64_t off = (((uint64_t)rd * p.n_kv_heads + it.hd) * p.tcap + kb) * OP::ROWB;
+    it.k = (uint64_t)(uintptr_t)p.kt + off;
+    it.v = (uint64_t)(uintptr_t)p.vt + off;
+    it.rec = p.np + split;
+    it.tok0 = rd * p.S;
+    it.r0 = tile * rows_of(WAY);
+    it.nrows = p.S * p.group;
+    attend<OP, WAY>(p, it, lds, wave, lane);
+}
+
+// New item x, a wave's: (reader, 16-row tile, kv head), kv head fastest
+template <class OP>
+__device__ __forceinline__ void new_item(const SharedParams &p, uint32_t x, int lane) {
+    constexpr int KEYS = 16, NT = OP::NT;      // (one part of a 16-bit stage: fewer registers)
+    int i = lane & 15, g = lane >> 4;
+    const int hd = (int)(x % p.n_kv_heads);
+    x /= p.n_kv_heads;
+    const int nrows = p.S * p.group, tiles = (nrows + 15) / 16;
+    const int tile = (int)(x % tiles), rd = (int)(x / tiles);
+    if (rd >= p.n) return;
     const int len = reader_len(p, rd);
     if (len < 0) return;
-    const int r0 = tile * kRowsOf(WAY), nrows = p.S * p.group;
-    const int share = (len + p.nt - 1) / p.nt;
-    const int chunk = (share + KEYS - 1) / KEYS * KEYS;
-    const int64_t kb = (int64_t)split * chunk;
-    const int64_t nk = max((int64_t)0, min((int64_t)chunk, len - kb));
-    const uint64_t head = (uint64_t)rd * p.n_kv_heads + hd;
-    const uint64_t off = (head * p.tcap + kb) * OP::ROWB;
-    const uint64_t k0 = (uint64_t)(uintptr_t)p.kt + off, v0 = (uint64_t)(uintptr_t)p.vt + off;
     // new rows that a row of this tile sees; the last tile sees all and stores them
-    const int seen = split == p.nt - 1 ? min(p.S, (min(r0 + kRowsOf(WAY), nrows) - 1) / p.group + 1) : 0;
-    const bool store = p.append && tile == p.t_tiles - 1;
+    const int seen = min(p.S, (min(tile * 16 + 16, nrows) - 1) / p.group + 1);
+    const bool store = p.append && tile == tiles - 1;
     const uint32_t nb = (uint32_t)p.n_kv_heads * OP::ROWB;
     const uint64_t src = ((uint64_t)rd * p.S * p.n_kv_heads + hd) * OP::ROWB;
-    const uint64_t kn = (uint64_t)(uintptr_t)p.kn + src, vn = (uint64_t)(uintptr_t)p.vn + src;
-    const uint64_t to = (head * p.tcap + len) * OP::ROWB;
-    unsigned char *kd = (unsigned char *)p.kt + to, *vd = (unsigned char *)p.vt + to;
-    Rows<OP, RT> R;
-    int row[RT];
-    if constexpr (WAY > kByRows) {
-        using RG = typename OP::Ring;
-        take_rows(p, R, row, hd, rd * p.S, r0 + wave * 16 * RT, nrows, i, g);
-        row_cached<OP, RG, RT>(R, k0, v0, nk, lds, p.scale_log2, wave, lane);
-        for (int c0 = 0; c0 < seen; c0 += KEYS) {
-            // the stage's rows through registers: a thread has chunk c of a row and the one
-            // half a row further, whose dims are each other's partners in the rotation
-            constexpr int PAIRS = RG::CH / 2;
-            const int n = min(seen - c0, KEYS);
-            const int r = threadIdx.x / PAIRS, c = threadIdx.x % PAIRS;
-            if (r < KEYS) {
-                u32x4 k[2], v[2];
+    const uint64_t to = (((uint64_t)rd * p.n_kv_heads + hd) * p.tcap + len) * OP::ROWB;
+    Rows<OP, 1> R;
+    typename OP::K k;
+    typename OP::V v;
+    auto load = [&](int c0) {
+        const int n = min(seen - c0, KEYS);
+        const uint64_t at = src + (uint64_t)c0 * nb;
+        OP::template load_k<1>(k, row_rsrc((uint64_t)(uintptr_t)p.kn + at, n, nb, OP::ROWB), nb, i, g);
+        OP::template load_v<1>(v, row_rsrc((uint64_t)(uintptr_t)p.vn + at, n, nb, OP::ROWB), nb, i, g);
+    };
+    load(0);
+    take_rows(p, R, hd, rd * p.S, tile * 16, nrows, i, g, len);
+    for (int c0 = 0; c0 < seen; c0 += KEYS) {
+        const int n = min(seen - c0, KEYS);
+        asm volatile("" : "+v"(i), "+v"(g));      // addresses are made in the loop: registers for all are not there
+        if (c0) load(c0);
+        if (p.rope) OP::template rotate_k<1>(k, p.rope + (p.pos0 + len + c0) * OP::DIM, n, i, g);
+        if (store)
+            OP::template store<1>(k, v, (unsigned char *)p.kt + to + (uint64_t)c0 * OP::ROWB,
+                                  (unsigned char *)p.vt + to + (uint64_t)c0 * OP::ROWB, n, i, g);
+        __builtin_amdgcn_sched_barrier(0);
+        float s[OP::NS];
+        typename OP::P w[1][1];
+        OP::scores(k, R.q[0], s);
+        const int lim = min(n - 1, R.tok[0] - c0);
+        float mx = -INFINITY;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) k[h] = v[h] = (u32x4){0u, 0u, 0u, 0u};
-                if (r < n) {
-                    const uint64_t at = (uint64_t)(c0 + r) * nb + 16 * c;
+        for (int e = 0; e < OP::NS; ++e) {
+            s[e] = OP::key_of(e, g) > lim ? -INFINITY : s[e];
+            mx = fmaxf(mx, s[e]);
+        }
+        const float mn = fmaxf(R.m[0], quad_max(mx) * p.scale_log2);
+        if (c0) {
+            const float alpha = __builtin_amdgcn_exp2f(R.m[0] - mn);
+            R.l[0] *= alpha;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        k[h] = *(const u32x4 *)(uintptr_t)(kn + at + 16 * PAIRS * h);
-                        v[h] = *(const u32x4 *)(uintptr_t)(vn + at + 16 * PAIRS * h);
-                    }
-                    if (p.rope) OP::rotate8(k[0], k[1], p.rope + (p.pos0 + len + c0 + r) * OP::DIM + 16 * c);
-                    if (store) {
-                        const uint64_t d = (uint64_t)(c0 + r) * OP::ROWB + 16 * c;
+            for (int t = 0; t < NT; ++t) R.o[0][t] *= alpha;
+        }
+        R.m[0] = mn;
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            *(u32x4 *)(kd + d + 16 * PAIRS * h) = k[h];
-                            *(u32x4 *)(vd + d + 16 * PAIRS * h) = v[h];
-                        }
-                    }
-                }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    unsigned char *l = lds + r * OP::ROWB + 16 * ((c + PAIRS * h) ^ RG::swz(r));
-                    *(u32x4 *)l = k[h];
-                    *(u32x4 *)(l + RG::HALF) = v[h];
-                }
+        for (int e = 0; e < OP::NS; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], p.scale_log2, -mn));
+        OP::weights(w[0][0], s);
+        OP::add(R.l[0], w[0][0]);
+        // A value that is no number must not reach the rows before it, whose weight for it is
+        // 0: a stage that has one goes key by key, each for the rows that see it.
+        if (__ballot(!OP::finite(v)) == 0) {
+            OP::template accumulate<1>(v, w, R.o);
+        } else {
+            for (int c = 0; c < n; ++c) {
+                const bool sees[1] = {c0 + c <= R.tok[0]};
+                OP::template accumulate_key<1>(v, w, R.o, c, sees, g);
             }
-            barrier_lds();
-            row_stage<OP, RG, RT, true>(R, lds, lds + RG::HALF, RG::row_at(i, g), RG::col_at(i, g), n, c0, p.scale_log2, g);
-            barrier_lds();
         }
-        put_rows<OP, RT>(p, R, p.np + split, row, g);
-    } else {
-        take_rows(p, R, row, hd, rd * p.S, r0, nrows, i, g);
-        // (16-bit: 16 query rows are 16 tokens at most, one part of a stage.)  Stage c of the
-        // new rows goes to the wave whose turn follows the cached stages
-        const int nst = (int)((nk + KEYS - 1) / KEYS);
-        for (int c = (wave - nst) & (WAVES - 1); c * KEYS < seen; c += WAVES) {
-            const int c0 = c * KEYS, n = min(seen - c0, KEYS);
-            typename OP::K k;
-            typename OP::V v;
-            const uint64_t at = (uint64_t)c0 * nb;
-            OP::template load_k<1>(k, row_rsrc(kn + at, n, nb, OP::ROWB), nb, i, g);
-            OP::template load_v<1>(v, row_rsrc(vn + at, n, nb, OP::ROWB), nb, i, g);
-            if (p.rope) OP::template rotate_k<1>(k, p.rope + (p.pos0 + len + c0) * OP::DIM, n, i, g);
-            if (store) OP::template store<1>(k, v, kd + (uint64_t)c0 * OP::ROWB, vd + (uint64_t)c0 * OP::ROWB, n, i, g);
-            float sc[RT][OP::NS];
-            typename OP::P w[RT];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) OP::scores(k, R.q[rt], sc[rt]);
-            softmax_step<OP, RT, true>(R, sc, w, n, c0, p.scale_log2, g);
-            accumulate_new<OP, RT>(R, v, w, n, c0, g);
-        }
-        cached_keys<OP, RT>(R, k0, v0, nk, wave, p.scale_log2, i, g);
-        join<OP, RT>(p, R, (float *)lds, p.np + split, row, wave, lane);
     }
+    const float l = OP::total(R.l[0]);
+    if (R.at[0] < 0) return;
+    float *po = record_o<OP>(p, p.nrec - 1, R.at[0]) + NT * 4 * g;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int t = 0; t < NT; t += 4)
+            *(f32x4 *)(po + NT * c + t) = (f32x4){R.o[0][t][c], R.o[0][t + 1][c], R.o[0][t + 2][c], R.o[0][t + 3][c]};
+    if (g == 0) *record_ml<OP>(p, p.nrec - 1, R.at[0]) = make_float2(R.m[0], l);
 }
 
 // PW, OW: the ways of prefix and own items
 template <class OP, int PW, int OW>
-__global__ __launch_bounds__(256, OP::ELT == 2 ? 3 : OW == 1 ? 2 : 1) void shared_kernel(const SharedParams p) {
+__global__ __launch_bounds__(256, OP::ELT == 2 ? 3 : 2) void shared_kernel(const SharedParams p) {
     constexpr int LP = lds_bytes<OP, PW>(), LO = lds_bytes<OP, OW>();
     __shared__ __attribute__((aligned(1024))) unsigned char lds[LP > LO ? LP : LO];
-    // blocks in groups of eight (one for each XCD), the own items' groups spread evenly
-    // among the prefix items': the first are bound by memory, the second by the
-    // matrix and vector units
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // Blocks in groups of eight, one for each XCD: prefix items, own items, new items.
     const uint32_t oct = blockIdx.x / 8, in8 = blockIdx.x % 8;
-    const uint32_t before = (uint32_t)(oct * p.own_share >> 32), upto = (uint32_t)((oct + 1) * p.own_share >> 32);
-    if (upto > before) own_item<OP, OW>(p, before * 8 + in8, lds);
-    else prefix_item<OP, PW>(p, oct - upto, in8, lds);
+    if (oct < p.oct_own) prefix_item<OP, PW>(p, oct, in8, lds, wave, lane);
+    else if (oct < p.oct_new) own_item<OP, OW>(p, (oct - p.oct_own) * 8 + in8, lds, wave, lane);
+    else new_item<OP>(p, ((oct - p.oct_new) * 8 + in8) * WAVES + wave, lane);
 }
 
-// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over the records of a row, in
-// record order.  D / 4 lanes a row, four values a lane.
+// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over the records of a row.  A wave
+// takes 64 / (D / 4) rows, four values a lane; the workgroup's waves take the records in
+// turn, and their sums are joined in wave order.
+constexpr int MERGE_WAVES = 4;
+
 template <class OP>
-__global__ __launch_bounds__(64) void shared_merge_kernel(const SharedParams p) {
-    constexpr int D = OP::DIM, LANES = D / 4, BATCH = 8;
-    const int64_t row = (int64_t)blockIdx.x * (64 / LANES) + threadIdx.x / LANES;
-    const int d = threadIdx.x % LANES * 4;
-    if (row >= p.rows) return;
-    if (reader_len(p, (int)(row / ((int64_t)p.n_q_heads * p.S))) < 0) return;
+__global__ __launch_bounds__(64 * MERGE_WAVES) void shared_merge_kernel(const SharedParams p) {
+    constexpr int D = OP::DIM, LANES = D / 4, BATCH = 4;
+    __shared__ f32x4 sums[MERGE_WAVES][64];
+    __shared__ float2 mls[MERGE_WAVES][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t at_row = (int64_t)blockIdx.x * (64 / LANES) + lane / LANES, row = min(at_row, p.rows - 1);
+    const int d = lane % LANES * 4;
+    const bool on = at_row < p.rows && reader_len(p, (int)(row / ((int64_t)p.n_q_heads * p.S))) >= 0;
     const float *o = p.ws + row * D + d;
     const float *ml = p.ws + (int64_t)p.nrec * p.rows * D + row * 2;
     float M = -1e30f, l = 0.f;
     f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < p.nrec; s0 += BATCH) {
+    for (int s0 = wave; s0 < p.nrec; s0 += MERGE_WAVES * BATCH) {
         f32x4 x[BATCH];
         float2 w[BATCH];
 #pragma unroll
         for (int s = 0; s < BATCH; ++s) {
-            const int64_t at = (int64_t)min(s0 + s, p.nrec - 1) * p.rows;
-            x[s] = *(const f32x4 *)(o + at * D);
-            w[s] = *(const float2 *)(ml + at * 2);
+            const int r = s0 + s * MERGE_WAVES;
+            w[s] = make_float2(-1e30f, 0.f);
+            x[s] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            if (r < p.nrec) {
+                x[s] = *(const f32x4 *)(o + r * p.rows * D);
+                w[s] = *(const float2 *)(ml + r * p.rows * 2);
+            }
         }
         float mx = M;
 #pragma unroll
@@ -519,11 +577,27 @@ __global__ __launch_bounds__(64) void shared_merge_kernel(const SharedParams p) 
         acc *= a;
 #pragma unroll
         for (int s = 0; s < BATCH; ++s) {
-            const float b = s0 + s < p.nrec ? __builtin_amdgcn_exp2f(w[s].x - M) : 0.f;
+            const float b = __builtin_amdgcn_exp2f(w[s].x - M);
             l = __builtin_fmaf(b, w[s].y, l);
 #pragma unroll
             for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(b, x[s][c], acc[c]);
         }
+    }
+    sums[wave][lane] = acc;
+    mls[wave][lane] = make_float2(M, l);
+    __syncthreads();
+    if (wave || !on) return;
+    float top = M;
+#pragma unroll
+    for (int s = 1; s < MERGE_WAVES; ++s) top = fmaxf(top, mls[s][lane].x);
+    float a = __builtin_amdgcn_exp2f(M - top);
+    l *= a;
+    acc *= a;
+#pragma unroll
+    for (int s = 1; s < MERGE_WAVES; ++s) {
+        a = __builtin_amdgcn_exp2f(mls[s][lane].x - top);
+        l = __builtin_fmaf(a, mls[s][lane].y, l);
+        acc += a * sums[s][lane];
     }
     const float inv = l > 0.f ? 1.f / l : 0.f;
     OP::put4((unsigned char *)p.out + row * OP::ROWB, d, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
@@ -546,7 +620,7 @@ hipError_t launch_op(const SharedParams &p, int pw, int ow, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int per = 64 / (OP::DIM / 4);
-    hipLaunchKernelGGL(shared_merge_kernel<OP>, dim3((unsigned)((p.rows + per - 1) / per)), dim3(64), 0, s, p);
+    hipLaunchKernelGGL(shared_merge_kernel<OP>, dim3((unsigned)((p.rows + per - 1) / per)), dim3(64 * MERGE_WAVES), 0, s, p);
     return hipGetLastError();
 }
 

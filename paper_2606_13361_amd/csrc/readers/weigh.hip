@@ -63,26 +63,44 @@ __device__ __forceinline__ void mask(float (&s)[OP::NS], int lim, int g) {
         if (OP::key_of(e, g) > lim) s[e] = -INFINITY;
 }
 
-constexpr float kSlack = 60.f;
+constexpr float kMost = 56.f, kSlack = 0x1p60f;
 
-// A stage's scores into the lane's running reference and sum
-template <class OP>
-__device__ __forceinline__ void add_scores(const float (&s)[OP::NS], float c2, float &m, float &l) {
-    float mx = s[0];
+// A stage's scores of RT row tiles into the lane's running references and sums.  A
+// reference need not be the maximum, only near enough: it moves there when a sum of
+// terms 2^(c2 s - m) grows too large (or is no number), and nothing is rounded
+// differently for it.  2^31 stages of up to kSlack (16 terms of 2^kMost) stay below the
+// type's largest value.
+template <class OP, int RT>
+__device__ __forceinline__ void add_scores(const float (&s)[RT][OP::NS], float c2, float (&m)[RT], float (&l)[RT]) {
+    float sum[RT];
+    auto sums = [&]() {
+        bool over = false;
 #pragma unroll
-    for (int e = 1; e < OP::NS; ++e) mx = fmaxf(mx, s[e]);
-    mx *= c2;
-    // The sum's reference need not be the maximum, only near enough: 2^31 terms of up to
-    // 2^kSlack stay below the type's largest value, and nothing is rounded differently for it
-    if (__ballot(mx > m + kSlack)) {
-        const float mn = fmaxf(m, mx);
-        l *= __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
+        for (int rt = 0; rt < RT; ++rt) {
+            float p[OP::NS];
+#pragma unroll
+            for (int e = 0; e < OP::NS; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][e], c2, -m[rt]));
+            sum[rt] = 0.f;
+#pragma unroll
+            for (int e = 0; e < OP::NS; ++e) sum[rt] += p[e];
+            over |= !(sum[rt] <= kSlack);
+        }
+        return over;
+    };
+    if (__ballot(sums())) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float mx = s[rt][0];
+#pragma unroll
+            for (int e = 1; e < OP::NS; ++e) mx = fmaxf(mx, s[rt][e]);
+            const float mn = mx * c2 > m[rt] + kMost ? mx * c2 : m[rt];      // each row for itself
+            l[rt] *= __builtin_amdgcn_exp2f(m[rt] - mn);
+            m[rt] = mn;
+        }
+        sums();
     }
-    float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < OP::NS; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c2, -m));
-    l += sum;
+    for (int rt = 0; rt < RT; ++rt) l[rt] += sum[rt];
 }
 
 // block: (row tile, split, kv head), kv head fastest.  A split's key range is p.chunk
@@ -117,15 +135,15 @@ __global__ __launch_bounds__(256) void weigh_stats_kernel(const WeighParams p) {
     typename OP::K k[2];
     auto step = [&](const typename OP::K &kk, int t) {
         const int n = keys.count(t);
-        const bool nw = keys.is_new(t);
-        const int c0 = (int)keys.first(t);
+        float s[RT][OP::NS];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            float s[OP::NS];
-            OP::scores(kk, q[rt], s);
-            if (nw || n < OP::KEYS) mask<OP>(s, nw ? min(n - 1, tok[rt] - c0) : n - 1, g);
-            add_scores<OP>(s, c2, m[rt], l[rt]);
+        for (int rt = 0; rt < RT; ++rt) OP::scores(kk, q[rt], s[rt]);
+        if (keys.is_new(t) || n < OP::KEYS) {
+            const int c0 = (int)keys.first(t);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) mask<OP>(s[rt], keys.is_new(t) ? min(n - 1, tok[rt] - c0) : n - 1, g);
         }
+        add_scores<OP, RT>(s, c2, m, l);
     };
     int t = t0 + wave;
     if (t < t1) keys.load(k[0], t, keys.count(t), i, g);
@@ -163,7 +181,7 @@ __global__ __launch_bounds__(256) void weigh_stats_kernel(const WeighParams p) {
 // rows shared in LDS
 template <class OP, class RG, int RT>
 __global__ __launch_bounds__(256) void weigh_stats_rows_kernel(const WeighParams p) {
-    constexpr int SLOTS = 3;
+    constexpr int SLOTS = 6;      // of 8 KB at head_dim 128: one is read while the others are on their way
     __shared__ __attribute__((aligned(1024))) unsigned char lds[SLOTS * RG::HALF];
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -192,33 +210,33 @@ __global__ __launch_bounds__(256) void weigh_stats_rows_kernel(const WeighParams
     const float c2 = p.scale_log2;
     auto load = [&](int t, int slot) {
         const uint64_t first = (uint64_t)keys.first(t);
-        if (keys.is_new(t)) RG::load(keys.kn + first * keys.new_b, keys.new_b, keys.count(t), lds + slot * RG::HALF, wave, lane);
-        else RG::load(keys.kc + first * OP::ROWB, OP::ROWB, keys.count(t), lds + slot * RG::HALF, wave, lane);
+        if (keys.is_new(t)) RG::template load<false>(keys.kn + first * keys.new_b, keys.new_b, keys.count(t), lds + slot * RG::HALF, wave, lane);
+        else RG::template load<false>(keys.kc + first * OP::ROWB, OP::ROWB, keys.count(t), lds + slot * RG::HALF, wave, lane);
     };
-    if (t0 < t1) load(t0, 0);
-    if (t0 + 1 < t1) load(t0 + 1, 1);
+    for (int x = 0; x < SLOTS - 1 && t0 + x < t1; ++x) load(t0 + x, x);
+    wait_vmcnt<0>();      // the query rows too: loads that the compiler knows of would be waited for in the loop
     int slot = 0;
     for (int t = t0; t < t1; ++t) {
-        if (t + 1 < t1) wait_vmcnt<RG::LOADS>();
+        if (t + SLOTS - 2 < t1) wait_vmcnt<(SLOTS - 2) * RG::LOADS>();
         else wait_vmcnt<0>();
         barrier_lds();      // the stage has landed, the slot of the one before is free
-        if (t + 2 < t1) load(t + 2, slot == 0 ? 2 : slot - 1);
+        if (t + SLOTS - 1 < t1) load(t + SLOTS - 1, slot == 0 ? SLOTS - 1 : slot - 1);
         const unsigned char *st = lds + slot * RG::HALF;
-        const int n = keys.count(t);
-        const bool nw = keys.is_new(t);
-        const int c0 = (int)keys.first(t);
         typename OP::K k;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int ks = 0; ks < OP::NK; ++ks) k.f[h][ks] = RG::row_frag(st, ka, h, ks);
+        float s[RT][OP::NS];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            float s[OP::NS];
-            OP::scores(k, q[rt], s);
-            if (nw || n < OP::KEYS) mask<OP>(s, nw ? min(n - 1, tok[rt] - c0) : n - 1, g);
-            add_scores<OP>(s, c2, m[rt], l[rt]);
+        for (int rt = 0; rt < RT; ++rt) OP::scores(k, q[rt], s[rt]);
+        const int n = keys.count(t);
+        if (keys.is_new(t) || n < OP::KEYS) {
+            const int c0 = (int)keys.first(t);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) mask<OP>(s[rt], keys.is_new(t) ? min(n - 1, tok[rt] - c0) : n - 1, g);
         }
+        add_scores<OP, RT>(s, c2, m, l);
         slot = slot == SLOTS - 1 ? 0 : slot + 1;
     }
     // the four lanes of a row
@@ -233,36 +251,53 @@ __global__ __launch_bounds__(256) void weigh_stats_rows_kernel(const WeighParams
 
 constexpr int ROWS_AT_ONCE = 1024;      // normalizers held in LDS
 
-// norm[r] = M + log2(l) of rows r0 .. r0 + nr - 1 of a kv head, joined from its splits by
-// eight lanes a row: a weight is one 2^x.  Rounding that exponent is an error of the size
-// that the score has already.  Rows up to `padded` get weight 0.
-__device__ __forceinline__ void join_norms(const WeighParams &p, float *norm, int hd, int rows, int r0, int nr, int padded) {
+// M + log2(l) of a row, joined from its splits by eight lanes (lane j8 of them): a weight
+// is one 2^x.  Rounding that exponent is an error of the size that the score has already.
+__device__ __forceinline__ float join_norm(const float2 *src, int nsplit, int rows, int j8) {
     constexpr int AT_ONCE = 4;
-    for (int x = threadIdx.x; x < padded * 8; x += 256) {
-        const int r = x >> 3;
-        const float2 *src = p.ws + (int64_t)hd * p.nsplit * rows + r0 + min(r, nr - 1);
-        float M = -1e30f, sum = 0.f;
-        for (int s0 = x & 7; s0 < p.nsplit; s0 += 8 * AT_ONCE) {
-            float2 v[AT_ONCE];
+    float M = -1e30f, sum = 0.f;
+    for (int s0 = j8; s0 < nsplit; s0 += 8 * AT_ONCE) {
+        float2 v[AT_ONCE];
 #pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) {
-                v[u] = src[(int64_t)min(s0 + 8 * u, p.nsplit - 1) * rows];
-                if (s0 + 8 * u >= p.nsplit) v[u] = make_float2(-1e30f, 0.f);
-            }
-#pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) {
-                const float mn = fmaxf(M, v[u].x);
-                sum = sum * __builtin_amdgcn_exp2f(M - mn) + v[u].y * __builtin_amdgcn_exp2f(v[u].x - mn);
-                M = mn;
-            }
+        for (int u = 0; u < AT_ONCE; ++u) {
+            v[u] = src[(int64_t)min(s0 + 8 * u, nsplit - 1) * rows];
+            if (s0 + 8 * u >= nsplit) v[u] = make_float2(-1e30f, 0.f);
         }
 #pragma unroll
-        for (int d = 1; d < 8; d <<= 1) {
-            const float M2 = __shfl_xor(M, d), sum2 = __shfl_xor(sum, d), mn = fmaxf(M, M2);
-            sum = sum * __builtin_amdgcn_exp2f(M - mn) + sum2 * __builtin_amdgcn_exp2f(M2 - mn);
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const float mn = fmaxf(M, v[u].x);
+            sum = sum * __builtin_amdgcn_exp2f(M - mn) + v[u].y * __builtin_amdgcn_exp2f(v[u].x - mn);
             M = mn;
         }
-        if ((x & 7) == 0) norm[r] = r < nr ? M + __builtin_amdgcn_logf(sum) : INFINITY;
+    }
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) {
+        const float M2 = __shfl_xor(M, d), sum2 = __shfl_xor(sum, d), mn = fmaxf(M, M2);
+        sum = sum * __builtin_amdgcn_exp2f(M - mn) + sum2 * __builtin_amdgcn_exp2f(M2 - mn);
+        M = mn;
+    }
+    return M + __builtin_amdgcn_logf(sum);
+}
+
+// All rows' norms, for the second pass's workgroups to read instead of joining them each
+__global__ __launch_bounds__(256) void weigh_norm_kernel(const WeighParams p) {
+    const int64_t rows = (int64_t)p.S * p.group, x = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
+    const int64_t at = min(x, rows * p.n_kv_heads - 1), hd = at / rows, r = at - hd * rows;
+    const float nm = join_norm(p.ws + hd * p.nsplit * rows + r, p.nsplit, (int)rows, threadIdx.x & 7);
+    if ((threadIdx.x & 7) == 0 && x == at) p.norm[x] = nm;
+}
+
+// norm[r] of rows r0 .. r0 + nr - 1 of a kv head into LDS.  Rows up to `padded` get weight 0.
+__device__ __forceinline__ void take_norms(const WeighParams &p, float *norm, int hd, int rows, int r0, int nr, int padded) {
+    if (p.norm) {
+        for (int r = threadIdx.x; r < padded; r += 256)
+            norm[r] = r < nr ? p.norm[(int64_t)hd * rows + r0 + r] : INFINITY;
+        return;
+    }
+    for (int x = threadIdx.x; x < padded * 8; x += 256) {
+        const int r = x >> 3;
+        const float nm = join_norm(p.ws + (int64_t)hd * p.nsplit * rows + r0 + min(r, nr - 1), p.nsplit, rows, x & 7);
+        if ((x & 7) == 0) norm[r] = r < nr ? nm : INFINITY;
     }
 }
 
@@ -286,9 +321,9 @@ __device__ __forceinline__ void add_to_buffer(const WeighParams &p, const Keys<O
     }
 }
 
-// block: (group of WAVES x HELD stages, kv head), kv head fastest.  The query rows go
-// through LDS in stages of 32.
-template <class OP, class RG, int HELD>
+// block: (group of WAVES stages, kv head), kv head fastest.  The query rows go through LDS
+// in stages of 32.
+template <class OP, class RG>
 __global__ __launch_bounds__(256) void weigh_sum_rows_kernel(const WeighParams p) {
     constexpr int SLOTS = 3, ROWS = 32;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[SLOTS * RG::HALF];
@@ -299,18 +334,15 @@ __global__ __launch_bounds__(256) void weigh_sum_rows_kernel(const WeighParams p
     const int G = p.group, rows = p.S * G;
     const Keys<OP> keys(p, hd);
     const int n_all = keys.n_pre + (p.S + OP::KEYS - 1) / OP::KEYS;
-    const int t0 = ((int)(blockIdx.x / p.n_kv_heads) * WAVES + wave) * HELD;
+    const int t = (int)(blockIdx.x / p.n_kv_heads) * WAVES + wave;
     const float c2 = p.scale_log2;
     const uint32_t qa = RG::row_at(i, g);
     const uint64_t q0 = (uint64_t)(uintptr_t)p.q + (uint64_t)hd * G * OP::ROWB;
-    typename OP::K k[HELD];
-    float acc[HELD][OP::NS];
+    typename OP::K k;
+    float acc[1][OP::NS];
+    keys.load(k, t, t < n_all ? keys.count(t) : 0, i, g);
 #pragma unroll
-    for (int h = 0; h < HELD; ++h) {
-        keys.load(k[h], t0 + h, t0 + h < n_all ? keys.count(t0 + h) : 0, i, g);
-#pragma unroll
-        for (int e = 0; e < OP::NS; ++e) acc[h][e] = 0.f;
-    }
+    for (int e = 0; e < OP::NS; ++e) acc[0][e] = 0.f;
     // this wave's quarter of query rows r .. r + 31 (past the last: it again)
     auto load = [&](int r, int slot) {
 #pragma unroll
@@ -319,44 +351,48 @@ __global__ __launch_bounds__(256) void weigh_sum_rows_kernel(const WeighParams p
             const int row = at / OP::ROWB + lane / RG::CH;
             const int rr = min(r + row, rows - 1), tok = rr / G;
             const uint64_t src = q0 + ((uint64_t)tok * p.n_q_heads + (rr - tok * G)) * OP::ROWB +
-                                 16u * (uint32_t)((lane & (RG::CH - 1)) ^ RG::swz(row));
+                                 16u * (uint32_t)((lane & (RG::CH - 1)) ^ RG::template swz<false>(row));
             dma16((const void *)(uintptr_t)src, lds + slot * RG::HALF + at);
+        }
+    };
+    // 32 query rows from LDS against the wave's keys; NEW: these are new rows
+    auto stage = [&](auto is_new, const unsigned char *st, int r0, int rr) {
+        constexpr bool NEW = decltype(is_new)::value;
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            typename OP::Q q;
+#pragma unroll
+            for (int ks = 0; ks < OP::NK; ++ks) q.f[ks] = RG::row_frag(st, qa, part, ks);
+            const float nm = norm[rr + 16 * part + i];
+            float s[OP::NS];
+            OP::scores(k, q, s);
+            if constexpr (NEW) mask<OP>(s, (r0 + rr + 16 * part + i) / G - (int)keys.first(t), g);
+#pragma unroll
+            for (int e = 0; e < OP::NS; ++e) acc[0][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c2, -nm));
         }
     };
     for (int r0 = 0; r0 < rows; r0 += ROWS_AT_ONCE) {
         const int nr = min(rows - r0, ROWS_AT_ONCE), padded = (nr + ROWS - 1) / ROWS * ROWS;
         if (r0) barrier_lds();
-        join_norms(p, norm, hd, rows, r0, nr, padded);
         load(r0, 0);
         if (ROWS < padded) load(r0 + ROWS, 1);
-        int slot = 0;
-        for (int rr = 0; rr < padded; rr += ROWS) {
-            if (rr + ROWS < padded) wait_vmcnt<RG::LOADS>();
-            else wait_vmcnt<0>();
-            barrier_lds();
-            if (rr + 2 * ROWS < padded) load(r0 + rr + 2 * ROWS, slot == 0 ? 2 : slot - 1);
-            const unsigned char *st = lds + slot * RG::HALF;
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                typename OP::Q q;
-#pragma unroll
-                for (int ks = 0; ks < OP::NK; ++ks) q.f[ks] = RG::row_frag(st, qa, part, ks);
-                const float nm = norm[rr + 16 * part + i];
-                const int tok = keys.is_new(t0 + HELD - 1) ? (r0 + rr + 16 * part + i) / G : 0;
-#pragma unroll
-                for (int h = 0; h < HELD; ++h) {
-                    float s[OP::NS];
-                    OP::scores(k[h], q, s);
-                    const int t = t0 + h;
-                    if (keys.is_new(t)) mask<OP>(s, tok - (int)keys.first(t), g);
-#pragma unroll
-                    for (int e = 0; e < OP::NS; ++e) acc[h][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c2, -nm));
-                }
+        take_norms(p, norm, hd, rows, r0, nr, padded);
+        wait_vmcnt<0>();      // the keys too: loads that the compiler knows of would be waited for in the loop
+        auto walk = [&](auto is_new) {
+            int slot = 0;
+            for (int rr = 0; rr < padded; rr += ROWS) {
+                if (rr + ROWS < padded) wait_vmcnt<RG::LOADS>();
+                else wait_vmcnt<0>();
+                barrier_lds();
+                if (rr + 2 * ROWS < padded) load(r0 + rr + 2 * ROWS, slot == 0 ? 2 : slot - 1);
+                stage(is_new, lds + slot * RG::HALF, r0, rr);
+                slot = slot == SLOTS - 1 ? 0 : slot + 1;
             }
-            slot = slot == SLOTS - 1 ? 0 : slot + 1;
-        }
+        };
+        if (keys.is_new(t)) walk(std::true_type{});
+        else walk(std::false_type{});
     }
-    add_to_buffer<OP, HELD>(p, keys, acc, hd, t0, n_all, i, g);
+    add_to_buffer<OP, 1>(p, keys, acc, hd, t, n_all, i, g);
 }
 
 // The same with the query rows straight from memory
@@ -384,7 +420,7 @@ __global__ __launch_bounds__(256) void weigh_sum_kernel(const WeighParams p) {
     for (int r0 = 0; r0 < rows; r0 += ROWS_AT_ONCE) {
         const int nr = min(rows - r0, ROWS_AT_ONCE), padded = (nr + 15) & ~15;
         if (r0) __syncthreads();
-        join_norms(p, norm, hd, rows, r0, nr, padded);
+        take_norms(p, norm, hd, rows, r0, nr, padded);
         int tok = (r0 + i) / G, rem = (r0 + i) - tok * G;
         typename OP::Q q, next;
         auto load = [&](typename OP::Q &to) {      // (rows past the last: any row)
@@ -420,7 +456,7 @@ __global__ __launch_bounds__(256) void weigh_sum_kernel(const WeighParams p) {
 
 template <class E, int D>
 struct Op : Op16<E, D> {
-    using Ring = Ring16<E, D>;
+    using Ring = Ring16<E, D, 32>;
 };
 
 template <class OP>
@@ -434,14 +470,16 @@ hipError_t launch_op(const WeighParams &p, int way, int held, hipStream_t s) {
         if (way == kByRows + 2) hipLaunchKernelGGL((weigh_stats_rows_kernel<OP, typename OP::Ring, 2>), grid, block, 0, s, p);
         else hipLaunchKernelGGL((weigh_stats_rows_kernel<OP, typename OP::Ring, 4>), grid, block, 0, s, p);
     }
-    const hipError_t e = hipGetLastError();
+    hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
+    if (p.norm) {
+        hipLaunchKernelGGL(weigh_norm_kernel, dim3((unsigned)(((int64_t)rows * p.n_kv_heads + 31) / 32)), block, 0, s, p);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
     const int64_t stages = (p.L + OP::KEYS - 1) / OP::KEYS + (p.S + OP::KEYS - 1) / OP::KEYS;
     const dim3 wgs((unsigned)((stages + WAVES * held - 1) / (WAVES * held) * p.n_kv_heads));
     if constexpr (OP::ELT == 2) {
-        using RG = typename OP::Ring;
-        if (held == 2) hipLaunchKernelGGL((weigh_sum_rows_kernel<OP, RG, 2>), wgs, block, 0, s, p);
-        else hipLaunchKernelGGL((weigh_sum_rows_kernel<OP, RG, 1>), wgs, block, 0, s, p);
+        hipLaunchKernelGGL((weigh_sum_rows_kernel<OP, typename OP::Ring>), wgs, block, 0, s, p);
     } else {
         if (held == 2) hipLaunchKernelGGL((weigh_sum_kernel<OP, 2>), wgs, block, 0, s, p);
         else hipLaunchKernelGGL((weigh_sum_kernel<OP, 1>), wgs, block, 0, s, p);

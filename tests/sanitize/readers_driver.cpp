@@ -42,31 +42,34 @@ hipError_t launch_shared(const SharedParams &p, int head_dim, int dtype, int pw,
     if (ow > pw || (f32 ? pw > 2 : pw == 2 || ow == 2 || pw > kByRows + 2 || ow > kByRows + 1)) BAD("ways %d %d", pw, ow);
     if (p.p_tiles != (rows_p + tp - 1) / tp || p.t_tiles != (rows_o + to - 1) / to) BAD("tiles");
     if (p.rows != (int64_t)p.n * p.S * p.n_q_heads || p.rows > 0x7fffffff) BAD("rows");
-    if (p.nrec != p.np + p.nt || p.nt < 1) BAD("records");
+    if (p.nrec != p.np + p.nt + 1 || p.nt < 0 || (p.tcap > 0 && p.nt < 1)) BAD("records");
     if ((p.L == 0) != (p.np == 0)) BAD("no split of a prefix");
     if (p.np && ((int64_t)p.np * p.chunk < p.L || (int64_t)(p.np - 1) * p.chunk >= p.L)) BAD("prefix splits");
     if ((size_t)p.nrec * p.rows * (head_dim + 2) * 4 > g_ws_given) BAD("workspace");
     const int64_t own = (int64_t)p.n * p.t_tiles * p.n_kv_heads * p.nt;
     const int64_t pre = (int64_t)p.np * p.n_kv_heads * p.p_tiles;
+    const int64_t fresh = (int64_t)p.n * p.n_kv_heads * ((rows_o + 15) / 16);
     if (p.oct_all * (int64_t)8 > 0x7fffffff) BAD("grid");
     if (p.oct_all < 100000) {
-        std::vector<uint8_t> seen_o((size_t)own), seen_p((size_t)pre);
-        for (uint32_t oct = 0; oct < p.oct_all; ++oct) {
-            const uint32_t before = (uint32_t)(oct * p.own_share >> 32), upto = (uint32_t)((oct + 1) * p.own_share >> 32);
-            if (upto - before > 1) BAD("a group of blocks lost");
-            for (uint32_t in8 = 0; in8 < 8; ++in8) {
-                if (upto > before) {
-                    const int64_t b = (int64_t)before * 8 + in8;
-                    if (b < own) ++seen_o[(size_t)b];      // past the last: split >= nt
-                } else {
-                    const uint32_t o = oct - upto, pair = o / p.p_tiles * 8 + in8;
-                    const int64_t split = pair / p.n_kv_heads;
-                    if (split < p.np) ++seen_p[(size_t)pair * p.p_tiles + o % p.p_tiles];
+        std::vector<uint8_t> seen_o((size_t)own), seen_p((size_t)pre), seen_n((size_t)fresh);
+        for (uint32_t oct = 0; oct < p.oct_all; ++oct)
+            for (uint32_t in8 = 0; in8 < 8; ++in8)
+                for (uint32_t wave = 0; wave < 4; ++wave) {
+                    if (oct < p.oct_own) {
+                        const uint32_t pair = oct / p.p_tiles * 8 + in8;
+                        const int64_t split = pair / p.n_kv_heads;
+                        if (wave == 0 && split < p.np) ++seen_p[(size_t)pair * p.p_tiles + oct % p.p_tiles];
+                    } else if (oct < p.oct_new) {
+                        const int64_t b = (int64_t)(oct - p.oct_own) * 8 + in8;
+                        if (wave == 0 && b < own) ++seen_o[(size_t)b];            // past the last: split >= nt
+                    } else {
+                        const int64_t b = (int64_t)((oct - p.oct_new) * 8 + in8) * 4 + wave;
+                        if (b < fresh) ++seen_n[(size_t)b];                       // past the last: reader >= n
+                    }
                 }
-            }
-        }
         for (uint8_t x : seen_o) if (x != 1) { BAD("own item seen %d times", x); break; }
         for (uint8_t x : seen_p) if (x != 1) { BAD("prefix item seen %d times", x); break; }
+        for (uint8_t x : seen_n) if (x != 1) { BAD("new item seen %d times", x); break; }
     }
     return hipErrorUnknown;
 }
