@@ -39,7 +39,8 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 }
 constexpr uint32_t kNan = 0xfffffffeu, kStays = 0xffffffffu, kNoRow = 0u;
 
-// Sum of x over the threads before this one, and of all threads
+// Sum of x over the threads before this one, and of all threads.  Callers have a barrier
+// between the last use of tmp and this one.
 __device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t *tmp, uint32_t &total) {
     const int wave = threadIdx.x >> 6;
     // inclusive over the wave's lanes by data-parallel moves: within rows of 16 lanes,
@@ -51,14 +52,14 @@ __device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t *tmp, uint32_t &to
     v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
     v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast 15, 31
     v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
-    __syncthreads();      // tmp of the scan before is read
     if ((threadIdx.x & 63) == 63) tmp[wave] = v;
     __syncthreads();
     uint32_t base = 0, all = 0;
 #pragma unroll
     for (int w = 0; w < NWAVES; ++w) {
-        if (w < wave) base += tmp[w];
-        all += tmp[w];
+        const uint32_t t = tmp[w];
+        base += w < wave ? t : 0u;
+        all += t;
     }
     total = all;
     return base + v - x;
@@ -66,47 +67,74 @@ __device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t *tmp, uint32_t &to
 
 template <int BITS>
 struct Search {
-    uint32_t hist[1 << BITS];
-    uint32_t few[kFew];
+    __attribute__((aligned(16))) uint32_t hist[1 << BITS];
+    __attribute__((aligned(16))) uint32_t few[kFew];
+    uint32_t rank[kFew];
     uint32_t tmp[NWAVES];
-    uint32_t found[3], n_few;
+    uint32_t found[3], n_few, zeros;
 };
 
-// Histogram of the keys' bits `shift` .. `shift` + BITS - 1, of those that agree with T above
-// them; then the bin where the count from the top reaches `need`: its bits into T, what
-// is left to take of its keys into `need`, and how many they are.
-template <int BITS, int SBITS, bool TOP, class EACH>
-__device__ __forceinline__ uint32_t narrow(Search<SBITS> &s, int shift, uint32_t &T, uint32_t &need, EACH each) {
+template <int BITS, int SBITS>
+__device__ __forceinline__ void clear(Search<SBITS> &s) {
+    constexpr int n = (1 << BITS) / 4;
+#pragma unroll
+    for (int b = threadIdx.x; b < n; b += THREADS) ((u32x4 *)s.hist)[b] = (u32x4){0, 0, 0, 0};
+}
+
+// Before find(), apart from it: the weights may be on their way meanwhile
+template <int BITS>
+__device__ __forceinline__ void prepare(Search<BITS> &s) {
+    clear<BITS>(s);
+    if (threadIdx.x < kFew) {
+        s.few[threadIdx.x] = kNoRow;
+        s.rank[threadIdx.x] = 0;
+    }
+    if (threadIdx.x == 0) s.n_few = s.zeros = 0;
+    __syncthreads();
+}
+
+// Histogram (cleared) of bits `shift` .. `shift` + BITS - 1 of the keys with among(key); then
+// the bin where the count from the top reaches `need`: its bits into T, what is left to
+// take of its keys into `need`, and how many they are.  If all of them are fewer than
+// `need`, that many, and `need` and T as they were.
+template <int BITS, int SBITS, class AMONG, class EACH>
+__device__ __forceinline__ uint32_t narrow(Search<SBITS> &s, int shift, uint32_t &T, uint32_t &need, AMONG among, EACH each) {
     constexpr uint32_t bins = 1u << BITS;
     constexpr int PER = bins > THREADS ? bins / THREADS : 1;
-    for (uint32_t b = threadIdx.x; b < bins; b += THREADS) s.hist[b] = 0;
-    __syncthreads();
-    // zeros are the one weight that many rows share: counted by wave, not one by one
-    uint32_t zeros = 0;
     each([&](uint32_t k) {
-        const bool mine = TOP ? k != kNoRow : k != kNoRow && k >> (shift + BITS) == T >> (shift + BITS);
-        zeros += __popcll(__ballot(mine && k == kZero));
-        if (mine && k != kZero) atomicAdd(&s.hist[(k >> shift) & (bins - 1)], 1u);
+        if (among(k)) atomicAdd(&s.hist[(k >> shift) & (bins - 1)], 1u);
     });
-    if ((threadIdx.x & 63) == 0 && zeros) atomicAdd(&s.hist[(kZero >> shift) & (bins - 1)], zeros);
     __syncthreads();
     uint32_t h[PER], sum = 0;
+    if constexpr (PER >= 4) {
+        const u32x4 *at = (const u32x4 *)(s.hist + bins - PER * (threadIdx.x + 1));
 #pragma unroll
-    for (int c = 0; c < PER; ++c) {
-        const uint32_t b = threadIdx.x * PER + c;
-        h[c] = b < bins ? s.hist[bins - 1 - b] : 0u;
-        sum += h[c];
+        for (int c = 0; c < PER; c += 4) {
+            const u32x4 x = at[c / 4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[PER - 1 - c - e] = x[e];
+        }
+    } else {
+        h[0] = threadIdx.x < bins ? s.hist[bins - 1 - threadIdx.x] : 0u;
     }
+#pragma unroll
+    for (int c = 0; c < PER; ++c) sum += h[c];
     uint32_t all;
     uint32_t before = scan(sum, s.tmp, all);
+    if (all < need) {
+        __syncthreads();      // the histogram is read
+        return all;
+    }
+    if (before < need && before + sum >= need) {      // one thread
 #pragma unroll
-    for (int c = 0; c < PER; ++c) {
-        if (before < need && before + h[c] >= need) {
-            s.found[0] = bins - 1 - (threadIdx.x * PER + c);
-            s.found[1] = need - before;
-            s.found[2] = h[c];
+        for (int c = 0; c < PER; ++c) {
+            if (before < need && before + h[c] >= need) {
+                s.found[0] = bins - 1 - (threadIdx.x * PER + c);
+                s.found[1] = need - before;
+                s.found[2] = h[c];
+            }
+            before += h[c];
         }
-        before += h[c];
     }
     __syncthreads();
     T |= s.found[0] << shift;
@@ -114,38 +142,75 @@ __device__ __forceinline__ uint32_t narrow(Search<SBITS> &s, int shift, uint32_t
     return s.found[2];
 }
 
-// The pick-th largest key T (pick > 0), and how many of the keys equal to it are taken.
-// each(f) calls f(key) for the thread's keys, all lanes of a wave together.
+// The pick-th largest key T (pick > 0; keys of no row apart), how many of the keys equal to
+// it are taken, and whether these are all.  each(f) calls f(key) for the thread's keys,
+// all lanes of a wave together.  Zeros, the one weight that many rows share, would all add
+// to one bin: the weights above them are counted first, zeros and those below only if
+// that is not enough.
 template <int BITS, class EACH>
-__device__ __forceinline__ uint32_t find(Search<BITS> &s, uint32_t pick, uint32_t &need, EACH each) {
+__device__ __forceinline__ uint32_t find(Search<BITS> &s, uint32_t pick, uint32_t &need, bool &all, EACH each) {
+    constexpr int TOP = 32 - BITS, HALF = TOP / 2;
     uint32_t T = 0;
     need = pick;
-    if (threadIdx.x == 0) s.n_few = 0;
-    const uint32_t n = narrow<BITS, BITS, true>(s, 32 - BITS, T, need, each);
+    uint32_t n = narrow<BITS>(s, TOP, T, need, [](uint32_t k) { return k > kZero; }, each);
+    if (n < need) {
+        need -= n;
+        uint32_t zeros = 0;
+        each([&](uint32_t k) { zeros += __popcll(__ballot(k == kZero)); });
+        if ((threadIdx.x & 63) == 0) atomicAdd(&s.zeros, zeros);
+        clear<BITS>(s);
+        __syncthreads();
+        if (s.zeros >= need) {
+            all = s.zeros == need;
+            return kZero;
+        }
+        need -= s.zeros;
+        n = narrow<BITS>(s, TOP, T, need, [](uint32_t k) { return k < kZero && k != kNoRow; }, each);
+    }
     if (n > kFew) {
-        constexpr int HALF = (32 - BITS) / 2;
-        narrow<HALF, BITS, false>(s, HALF, T, need, each);
-        narrow<HALF, BITS, false>(s, 0, T, need, each);
+        clear<HALF>(s);
+        __syncthreads();
+        narrow<HALF>(s, HALF, T, need, [=](uint32_t k) { return k >> TOP == T >> TOP; }, each);
+        clear<HALF>(s);
+        __syncthreads();
+        n = narrow<HALF>(s, 0, T, need, [=](uint32_t k) { return k >> HALF == T >> HALF; }, each);
+        all = n == need;
         return T;
     }
     each([&](uint32_t k) {
-        if (k != kNoRow && k >> (32 - BITS) == T >> (32 - BITS)) s.few[atomicAdd(&s.n_few, 1u)] = k;
+        if (k >> TOP == T >> TOP && k != kZero) s.few[atomicAdd(&s.n_few, 1u)] = k;      // (the least weights share zero's bin)
     });
     __syncthreads();
-    if (threadIdx.x < n) {
-        const uint32_t k = s.few[threadIdx.x];
+    // the keys above a key (low half) and equal to it (high half), by four threads
+    const uint32_t c = threadIdx.x % kFew;
+    const uint32_t k = s.few[c];
+    if (c < n) {
         uint32_t above = 0, equal = 0;
-        for (uint32_t x = 0; x < n; ++x) {
-            above += s.few[x] > k;
-            equal += s.few[x] == k;
+        for (uint32_t x = threadIdx.x / kFew * 16; x < n; x += THREADS / kFew * 16) {      // (behind the last: no row's key)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const u32x4 f = ((const u32x4 *)s.few)[x / 4 + y];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    above += f[e] > k;
+                    equal += f[e] == k;
+                }
+            }
         }
+        atomicAdd(&s.rank[c], above | equal << 16);
+    }
+    __syncthreads();
+    if (threadIdx.x < n) {
+        const uint32_t above = s.rank[c] & 0xffff, equal = s.rank[c] >> 16;
         if (above < need && above + equal >= need) {      // the same from every thread with this key
             s.found[0] = k;
             s.found[1] = need - above;
+            s.found[2] = equal;
         }
     }
     __syncthreads();
     need = s.found[1];
+    all = s.found[2] == need;
     return s.found[0];
 }
 
@@ -153,91 +218,135 @@ __device__ __forceinline__ uint32_t lanes_before(uint64_t mask) {
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
 }
 
+// Whether this is lane i, without a comparison
+__device__ __forceinline__ bool lane_is(int i) { return __builtin_amdgcn_inverse_ballot_w64(1ull << i); }
+
+// A thread's keys: those of rows j0 + threadIdx.x + THREADS i, so that blocks of 64 rows,
+// in order, are those of wave 0, wave 1, ... for i = 0, then for i = 1, ...
+template <int PER>
+struct Keys {
+    uint32_t k[PER];
+    __device__ __forceinline__ void load(const EvictParams &p, const float *w, uint32_t j0) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            k[i] = __float_as_uint(w[min(j0 + THREADS * i + threadIdx.x, (uint32_t)p.L - 1)]);
+    }
+    __device__ __forceinline__ void make(const EvictParams &p, uint32_t j0) {
+        const uint32_t lane = threadIdx.x & 63, b0 = j0 + 64 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) most = max(most, k[i]);
+        if (__ballot(most > 0x7f800000u)) {      // a sign or no number
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const float x = __uint_as_float(k[i]);
+                k[i] = x != x ? kNan : key_of(x + 0.f);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) k[i] |= 0x80000000u;
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint32_t b = b0 + THREADS * i, first = p.n_first, last = p.L - p.n_last;
+            if (b < first || b + 64 > last) {      // one of the block may be no candidate
+                const uint32_t j = b + lane;
+                if (j < first || j >= last) k[i] = j < (uint32_t)p.L ? kStays : kNoRow;
+            }
+        }
+    }
+};
+
+// Keys above T (low half) and equal to it (high half), up to 2^15 each: lane i gets the
+// counts of the wave's block i, and of all blocks before it.  all: nothing equal is to be
+// told apart, T is the largest key that goes.
+template <int PER>
+__device__ __forceinline__ void count(Keys<PER> &keys, uint32_t T, bool all, uint32_t *counts, uint32_t *tmp, uint32_t &mine,
+                                      uint32_t &before, uint32_t &total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    mine = 0;
+    if (all) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint32_t a = __popcll(__ballot(keys.k[i] > T));
+            mine = lane_is(i) ? a : mine;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint32_t a = __popcll(__ballot(keys.k[i] > T)), e = __popcll(__ballot(keys.k[i] == T)), ae = a | e << 16;
+            mine = lane_is(i) ? ae : mine;
+        }
+    }
+    if (lane < PER) counts[lane * NWAVES + wave] = mine;
+    __syncthreads();
+    const bool one = threadIdx.x < PER * NWAVES;
+    const uint32_t b = scan(one ? counts[threadIdx.x] : 0u, tmp, total);
+    if (one) counts[threadIdx.x] = b;
+    __syncthreads();
+    before = lane < PER ? counts[lane * NWAVES + wave] : 0u;
+}
+
+// put(place, row) for the kept rows with places r0 .. r0 + n - 1.  above, equal: keys before
+// those that count() saw
+template <int PER, class PUT>
+__device__ __forceinline__ void place(Keys<PER> &keys, uint32_t T, uint32_t need, uint32_t j0, uint32_t mine, uint32_t before,
+                                      uint32_t above, uint32_t equal, int r0, int n, PUT put) {
+    const int lane = threadIdx.x & 63;
+    const uint32_t a0 = above + (before & 0xffff), e0 = equal + (before >> 16);
+    const int first = (int)(a0 + min(e0, need)), last = (int)(a0 + (mine & 0xffff) + min(e0 + (mine >> 16), need));
+    const uint64_t blocks = __ballot(lane < PER && last > r0 && first < r0 + n && last > first);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (!(blocks >> i & 1)) continue;
+        asm volatile("" : "+v"(keys.k[i]));      // compared anew: 4 PER registers of masks are more than there are
+        const uint64_t ma = __ballot(keys.k[i] > T), me = __ballot(keys.k[i] == T);
+        const uint32_t eq = __builtin_amdgcn_readlane(e0, i) + lanes_before(me);
+        const int at = (int)(__builtin_amdgcn_readlane(a0, i) + lanes_before(ma) + min(eq, need)) - r0;
+        if ((keys.k[i] > T || (keys.k[i] == T && eq < need)) && at >= 0 && at < n) put(at, (int)(j0 + THREADS * i + threadIdx.x));
+    }
+}
+
 constexpr int LIST = 2048;      // kept rows that a workgroup copies at a time
 
-// PER: keys per thread.  Wave w holds rows 64 PER w .. 64 PER (w + 1) - 1, its lanes
-// side by side: a wave counts its kept rows with ballots, and only the waves that hold
-// rows of the workgroup's share place them.
+// PER: keys per thread
 template <int PER, int BITS>
 __global__ __launch_bounds__(THREADS) void evict_kernel(const EvictParams p) {
     __shared__ Search<BITS> s;
-    __shared__ uint32_t count[NWAVES][2];
+    __shared__ uint32_t counts[PER * NWAVES];
     __shared__ int32_t list[LIST];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int hd = blockIdx.x % p.n_kv_heads, part = blockIdx.x / p.n_kv_heads;
     const float *w = p.weight + (int64_t)hd * p.cap;
-    const int w0 = __builtin_amdgcn_readfirstlane(wave) * 64 * PER, j0 = w0 + lane;
-    float x[PER];
+    Keys<PER> keys;
+    keys.load(p, w, 0);
+    prepare(s);
+    keys.make(p, 0);
+    uint32_t need, mine, before, total;
+    bool all;
+    uint32_t T = find<BITS>(s, (uint32_t)p.n_keep, need, all, [&](auto f) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) x[i] = w[min(j0 + 64 * i, p.L - 1)];
-    uint32_t key[PER];
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        odd |= x[i] != x[i];
-        key[i] = key_of(x[i] + 0.f);
-    }
-    if (__ballot(odd)) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) key[i] = x[i] != x[i] ? kNan : key[i];
-    }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int b = w0 + 64 * i, j = b + lane;
-        if (b < p.n_first || b + 64 > p.L - p.n_last) {      // one of the wave's 64 may be no candidate
-            if (j < p.n_first || j >= p.L - p.n_last) key[i] = kStays;
-            if (j >= p.L) key[i] = kNoRow;
-        }
-    }
-    uint32_t need;
-    const uint32_t T = find<BITS>(s, (uint32_t)p.n_keep, need, [&](auto f) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) f(key[i]);
+        for (int i = 0; i < PER; ++i) f(keys.k[i]);
     });
-    // keys above T, and equal to it, of each wave
-    uint32_t a = 0, e = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        a += __popcll(__ballot(key[i] > T));
-        e += __popcll(__ballot(key[i] == T));
-    }
-    if (lane == 0) {
-        count[wave][0] = a;
-        count[wave][1] = e;
-    }
-    __syncthreads();
-    uint32_t a0 = 0, e0 = 0;      // of the waves before
-    for (int x = 0; x < wave; ++x) {
-        a0 += count[x][0];
-        e0 += count[x][1];
-    }
-    const uint32_t first = a0 + min(e0, need), last = a0 + a + min(e0 + e, need);      // places of this wave's rows
+    if (all) --T, need = 0;
+    count(keys, T, all, counts, s.tmp, mine, before, total);
     const int share = (p.n_keep + p.parts - 1) / p.parts;
     const int r_end = min(p.n_keep, (part + 1) * share);
     for (int r0 = part * share; r0 < r_end; r0 += LIST) {
         const int n = min(LIST, r_end - r0);
-        if ((int)last > r0 && (int)first < r0 + n) {
-            uint32_t ca = a0, ce = e0;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                asm volatile("" : "+v"(key[i]));      // compared anew: 4 PER registers of masks are more than there are
-                const uint64_t ma = __ballot(key[i] > T), me = __ballot(key[i] == T);
-                const uint32_t eq = ce + lanes_before(me);
-                const int at = (int)(ca + lanes_before(ma) + min(eq, need)) - r0;
-                if ((key[i] > T || (key[i] == T && eq < need)) && at >= 0 && at < n) list[at] = j0 + 64 * i;
-                ca += __popcll(ma);
-                ce += __popcll(me);
-            }
-        }
+        place(keys, T, need, 0, mine, before, 0, 0, r0, n, [&](int at, int j) { list[at] = j; });
         __syncthreads();
+        for (int r = threadIdx.x; r < n; r += THREADS) {
+            if (p.index) p.index[(int64_t)hd * p.n_keep + r0 + r] = list[r];
+            if (p.weight_out) p.weight_out[(int64_t)hd * p.cap_out + r0 + r] = w[list[r]];
+        }
         // the rows, 16 bytes a thread, several in flight
         constexpr int BATCH = 4;
-        const int total = n * p.row_chunks;
-        for (int x0 = threadIdx.x; x0 < total; x0 += BATCH * THREADS) {
+        const int chunks = n * p.row_chunks;
+        for (int x0 = threadIdx.x; x0 < chunks; x0 += BATCH * THREADS) {
             u32x4 k[BATCH], v[BATCH];
 #pragma unroll
             for (int b = 0; b < BATCH; ++b) {
-                const int x = min(x0 + b * THREADS, total - 1);
+                const int x = min(x0 + b * THREADS, chunks - 1);
                 const int r = x >> p.chunk_bits;
                 const int64_t src = (((int64_t)hd * p.cap + list[r]) << p.chunk_bits) + (x & (p.row_chunks - 1));
                 k[b] = ((const u32x4 *)p.kc)[src];
@@ -246,45 +355,45 @@ __global__ __launch_bounds__(THREADS) void evict_kernel(const EvictParams p) {
 #pragma unroll
             for (int b = 0; b < BATCH; ++b) {
                 const int x = x0 + b * THREADS;
-                if (x >= total) break;
+                if (x >= chunks) break;
                 const int64_t dst = (((int64_t)hd * p.cap_out + r0) << p.chunk_bits) + x;
                 ((u32x4 *)p.ko)[dst] = k[b];
                 ((u32x4 *)p.vo)[dst] = v[b];
             }
-        }
-        for (int r = threadIdx.x; r < n; r += THREADS) {
-            if (p.index) p.index[(int64_t)hd * p.n_keep + r0 + r] = list[r];
-            if (p.weight_out) p.weight_out[(int64_t)hd * p.cap_out + r0 + r] = w[list[r]];
         }
         __syncthreads();      // the list is read
     }
 }
 
 __global__ __launch_bounds__(THREADS) void evict_select_kernel(const EvictParams p) {
+    constexpr int PER = 8;
     __shared__ Search<14> s;
+    __shared__ uint32_t counts[PER * NWAVES];
     const int hd = blockIdx.x;
     const float *w = p.weight + (int64_t)hd * p.cap;
     int32_t *out = p.list + (int64_t)hd * p.n_keep;
-    const int64_t L = p.L;
-    auto key = [&](int64_t j) {
-        const float x = w[min(j, L - 1)];
-        if (j >= L) return kNoRow;
-        if (j < p.n_first || j >= L - p.n_last) return kStays;
-        return x != x ? kNan : key_of(x + 0.f);
-    };
+    prepare(s);
+    Keys<PER> keys;
     uint32_t need;
-    const uint32_t T = find<14>(s, (uint32_t)p.n_keep, need, [&](auto f) {
-        for (int64_t j0 = 0; j0 < L; j0 += THREADS) f(key(j0 + threadIdx.x));
+    bool all;
+    uint32_t T = find<14>(s, (uint32_t)p.n_keep, need, all, [&](auto f) {
+        for (uint32_t j0 = 0; j0 < (uint32_t)p.L; j0 += PER * THREADS) {
+            keys.load(p, w, j0);
+            keys.make(p, j0);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) f(keys.k[i]);
+        }
     });
+    if (all) --T, need = 0;
     uint32_t above = 0, equal = 0;
-    for (int64_t j0 = 0; j0 < L; j0 += THREADS) {
-        const int64_t j = j0 + threadIdx.x;
-        const uint32_t k = key(j), a = k > T, e = k == T;
-        uint32_t ta, te;
-        const uint32_t ca = above + scan(a, s.tmp, ta), ce = equal + scan(e, s.tmp, te);
-        if (a || (e && ce < need)) out[ca + min(ce, need)] = (int)j;
-        above += ta;
-        equal += te;
+    for (uint32_t j0 = 0; j0 < (uint32_t)p.L; j0 += PER * THREADS) {
+        uint32_t mine, before, total;
+        keys.load(p, w, j0);
+        keys.make(p, j0);
+        count(keys, T, all, counts, s.tmp, mine, before, total);
+        place(keys, T, need, j0, mine, before, above, equal, 0, p.n_keep, [&](int at, int j) { out[at] = j; });
+        above += total & 0xffff;
+        equal += total >> 16;
     }
 }
 

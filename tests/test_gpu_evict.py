@@ -109,6 +109,7 @@ EVICT = [
     (100, 99, 4, 3, "normal"), (1000, 1, 0, 0, "normal"), (1000, 7, 4, 3, "normal"), (1000, 333, 4, 32, "ties"),
     (1023, 500, 0, 0, "equal"), (1025, 500, 1, 0, "zeros"), (5000, 1250, 4, 24, "normal"), (4096, 4000, 0, 1, "ties"),
     (3333, 1000, 2, 2, "odd"), (20000, 5000, 4, 128, "normal"), (70001, 30000, 0, 0, "normal"),
+    (500, 100, 0, 0, "tiny"), (1000, 200, 4, 3, "tiny"), (1000, 900, 4, 3, "tiny"), (40000, 100, 0, 5, "tiny"),
 ]
 
 
@@ -120,6 +121,9 @@ def evict_weights(kind, Hkv, cap, g):
         w = torch.full((Hkv, cap), 0.25)
     elif kind == "zeros":
         w[torch.rand((Hkv, cap), generator=g) < 0.8] = 0.0
+    elif kind == "tiny":       # the type's least weights among zeros
+        w = torch.randint(1, 60, (Hkv, cap), generator=g) * 2.0 ** -149
+        w[torch.rand((Hkv, cap), generator=g) < 0.7] = 0.0
     elif kind == "odd":        # signs, infinities, both zeros, no numbers, the type's extremes
         v = torch.tensor([0.0, -0.0, -1.0, 2.0, float("inf"), -float("inf"), float("nan"), 1e-45, -1e-45,
                           torch.finfo(F32).max, torch.finfo(F32).min])
