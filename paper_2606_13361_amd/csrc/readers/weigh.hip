@@ -343,16 +343,29 @@ __global__ __launch_bounds__(256) void weigh_sum_rows_kernel(const WeighParams p
     keys.load(k, t, t < n_all ? keys.count(t) : 0, i, g);
 #pragma unroll
     for (int e = 0; e < OP::NS; ++e) acc[0][e] = 0.f;
-    // this wave's quarter of query rows r .. r + 31 (past the last: it again)
-    auto load = [&](int r, int slot) {
+    // This wave's quarter of each stage, rows of the kv head one after the other (past the
+    // last: it again): from one stage to the next a row's head goes on by 32 mod G, its
+    // token by 32 / G, and one more where the head passes the group's last.
+    uint64_t src[RG::LOADS], last[RG::LOADS];
+    int head[RG::LOADS];
+    const int more = ROWS % G;
+    const uint64_t step = ((uint64_t)(ROWS / G) * p.n_q_heads + more) * OP::ROWB;
+    const uint64_t wrap = (uint64_t)(p.n_q_heads - G) * OP::ROWB;
+#pragma unroll
+    for (int x = 0; x < RG::LOADS; ++x) {
+        const int row = (wave * RG::LOADS + x) * 1024 / OP::ROWB + lane / RG::CH;
+        const uint64_t chunk = q0 + 16u * (uint32_t)((lane & (RG::CH - 1)) ^ RG::template swz<false>(row));
+        head[x] = row % G;
+        src[x] = chunk + ((uint64_t)(row / G) * p.n_q_heads + head[x]) * OP::ROWB;
+        last[x] = chunk + ((uint64_t)(p.S - 1) * p.n_q_heads + G - 1) * OP::ROWB;
+    }
+    auto load = [&](int slot) {
 #pragma unroll
         for (int x = 0; x < RG::LOADS; ++x) {
-            const int at = (wave * RG::LOADS + x) * 1024;
-            const int row = at / OP::ROWB + lane / RG::CH;
-            const int rr = min(r + row, rows - 1), tok = rr / G;
-            const uint64_t src = q0 + ((uint64_t)tok * p.n_q_heads + (rr - tok * G)) * OP::ROWB +
-                                 16u * (uint32_t)((lane & (RG::CH - 1)) ^ RG::template swz<false>(row));
-            dma16((const void *)(uintptr_t)src, lds + slot * RG::HALF + at);
+            dma16((const void *)(uintptr_t)min(src[x], last[x]), lds + slot * RG::HALF + (wave * RG::LOADS + x) * 1024);
+            head[x] += more;
+            src[x] += step + (head[x] >= G ? wrap : 0);
+            head[x] -= head[x] >= G ? G : 0;
         }
     };
     // 32 query rows from LDS against the wave's keys; NEW: these are new rows
@@ -374,8 +387,8 @@ __global__ __launch_bounds__(256) void weigh_sum_rows_kernel(const WeighParams p
     for (int r0 = 0; r0 < rows; r0 += ROWS_AT_ONCE) {
         const int nr = min(rows - r0, ROWS_AT_ONCE), padded = (nr + ROWS - 1) / ROWS * ROWS;
         if (r0) barrier_lds();
-        load(r0, 0);
-        if (ROWS < padded) load(r0 + ROWS, 1);
+        load(0);
+        if (ROWS < padded) load(1);
         take_norms(p, norm, hd, rows, r0, nr, padded);
         wait_vmcnt<0>();      // the keys too: loads that the compiler knows of would be waited for in the loop
         auto walk = [&](auto is_new) {
@@ -384,7 +397,7 @@ __global__ __launch_bounds__(256) void weigh_sum_rows_kernel(const WeighParams p
                 if (rr + ROWS < padded) wait_vmcnt<RG::LOADS>();
                 else wait_vmcnt<0>();
                 barrier_lds();
-                if (rr + 2 * ROWS < padded) load(r0 + rr + 2 * ROWS, slot == 0 ? 2 : slot - 1);
+                if (rr + 2 * ROWS < padded) load(slot == 0 ? 2 : slot - 1);
                 stage(is_new, lds + slot * RG::HALF, r0, rr);
                 slot = slot == SLOTS - 1 ? 0 : slot + 1;
             }
