@@ -181,7 +181,7 @@ __global__ __launch_bounds__(256) void weigh_stats_kernel(const WeighParams p) {
 // rows shared in LDS
 template <class OP, class RG, int RT>
 __global__ __launch_bounds__(256) void weigh_stats_rows_kernel(const WeighParams p) {
-    constexpr int SLOTS = 6;      // of 8 KB at head_dim 128: one is read while the others are on their way
+    constexpr int SLOTS = 3;      // one is read while the others are on their way
     __shared__ __attribute__((aligned(1024))) unsigned char lds[SLOTS * RG::HALF];
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
