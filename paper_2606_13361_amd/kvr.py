@@ -469,24 +469,43 @@ def kvr_continue_batched_rope(desc, rope, Qs, Ks, Vs, cu_seqlens, kcache, vcache
 
 
 # ---------------------------------------------------------------- many readers, later turns
-def _check_typed(t, name, dtype, shape):
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s GPU tensor" % (name, dtype))
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
-    return t.data_ptr()
+def _device(t, name):
+    """The GPU of a call's first tensor; the others have to be there (_at)."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError("%s must be a torch tensor" % name)
+    if not t.is_cuda:
+        raise ValueError("%s must be on the GPU" % name)
+    return t.get_device()
 
 
-def _launch(call, where, stream, first, *others):
-    """call(stream handle) with the tensors' device current; they all have to be on one."""
-    dev = first.device
-    for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError("%s: tensors on %s and %s" % (where, dev, t.device))
-    if isinstance(stream, torch.cuda.Stream) and stream.device != dev:
-        raise ValueError("%s: tensors on %s, the stream is of %s" % (where, dev, stream.device))
-    if dev.index == torch.cuda.current_device():
-        _raise(call(_stream(stream)), where)
+def _at(t, name, dtype, shape, dev):
+    """Address of a contiguous tensor of this type and shape (a tuple) on GPU dev.  One
+    expression where all is well: a small call is bound by its checks on the host."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == dev and t.is_contiguous()
+            and t.shape == shape):
+        return t.data_ptr()
+    _device(t, name)
+    if t.dtype != dtype or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor, not %s" % (name, dtype, t.dtype))
+    if t.get_device() != dev:
+        raise ValueError("%s is on GPU %d, other tensors of the call on GPU %d" % (name, t.get_device(), dev))
+    raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), shape))
+
+
+def _scratch(ws, dev):
+    if ws is None:
+        return None, 0
+    if isinstance(ws, torch.Tensor) and ws.is_cuda and ws.get_device() != dev:
+        raise ValueError("ws is on GPU %d, other tensors of the call on GPU %d" % (ws.get_device(), dev))
+    return _workspace(ws)
+
+
+def _launch(call, where, stream, dev):
+    """call(stream handle) with GPU dev current."""
+    if isinstance(stream, torch.cuda.Stream) and stream.device.index != dev:
+        raise ValueError("%s: tensors on GPU %d, the stream is of %s" % (where, dev, stream.device))
+    if dev == torch._C._cuda_getDevice():
+        _raise(call(torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)), where)
     else:
         with torch.cuda.device(dev):
             _raise(call(_stream(stream)), where)
@@ -516,30 +535,39 @@ def kvr_continue_shared(desc, Qs, Ks, Vs, kcache, vcache, L_prefix, ktail, vtail
     ktail, vtail [n, n_kv_heads, tail_capacity, head_dim] (None: the readers have no
     rows); tail_len: int32 GPU tensor [n].  rope: a RopeTable that rotates the rows
     at pos0 + tail_len[r] + i (pos0: L_prefix by default)."""
-    Hq, Hkv, d = desc.n_q_heads, desc.n_kv_heads, desc.head_dim
-    if not isinstance(Qs, torch.Tensor) or Qs.dim() != 4:
+    Hq, Hkv, d, dt = desc.n_q_heads, desc.n_kv_heads, desc.head_dim, _TORCH_DTYPE.get(desc.dtype)
+    dev = _device(Qs, "Qs")
+    if Qs.dim() != 4:
         raise ValueError("Qs must be a tensor [n, S, n_q_heads, head_dim]")
-    n, S = Qs.shape[0], Qs.shape[1]
-    q = _check(Qs, "Qs", desc, (n, S, Hq, d))
-    k = _check(Ks, "Ks", desc, (n, S, Hkv, d))
-    v = _check(Vs, "Vs", desc, (n, S, Hkv, d))
-    o = _check(out, "out", desc, (n, S, Hq, d))
-    kc, vc = _cache_ptrs(desc, kcache, vcache, L_prefix > 0)
-    cap, kt, vt = 0, None, None
+    n, S = Qs.shape[:2]
+    rows, new = (n, S, Hq, d), (n, S, Hkv, d)
+    q = _at(Qs, "Qs", dt, rows, dev)
+    k = _at(Ks, "Ks", dt, new, dev)
+    v = _at(Vs, "Vs", dt, new, dev)
+    o = _at(out, "out", dt, rows, dev)
+    kc = vc = kt = vt = rp = None
+    if L_prefix > 0 or kcache is not None or vcache is not None:
+        shape = (Hkv, desc.capacity, d)
+        kc = _at(kcache, "kcache", dt, shape, dev)
+        vc = _at(vcache, "vcache", dt, shape, dev)
+    cap = 0
     if ktail is not None or vtail is not None:
         if not isinstance(ktail, torch.Tensor) or ktail.dim() != 4:
             raise ValueError("ktail must be a tensor [n, n_kv_heads, tail_capacity, head_dim]")
         cap = ktail.shape[2]
-        kt = _check(ktail, "ktail", desc, (n, Hkv, cap, d))
-        vt = _check(vtail, "vtail", desc, (n, Hkv, cap, d))
-    ln = _check_typed(tail_len, "tail_len", torch.int32, (n,))
-    wp, wn = _workspace(ws)
-    rp = None if rope is None else _rope(rope, desc)
+        shape = (n, Hkv, cap, d)
+        kt = _at(ktail, "ktail", dt, shape, dev)
+        vt = _at(vtail, "vtail", dt, shape, dev)
+    ln = _at(tail_len, "tail_len", torch.int32, (n,), dev)
+    wp, wn = _scratch(ws, dev)
+    if rope is not None:
+        rp = _rope(rope, desc)
+        if rope.cos_sin.get_device() != dev:
+            raise ValueError("rope is on GPU %d, other tensors of the call on GPU %d" % (rope.cos_sin.get_device(), dev))
     at = int(L_prefix if pos0 is None else pos0)
     _launch(lambda s: load().kvr_continue_shared(ctypes.byref(desc), rp, q, k, v, n, S, kc, vc, int(L_prefix), at, kt,
                                                  vt, cap, ln, 1 if append else 0, o, wp, wn, s),
-            "kvr_continue_shared", stream, Qs, Ks, Vs, out, kcache, vcache, ktail, vtail, tail_len, ws,
-            None if rope is None else rope.cos_sin)
+            "kvr_continue_shared", stream, dev)
 
 
 def kvr_workspace_bytes_weigh(desc, L_prefix, S):
@@ -554,14 +582,15 @@ def workspace_for_weigh(desc, L_prefix, S, device="cuda"):
 def kvr_cache_weigh(desc, Qs, Ks, kcache, L_prefix, S, weight, ws, stream=None):
     """Add to weight [n_kv_heads, capacity] (float32) the attention weight that each row
     receives from the S tokens at positions L_prefix.. ."""
-    Hq, Hkv, d = desc.n_q_heads, desc.n_kv_heads, desc.head_dim
-    q = _check(Qs, "Qs", desc, (S, Hq, d))
-    k = _check(Ks, "Ks", desc, (S, Hkv, d))
-    kc = _check(kcache, "kcache", desc, (Hkv, desc.capacity, d)) if L_prefix > 0 or kcache is not None else None
-    w = _check_typed(weight, "weight", torch.float32, (Hkv, desc.capacity))
-    wp, wn = _workspace(ws)
+    Hq, Hkv, d, dt = desc.n_q_heads, desc.n_kv_heads, desc.head_dim, _TORCH_DTYPE.get(desc.dtype)
+    dev = _device(Qs, "Qs")
+    q = _at(Qs, "Qs", dt, (S, Hq, d), dev)
+    k = _at(Ks, "Ks", dt, (S, Hkv, d), dev)
+    kc = _at(kcache, "kcache", dt, (Hkv, desc.capacity, d), dev) if L_prefix > 0 or kcache is not None else None
+    w = _at(weight, "weight", torch.float32, (Hkv, desc.capacity), dev)
+    wp, wn = _scratch(ws, dev)
     _launch(lambda s: load().kvr_cache_weigh(ctypes.byref(desc), q, k, kc, int(L_prefix), int(S), w, wp, wn, s),
-            "kvr_cache_weigh", stream, Qs, Ks, kcache, weight, ws)
+            "kvr_cache_weigh", stream, dev)
 
 
 def kvr_workspace_bytes_evict(desc, L):
@@ -578,17 +607,19 @@ def kvr_cache_evict(desc, kcache, vcache, L, weight, n_keep, kout, vout, n_first
     """Copy the n_keep rows of [0, L) with the most weight (the first n_first and the last
     n_last always) into kout, vout [n_kv_heads, capacity_out, head_dim]; weight_out
     [n_kv_heads, capacity_out] and index (int32 [n_kv_heads, n_keep]) are optional."""
-    Hkv, d = desc.n_kv_heads, desc.head_dim
-    kc, vc = _cache_ptrs(desc, kcache, vcache, True)
-    w = _check_typed(weight, "weight", torch.float32, (Hkv, desc.capacity))
+    Hkv, d, dt = desc.n_kv_heads, desc.head_dim, _TORCH_DTYPE.get(desc.dtype)
+    dev = _device(kcache, "kcache")
+    kc = _at(kcache, "kcache", dt, (Hkv, desc.capacity, d), dev)
+    vc = _at(vcache, "vcache", dt, (Hkv, desc.capacity, d), dev)
+    w = _at(weight, "weight", torch.float32, (Hkv, desc.capacity), dev)
     if not isinstance(kout, torch.Tensor) or kout.dim() != 3:
         raise ValueError("kout must be a tensor [n_kv_heads, capacity_out, head_dim]")
     cap = kout.shape[1]
-    ko = _check(kout, "kout", desc, (Hkv, cap, d))
-    vo = _check(vout, "vout", desc, (Hkv, cap, d))
-    wo = None if weight_out is None else _check_typed(weight_out, "weight_out", torch.float32, (Hkv, cap))
-    ix = None if index is None else _check_typed(index, "index", torch.int32, (Hkv, n_keep))
-    wp, wn = _workspace(ws)
+    ko = _at(kout, "kout", dt, (Hkv, cap, d), dev)
+    vo = _at(vout, "vout", dt, (Hkv, cap, d), dev)
+    wo = None if weight_out is None else _at(weight_out, "weight_out", torch.float32, (Hkv, cap), dev)
+    ix = None if index is None else _at(index, "index", torch.int32, (Hkv, n_keep), dev)
+    wp, wn = _scratch(ws, dev)
     _launch(lambda s: load().kvr_cache_evict(ctypes.byref(desc), kc, vc, int(L), w, int(n_first), int(n_last),
                                              int(n_keep), ko, vo, cap, wo, ix, wp, wn, s),
-            "kvr_cache_evict", stream, kcache, vcache, weight, kout, vout, weight_out, index, ws)
+            "kvr_cache_evict", stream, dev)
