@@ -39,6 +39,13 @@ int64_t way_rows(int way) { return way > kByRows ? 64 * (way - kByRows) : 16 * w
 // of more records.
 constexpr int64_t kMinKeysByKeys = 128, kMinKeysByRows = 256, kMinOwnKeys = 512;
 constexpr int64_t kMaxOwnSplits = 16;
+// A call of at most this many stages of prefix and own rows is one launch (kAlone), not the
+// items' and the merge's.  With 64 own rows, 2 readers: 8.3 us instead of 5.8 + 3.2 and the
+// gap between them at 255 keys, 10.3 instead of 5.8 + 3.1 at 512 (and one launch less to
+// issue, 3 us of the host's time), 14.1 instead of 5.9 + 3.2 at 1024; 64 readers: 15.3
+// instead of 15.2 + 4.0 at 255.  fp32, 255 keys: 13.1 instead of 8.3 + 3.1 for 2 readers, 26.6
+// instead of 19.3 + 4.1 for 64.
+constexpr int64_t kAloneStages = 20, kAloneStagesF32 = 10;
 
 struct SharedPlan {
     int pw, ow;
@@ -83,6 +90,8 @@ bool plan_shared(const kvr_desc *d, int64_t L, int64_t n, int64_t S, int64_t tca
         s.octs_o = ceil_div(own * s.nt, 8);
         s.octs_n = ceil_div(n * ceil_div(rows_o, 16) * d->n_kv_heads, 8 * kWaves);
         if ((s.octs_p + s.octs_o + s.octs_n) * 8 > kMaxGrid || s.rows > kMaxGrid) return false;
+        if (rows_o <= 16 && ceil_div(L, stage_keys(d)) + ceil_div(tcap, stage_keys(d)) <= (f32 ? kAloneStagesF32 : kAloneStages))
+            s.pw = kAlone;
         s.ws_bytes = (size_t)(want + s.nt + 1) * (size_t)s.rows * (d->head_dim + 2) * sizeof(float);
     }
     *out = s;

@@ -32,8 +32,9 @@ struct SharedParams {
 };
 // pw, ow: the ways of prefix and own items, ow <= pw.  1, 2: the four waves share 16 or 32
 // query rows and split the keys (2: fp32 only); kByRows + 1, + 2: each wave has 16 or 32
-// rows of its own (16-bit only; own items: + 1)
-constexpr int kByRows = 10;
+// rows of its own (16-bit only; own items: + 1).  pw kAlone: one launch, a workgroup for
+// each reader and kv head, at most 16 rows each
+constexpr int kByRows = 10, kAlone = 0;
 hipError_t launch_shared(const SharedParams &p, int head_dim, int dtype, int pw, int ow, hipStream_t s);
 
 // Attention weight received by each cached row (weigh.hip)

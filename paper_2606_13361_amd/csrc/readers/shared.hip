@@ -159,100 +159,127 @@ __device__ __forceinline__ int stage_rows(int64_t n, int t) {
 }
 
 // ---- by keys
-// A wave's stages first, first + WAVES, ... of `nkeys` cached rows at kb / vb.  K and V have
-// one set of registers each: the next stage's K is asked for when the scores are done,
-// its V when the outputs are.  begin() asks for the first; the caller takes its rows
-// meanwhile.
-template <class OP, int RT>
-struct ByKeys {
-    static constexpr int KEYS = OP::KEYS;
+// Consecutive cached rows, in stages
+template <class OP>
+struct Range {
     uint64_t kb, vb;
     int64_t nkeys;
-    int first, i, g;
+    __device__ __forceinline__ int stages() const { return (int)((nkeys + OP::KEYS - 1) / OP::KEYS); }
+    __device__ __forceinline__ int count(int t) const { return stage_rows<OP::KEYS>(nkeys, t); }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t k(int t) const { return rows(kb, t); }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t v(int t) const { return rows(vb, t); }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows(uint64_t base, int t) const {
+        return row_rsrc(base + (uint64_t)t * OP::KEYS * OP::ROWB, count(t), OP::ROWB, OP::ROWB);
+    }
+};
+
+// One after the other
+template <class OP>
+struct Ranges {
+    Range<OP> a, b;
+    int na;      // stages of a
+    __device__ __forceinline__ int stages() const { return na + b.stages(); }
+    __device__ __forceinline__ int count(int t) const { return t < na ? a.count(t) : b.count(t - na); }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t k(int t) const { return t < na ? a.k(t) : b.k(t - na); }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t v(int t) const { return t < na ? a.v(t) : b.v(t - na); }
+};
+
+// A wave's stages first, first + STEP, ... of a range.  K and V have one set of registers
+// each: the next stage's K is asked for when the scores are done, its V when the outputs
+// are.  begin() asks for the first; the caller takes its rows meanwhile.
+template <class OP, int RT, int STEP>
+struct ByKeys {
     typename OP::K k;
     typename OP::V v;
-    __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(uint64_t base, int t) const {
-        return row_rsrc(base + (uint64_t)t * KEYS * OP::ROWB, stage_rows<KEYS>(nkeys, t), OP::ROWB, OP::ROWB);
+    __device__ __forceinline__ void begin(const Range<OP> &r, int first, int i, int g) {
+        OP::load_k(k, r.k(first), OP::ROWB, i, g);
+        OP::load_v(v, r.v(first), OP::ROWB, i, g);
     }
-    __device__ __forceinline__ void begin(uint64_t kb_, uint64_t vb_, int64_t nkeys_, int first_, int lane) {
-        kb = kb_; vb = vb_; nkeys = nkeys_; first = first_;
-        i = lane & 15;
-        g = lane >> 4;
-        OP::load_k(k, rows_of(kb, first), OP::ROWB, i, g);
-        OP::load_v(v, rows_of(vb, first), OP::ROWB, i, g);
-    }
-    __device__ __forceinline__ void run(Rows<OP, RT> &R, float c2) {
-        const int nst = (int)((nkeys + KEYS - 1) / KEYS);
-        for (int t = first; t < nst; t += WAVES) {
+    template <class RANGE>
+    __device__ __forceinline__ void run(const RANGE &r, int first, Rows<OP, RT> &R, float c2, int i, int g) {
+        const int nst = r.stages();
+        for (int t = first; t < nst; t += STEP) {
             float s[RT][1][OP::NS];
             typename OP::P w[RT][1];
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) OP::scores(k, R.q[rt], s[rt][0]);
             __builtin_amdgcn_sched_barrier(0);
-            OP::load_k(k, rows_of(kb, t + WAVES), OP::ROWB, i, g);
+            OP::load_k(k, r.k(t + STEP), OP::ROWB, i, g);
             __builtin_amdgcn_sched_barrier(0);
-            softmax_step<OP, RT, 1>(R, s, w, stage_rows<KEYS>(nkeys, t), c2, g);
+            softmax_step<OP, RT, 1>(R, s, w, r.count(t), c2, g);
             OP::template accumulate<RT>(v, w, R.o);
             __builtin_amdgcn_sched_barrier(0);
-            OP::load_v(v, rows_of(vb, t + WAVES), OP::ROWB, i, g);
+            OP::load_v(v, r.v(t + STEP), OP::ROWB, i, g);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
 };
 
-// LDS of the join of one row tile: O of every wave, component c of the lane's four in
-// row c, then (m, l)
-template <class OP>
+// LDS of the join of one row tile by W waves: O of every wave, component c of the lane's
+// four in row c, then (m, l)
+template <class OP, int W>
 constexpr int obuf_floats() {
-    return WAVES * 4 * 64 * OP::NT;
+    return W * 4 * 64 * OP::NT;
 }
-template <class OP>
+template <class OP, int W>
 constexpr int join_floats() {
-    return obuf_floats<OP>() + 2 * WAVES * 64;
+    return obuf_floats<OP, W>() + 2 * W * 64;
 }
 
-// The partials of the workgroup's waves: every wave posts its own, then joins, in wave
-// order, one component of each row's outputs (NT consecutive head-dim indices a lane) and
-// stores it to record `rec`.
+// Every wave posts its partial of a row tile; after a barrier a wave joins, in wave order,
+// component c of each row's outputs (head-dim indices NT (4 g + c) .. of the lane) over
+// the larger reference M
+template <class OP, int W>
+__device__ __forceinline__ void post(const f32x4 (&o)[OP::NT], float m, float l, float *lds, int wave, int lane) {
+    constexpr int NT = OP::NT;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int t = 0; t < NT; t += 4)
+            *(f32x4 *)(lds + ((wave * 4 + c) * 64 + lane) * NT + t) = (f32x4){o[t][c], o[t + 1][c], o[t + 2][c], o[t + 3][c]};
+    *(float2 *)(lds + obuf_floats<OP, W>() + (wave * 64 + lane) * 2) = make_float2(m, l);
+}
+template <class OP, int W>
+__device__ __forceinline__ void joined(const float *lds, int c, int lane, f32x4 (&acc)[OP::NT / 4], float &M, float &l) {
+    constexpr int NT = OP::NT;
+    const float *ml = lds + obuf_floats<OP, W>();
+    M = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int t = 0; t < NT / 4; ++t) acc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < W; ++s) M = fmaxf(M, ml[(s * 64 + lane) * 2]);
+#pragma unroll
+    for (int s = 0; s < W; ++s) {
+        const float2 w = *(const float2 *)(ml + (s * 64 + lane) * 2);
+        const float a = __builtin_amdgcn_exp2f(w.x - M);
+        l = __builtin_fmaf(a, w.y, l);
+#pragma unroll
+        for (int t = 0; t < NT / 4; ++t) {
+            const f32x4 x = *(const f32x4 *)(lds + ((s * 4 + c) * 64 + lane) * NT + 4 * t);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[t][e] = __builtin_fmaf(a, x[e], acc[t][e]);
+        }
+    }
+}
+
+// The partials of the workgroup's waves to record `rec`
 template <class OP, int RT>
 __device__ __forceinline__ void join(const SharedParams &p, Rows<OP, RT> &R, float *lds, int64_t rec, int wave, int lane) {
-    constexpr int NT = OP::NT;
-    const int g = lane >> 4, c = wave;
-    float *ml = lds + obuf_floats<OP>();
+    const int g = lane >> 4;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         if (rt) __syncthreads();
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int t = 0; t < NT; t += 4)
-                *(f32x4 *)(lds + ((wave * 4 + c) * 64 + lane) * NT + t) =
-                    (f32x4){R.o[rt][t][c], R.o[rt][t + 1][c], R.o[rt][t + 2][c], R.o[rt][t + 3][c]};
-        *(float2 *)(ml + (wave * 64 + lane) * 2) = make_float2(R.m[rt], OP::total(R.l[rt]));
+        post<OP, WAVES>(R.o[rt], R.m[rt], OP::total(R.l[rt]), lds, wave, lane);
         __syncthreads();
-        float M = -INFINITY, l = 0.f;
-        f32x4 acc[NT / 4];
-#pragma unroll
-        for (int t = 0; t < NT / 4; ++t) acc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < WAVES; ++s) M = fmaxf(M, ml[(s * 64 + lane) * 2]);
-#pragma unroll
-        for (int s = 0; s < WAVES; ++s) {
-            const float2 w = *(const float2 *)(ml + (s * 64 + lane) * 2);
-            const float a = __builtin_amdgcn_exp2f(w.x - M);
-            l = __builtin_fmaf(a, w.y, l);
-#pragma unroll
-            for (int t = 0; t < NT / 4; ++t) {
-                const f32x4 x = *(const f32x4 *)(lds + ((s * 4 + c) * 64 + lane) * NT + 4 * t);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[t][e] = __builtin_fmaf(a, x[e], acc[t][e]);
-            }
-        }
+        f32x4 acc[OP::NT / 4];
+        float M, l;
+        joined<OP, WAVES>(lds, wave, lane, acc, M, l);
         if (R.at[rt] < 0) continue;
-        float *po = record_o<OP>(p, rec, R.at[rt]) + NT * (4 * g + c);
+        float *po = record_o<OP>(p, rec, R.at[rt]) + OP::NT * (4 * g + wave);
 #pragma unroll
-        for (int t = 0; t < NT / 4; ++t) *(f32x4 *)(po + 4 * t) = acc[t];
-        if (c == 0 && g == 0) *record_ml<OP>(p, rec, R.at[rt]) = make_float2(M, l);
+        for (int t = 0; t < OP::NT / 4; ++t) *(f32x4 *)(po + 4 * t) = acc[t];
+        if (wave == 0 && g == 0) *record_ml<OP>(p, rec, R.at[rt]) = make_float2(M, l);
     }
 }
 
@@ -359,7 +386,7 @@ constexpr int rows_of(int way) { return way > kByRows ? 64 * (way - kByRows) : 1
 template <class OP, int WAY>
 constexpr int lds_bytes() {
     if constexpr (WAY > kByRows) return SLOTS * 2 * OP::Ring::HALF;
-    else return join_floats<OP>() * 4;
+    else return join_floats<OP, WAVES>() * 4;
 }
 
 // Rows r0 .. of `nrows` query rows (take_rows) over `nkeys` cached rows at k / v, to record
@@ -382,10 +409,11 @@ __device__ __forceinline__ void attend(const SharedParams &p, const Item &it, un
         keys.run(R, p.scale_log2);
         put_rows<OP, RT>(p, R, it.rec, g);
     } else {
-        ByKeys<OP, RT> keys;
-        keys.begin(it.k, it.v, it.nkeys, wave, lane);
+        const Range<OP> range{it.k, it.v, it.nkeys};
+        ByKeys<OP, RT, WAVES> keys;
+        keys.begin(range, wave, i, g);
         take_rows(p, R, it.hd, it.tok0, it.r0, it.nrows, i, g, it.len);
-        keys.run(R, p.scale_log2);
+        keys.run(range, wave, R, p.scale_log2, i, g);
         join<OP, RT>(p, R, (float *)lds, it.rec, wave, lane);
     }
 }
@@ -441,21 +469,16 @@ __device__ __forceinline__ void own_item(const SharedParams &p, uint32_t x, unsi
     attend<OP, WAY>(p, it, lds, wave, lane);
 }
 
-// New item x, a wave's: (reader, 16-row tile, kv head), kv head fastest
-template <class OP>
-__device__ __forceinline__ void new_item(const SharedParams &p, uint32_t x, int lane) {
-    constexpr int KEYS = 16, NT = OP::NT;      // (one part of a 16-bit stage: fewer registers)
+// ---- new rows
+// Rows r0 .. r0 + 15 of reader rd and kv head hd over its new rows, causally: a wave's
+// partial, for done(R, g).  store: and these rows to the reader's cache, behind its len
+// rows there.
+template <class OP, class DONE>
+__device__ __forceinline__ void attend_new(const SharedParams &p, int rd, int hd, int r0, int len, bool store, int lane, DONE done) {
+    constexpr int KEYS = 16;      // (one part of a 16-bit stage: fewer registers)
     int i = lane & 15, g = lane >> 4;
-    const int hd = (int)(x % p.n_kv_heads);
-    x /= p.n_kv_heads;
-    const int nrows = p.S * p.group, tiles = (nrows + 15) / 16;
-    const int tile = (int)(x % tiles), rd = (int)(x / tiles);
-    if (rd >= p.n) return;
-    const int len = reader_len(p, rd);
-    if (len < 0) return;
-    // new rows that a row of this tile sees; the last tile sees all and stores them
-    const int seen = min(p.S, (min(tile * 16 + 16, nrows) - 1) / p.group + 1);
-    const bool store = p.append && tile == tiles - 1;
+    const int nrows = p.S * p.group;
+    const int seen = min(p.S, (min(r0 + 16, nrows) - 1) / p.group + 1);      // new rows that a row sees
     const uint32_t nb = (uint32_t)p.n_kv_heads * OP::ROWB;
     const uint64_t src = ((uint64_t)rd * p.S * p.n_kv_heads + hd) * OP::ROWB;
     const uint64_t to = (((uint64_t)rd * p.n_kv_heads + hd) * p.tcap + len) * OP::ROWB;
@@ -469,7 +492,7 @@ __device__ __forceinline__ void new_item(const SharedParams &p, uint32_t x, int 
         OP::template load_v<1>(v, row_rsrc((uint64_t)(uintptr_t)p.vn + at, n, nb, OP::ROWB), nb, i, g);
     };
     load(0);
-    take_rows(p, R, hd, rd * p.S, tile * 16, nrows, i, g, len);
+    take_rows(p, R, hd, rd * p.S, r0, nrows, i, g, len);
     for (int c0 = 0; c0 < seen; c0 += KEYS) {
         const int n = min(seen - c0, KEYS);
         asm volatile("" : "+v"(i), "+v"(g));      // addresses are made in the loop: registers for all are not there
@@ -494,7 +517,7 @@ __device__ __forceinline__ void new_item(const SharedParams &p, uint32_t x, int 
             const float alpha = __builtin_amdgcn_exp2f(R.m[0] - mn);
             R.l[0] *= alpha;
 #pragma unroll
-            for (int t = 0; t < NT; ++t) R.o[0][t] *= alpha;
+            for (int t = 0; t < OP::NT; ++t) R.o[0][t] *= alpha;
         }
         R.m[0] = mn;
 #pragma unroll
@@ -512,15 +535,32 @@ __device__ __forceinline__ void new_item(const SharedParams &p, uint32_t x, int 
             }
         }
     }
-    const float l = OP::total(R.l[0]);
-    if (R.at[0] < 0) return;
-    float *po = record_o<OP>(p, p.nrec - 1, R.at[0]) + NT * 4 * g;
+    done(R, g);
+}
+
+// New item x, a wave's: (reader, 16-row tile, kv head), kv head fastest.  The last tile sees
+// all new rows, and stores them.
+template <class OP>
+__device__ __forceinline__ void new_item(const SharedParams &p, uint32_t x, int lane) {
+    constexpr int NT = OP::NT;
+    const int hd = (int)(x % p.n_kv_heads);
+    x /= p.n_kv_heads;
+    const int tiles = (p.S * p.group + 15) / 16;
+    const int tile = (int)(x % tiles), rd = (int)(x / tiles);
+    if (rd >= p.n) return;
+    const int len = reader_len(p, rd);
+    if (len < 0) return;
+    attend_new<OP>(p, rd, hd, tile * 16, len, p.append && tile == tiles - 1, lane, [&](const Rows<OP, 1> &R, int g) {
+        const float l = OP::total(R.l[0]);
+        if (R.at[0] < 0) return;
+        float *po = record_o<OP>(p, p.nrec - 1, R.at[0]) + NT * 4 * g;
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+        for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int t = 0; t < NT; t += 4)
-            *(f32x4 *)(po + NT * c + t) = (f32x4){R.o[0][t][c], R.o[0][t + 1][c], R.o[0][t + 2][c], R.o[0][t + 3][c]};
-    if (g == 0) *record_ml<OP>(p, p.nrec - 1, R.at[0]) = make_float2(R.m[0], l);
+            for (int t = 0; t < NT; t += 4)
+                *(f32x4 *)(po + NT * c + t) = (f32x4){R.o[0][t][c], R.o[0][t + 1][c], R.o[0][t + 2][c], R.o[0][t + 3][c]};
+        if (g == 0) *record_ml<OP>(p, p.nrec - 1, R.at[0]) = make_float2(R.m[0], l);
+    });
 }
 
 // PW, OW: the ways of prefix and own items
@@ -535,6 +575,57 @@ __global__ __launch_bounds__(256, OP::ELT == 2 ? 3 : 2) void shared_kernel(const
     if (oct < p.oct_own) prefix_item<OP, PW>(p, oct, in8, lds, wave, lane);
     else if (oct < p.oct_new) own_item<OP, OW>(p, (oct - p.oct_own) * 8 + in8, lds, wave, lane);
     else new_item<OP>(p, ((oct - p.oct_new) * 8 + in8) * WAVES + wave, lane);
+}
+
+// ---- alone
+// A short call in one launch: a workgroup does all that the rows of one reader and kv head
+// see, the last wave the new rows, the others the stages of prefix and own rows in turn.
+// Every reader reads the prefix anew, no partial goes through memory.
+constexpr int ALONE_WAVES = 8;
+
+template <class OP>
+__global__ __launch_bounds__(64 * ALONE_WAVES) void shared_alone_kernel(const SharedParams p) {
+    constexpr int W = ALONE_WAVES;
+    __shared__ __attribute__((aligned(16))) float lds[join_floats<OP, W>()];
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hd = blockIdx.x % p.n_kv_heads, rd = blockIdx.x / p.n_kv_heads;
+    Rows<OP, 1> R;
+    int len;
+    if (wave == W - 1) {
+        len = reader_len(p, rd);
+        if (len >= 0)
+            attend_new<OP>(p, rd, hd, 0, len, p.append != 0, lane, [&](const Rows<OP, 1> &N, int) {
+                post<OP, W>(N.o[0], N.m[0], OP::total(N.l[0]), lds, wave, lane);
+            });
+    } else {
+        const uint64_t at = (uint64_t)hd * p.cap * OP::ROWB;
+        Ranges<OP> keys;
+        keys.a = Range<OP>{(uint64_t)(uintptr_t)p.kc + at, (uint64_t)(uintptr_t)p.vc + at, p.L};
+        keys.na = keys.a.stages();
+        ByKeys<OP, 1, W - 1> by;
+        if (wave < keys.na) by.begin(keys.a, wave, i, g);
+        len = reader_len(p, rd);
+        const uint64_t own = ((uint64_t)rd * p.n_kv_heads + hd) * p.tcap * OP::ROWB;
+        keys.b = Range<OP>{(uint64_t)(uintptr_t)p.kt + own, (uint64_t)(uintptr_t)p.vt + own, max(len, 0)};
+        if (wave >= keys.na) by.begin(keys.b, wave - keys.na, i, g);
+        if (len >= 0) {
+            take_rows(p, R, hd, rd * p.S, 0, p.S * p.group, i, g, len);
+            by.run(keys, wave, R, p.scale_log2, i, g);
+            post<OP, W>(R.o[0], R.m[0], OP::total(R.l[0]), lds, wave, lane);
+        }
+    }
+    if (len < 0) return;      // all waves
+    __syncthreads();
+    if (wave >= 4 || R.at[0] < 0) return;
+    f32x4 acc[OP::NT / 4];
+    float M, l;
+    joined<OP, W>(lds, wave, lane, acc, M, l);
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int t = 0; t < OP::NT / 4; ++t)
+        OP::put4((unsigned char *)p.out + (int64_t)R.at[0] * OP::ROWB, OP::NT * (4 * g + wave) + 4 * t, acc[t][0] * inv,
+                 acc[t][1] * inv, acc[t][2] * inv, acc[t][3] * inv);
 }
 
 // out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over the records of a row.  A wave
@@ -607,6 +698,10 @@ template <class OP>
 hipError_t launch_op(const SharedParams &p, int pw, int ow, hipStream_t s) {
     const dim3 grid((unsigned)(p.oct_all * 8)), block(256);
     constexpr int R = kByRows;
+    if (pw == kAlone) {
+        hipLaunchKernelGGL(shared_alone_kernel<OP>, dim3((unsigned)(p.n * p.n_kv_heads)), dim3(64 * ALONE_WAVES), 0, s, p);
+        return hipGetLastError();
+    }
     if (pw == 1) hipLaunchKernelGGL((shared_kernel<OP, 1, 1>), grid, block, 0, s, p);
     else if constexpr (OP::ELT == 2) {
         if (pw == R + 1 && ow == 1) hipLaunchKernelGGL((shared_kernel<OP, R + 1, 1>), grid, block, 0, s, p);

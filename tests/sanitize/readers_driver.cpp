@@ -38,6 +38,12 @@ hipError_t launch_shared(const SharedParams &p, int head_dim, int dtype, int pw,
     ++g_launches;
     const int64_t G = p.group, rows_p = (int64_t)p.n * p.S * G, rows_o = (int64_t)p.S * G;
     const bool f32 = dtype == KVR_F32;
+    if (pw == kAlone) {      // a workgroup for each reader and kv head
+        const int64_t keys = f32 ? 16 : 32;
+        if (rows_o > 16 || (p.L + keys - 1) / keys + (p.tcap + keys - 1) / keys > 20) BAD("alone");
+        if ((int64_t)p.n * p.n_kv_heads > 0xffffff) BAD("alone: grid");
+        return hipErrorUnknown;
+    }
     const int64_t tp = pw > kByRows ? 64 * (pw - kByRows) : 16 * pw, to = ow > kByRows ? 64 * (ow - kByRows) : 16 * ow;
     if (ow > pw || (f32 ? pw > 2 : pw == 2 || ow == 2 || pw > kByRows + 2 || ow > kByRows + 1)) BAD("ways %d %d", pw, ow);
     if (p.p_tiles != (rows_p + tp - 1) / tp || p.t_tiles != (rows_o + to - 1) / to) BAD("tiles");

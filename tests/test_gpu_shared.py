@@ -135,6 +135,19 @@ PARITY = [
     (F32, Q, 2, 1, 100, [0, 21], 40),
     (F32, (6, 3, 128), 5, 17, 49, [0, 1, 15, 16, 17], 40),
     (BF16, (5, 5, 64), 2, 1, 0, [700, 3], 701),                   # no prefix, split own rows
+    # one launch up to 20 stages (fp32: 10) of 32 (16) prefix and own rows, up to 16 rows a reader and kv head
+    (BF16, Q, 3, 4, 320, [320, 0, 314], 320), (BF16, Q, 3, 4, 321, [320, 0, 314], 320), (F16, Q, 3, 5, 320, [315, 0, 9], 320),
+    (F32, Q, 3, 4, 80, [80, 0, 70], 80), (F32, Q, 3, 4, 81, [80, 0, 70], 80), (BF16, (8, 8, 64), 2, 16, 30, [0, 9], 40),
+    (F16, (8, 8, 64), 2, 17, 30, [0, 9], 40), (BF16, Q, 1, 1, 0, [639], 640), (BF16, Q, 300, 1, 40, list(range(300)), 301),
+    # the same readers as before, in items
+    (BF16, Q, 1, 1, 0, [0], 700), (BF16, Q, 1, 1, 1, [0], 700), (BF16, Q, 9, 1, 300, [-1, 0, 31, 32, 33, 64, 127, 128, 129], 800),
+    (F16, Q, 5, 4, 129, [0, 5, 28, 60, 61], 700), (BF16, (8, 8, 128), 33, 1, 127, list(range(33)), 700),
+    (F16, (12, 3, 128), 7, 3, 200, [0, 1, 2, 50, -1, 33, 17], 700), (F32, Q, 2, 1, 100, [0, 21], 400),
+    # rows of a kv head where a prefix item has 16, 64 and 128 of them, and one more
+    (BF16, Q, 4, 1, 700, [1, 2, 3, 4], 30), (BF16, Q, 16, 1, 700, list(range(16)), 30), (BF16, Q, 17, 1, 700, list(range(17)), 30),
+    (BF16, Q, 32, 1, 700, list(range(32)), 40), (BF16, Q, 33, 1, 700, list(range(33)), 40),
+    (F32, (8, 8, 64), 16, 1, 300, list(range(16)), 30), (F32, (8, 8, 64), 33, 1, 300, list(range(33)), 40),
+    (BF16, (4096, 4096, 64), 1, 1, 5, [3], 8), (F16, (4096, 1, 64), 1, 1, 5, [3], 8),      # the most heads
 ]
 
 
@@ -145,9 +158,14 @@ def test_parity(case, rope, append):
     run(Batch(*case, rope_base=rope, seed=len(case[5])), append)
 
 
-def test_no_tails():
+# prefixes of a call in one launch and of one in items and a merge
+BOTH = pytest.mark.parametrize("L", [64, 700])
+
+
+@BOTH
+def test_no_tails(L):
     """First tokens of readers that have no rows yet and keep none: no tail tensors."""
-    b = Batch(BF16, Q, 3, 4, 200, [0, 0, 0], 0)
+    b = Batch(BF16, Q, 3, 4, L, [0, 0, 0], 0)
     t = b.gpu()
     t["kt"] = t["vt"] = None
     b.call(t, append=False)
@@ -155,24 +173,27 @@ def test_no_tails():
     b.check(t, append=False)
 
 
-def test_positions_go_on_from_pos0():
+@BOTH
+def test_positions_go_on_from_pos0(L):
     """A prefix that rows were evicted from: positions are not row numbers."""
-    run(Batch(BF16, Q, 2, 2, 100, [5, 40], 64, rope_base=1e6, pos0=4000))
+    run(Batch(BF16, Q, 2, 2, L, [5, 40], 64, rope_base=1e6, pos0=4000))
 
 
-def test_readers_that_do_not_fit_take_no_part():
-    b = Batch(BF16, Q, 6, 3, 64, [-1, 30, 29, 32, 33, -2 ** 31], 32)
+@BOTH
+def test_readers_that_do_not_fit_take_no_part(L):
+    b = Batch(BF16, Q, 6, 3, L, [-1, 30, 29, 32, 33, -2 ** 31], 32)
     assert b.active(True) == [False, False, True, False, False, False]
     assert b.active(False) == [False, True, True, True, False, False]
     run(b, True)
     run(b, False)
 
 
+@BOTH
 @pytest.mark.parametrize("dt", [BF16, F16, F32], ids=str)
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-def test_later_tokens_do_not_reach_earlier_ones(dt, bad):
+def test_later_tokens_do_not_reach_earlier_ones(dt, bad, L):
     """Token 2 of reader 1 holds no numbers: the tokens before it, and other readers, are as without it."""
-    b = Batch(dt, (16, 4, 64), 3, 5, 70, [0, 9, 40], 64, rope_base=1e4)
+    b = Batch(dt, (16, 4, 64), 3, 4 if L < 700 else 5, L, [0, 9, 40], 64, rope_base=1e4)
     good = run(b)
     b.k[1, 2], b.v[1, 2] = bad, bad
     t = b.gpu()
@@ -184,23 +205,24 @@ def test_later_tokens_do_not_reach_earlier_ones(dt, bad):
     assert not torch.isfinite(got[1, 2:].float()).any()
 
 
-def test_far_rows():
+@BOTH
+def test_far_rows(L):
     """Offsets past 2^32 bytes: the last kv head's prefix, the last reader's rows."""
     Hq, Hkv, d = 16, 8, 128
     cap = 2_400_000                       # 8 x 2.4M x 256 bytes = 4.9 GB
-    b = Batch(BF16, (Hq, Hkv, d), 3, 1, 77, [3, 0, 20], 24)
+    b = Batch(BF16, (Hq, Hkv, d), 3, 1, L, [3, 0, 20], 24)
     t = b.gpu()
     big = torch.zeros((Hkv, cap, d), dtype=BF16, device=DEV)
-    big[:, :77] = t["kc"][:, :77]
+    big[:, :L] = t["kc"][:, :L]
     t["kc"] = big
     big = torch.zeros((Hkv, cap, d), dtype=BF16, device=DEV)
-    big[:, :77] = t["vc"][:, :77]
+    big[:, :L] = t["vc"][:, :L]
     t["vc"] = big
     b.desc = kvr.make_desc(Hq, Hkv, d, BF16, cap)
     b.call(t)
     b.check(t)
     del t, big
-    b = Batch(BF16, (Hq, Hkv, d), 3, 1, 77, [3, -1, 20], 24)
+    b = Batch(BF16, (Hq, Hkv, d), 3, 1, L, [3, -1, 20], 24)
     t = b.gpu()
     tcap = 900_000                        # 3 readers x 8 heads x 0.9M x 256 bytes = 5.5 GB
     kt, vt = (torch.zeros((3, Hkv, tcap, d), dtype=BF16, device=DEV) for _ in range(2))
@@ -213,8 +235,9 @@ def test_far_rows():
     b.check(t)
 
 
-def test_same_bits_twice_and_on_another_stream():
-    b = Batch(BF16, Q, 20, 2, 700, list(range(0, 200, 10)), 210, rope_base=1e6)
+@BOTH
+def test_same_bits_twice_and_on_another_stream(L):
+    b = Batch(BF16, Q, 20, 2, L, list(range(0, 200, 10)), 210, rope_base=1e6)
     one = run(b)
     s = torch.cuda.Stream()
     t = b.gpu()
@@ -228,10 +251,11 @@ def test_same_bits_twice_and_on_another_stream():
     assert torch.equal(t["out"].cpu(), one)
 
 
-def test_one_graph_serves_a_decode():
+@BOTH
+def test_one_graph_serves_a_decode(L):
     """Lengths, rows and outputs of a captured step follow the tensors: eager steps give the same bits,
     with the program's own work between the replays."""
-    b = Batch(BF16, Q, 7, 1, 400, [0, 3, 30, 31, -1, 60, 5], 70, rope_base=1e6)
+    b = Batch(BF16, Q, 7, 1, L, [0, 3, 30, 31, -1, 60, 5], 70, rope_base=1e6)
     t, e = b.gpu(), b.gpu()
     t["step"] = (t["len"] >= 0).int()
     b.call(t)                                   # warm up
@@ -254,8 +278,9 @@ def test_one_graph_serves_a_decode():
             assert torch.equal(t[x].view(torch.int16), e[x].view(torch.int16)), (step, x)
 
 
-def test_two_streams_with_a_workspace_each():
-    b, c = (Batch(BF16, Q, 16, 1, 900, [10 * i for i in range(16)], 160, seed=s) for s in (1, 2))
+@BOTH
+def test_two_streams_with_a_workspace_each(L):
+    b, c = (Batch(BF16, Q, 16, 1, L, [10 * i for i in range(16)], 160, seed=s) for s in (1, 2))
     t, u = b.gpu(), c.gpu()
     torch.cuda.synchronize()
     s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
@@ -267,9 +292,10 @@ def test_two_streams_with_a_workspace_each():
     c.check(u, append=False)
 
 
-def test_agrees_with_single_continuations():
+@BOTH
+def test_agrees_with_single_continuations(L):
     """Each reader alone, over its own copy of prefix and rows, through kvr_continue: within both calls' bounds."""
-    b = Batch(BF16, Q, 4, 3, 250, [0, 17, 64, 100], 128)
+    b = Batch(BF16, Q, 4, 3, L, [0, 17, 64, 100], 128)
     got = run(b)
     Hq, Hkv, d = b.heads
     for i, ln in enumerate(b.lens):
@@ -286,8 +312,9 @@ def test_agrees_with_single_continuations():
         assert (np.abs(O._f64(out) - O._f64(got[i])) <= far).all()
 
 
-def test_a_scale_of_its_own():
-    b = Batch(BF16, Q, 2, 2, 60, [4, 9], 32)
+@BOTH
+def test_a_scale_of_its_own(L):
+    b = Batch(BF16, Q, 2, 2, L, [4, 9], 32)
     b.desc = kvr.make_desc(*Q, BF16, b.kc.shape[1], scale=0.03)
     t = b.gpu()
     b.call(t)
