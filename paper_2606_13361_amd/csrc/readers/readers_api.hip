@@ -121,7 +121,8 @@ bool plan_weigh(const kvr_desc *d, int64_t L, int64_t S, WeighPlan *out) {
         int64_t want = ceil_div(2 * kCus, base);
         const int64_t most = ceil_div(stages, kWaves);
         if (want > most) want = most;
-        w.chunk = ceil_div(ceil_div(stages, want), kWaves) * kWaves;
+        const int64_t step = w.way > kByRows ? 1 : kWaves;      // the waves share a stage, or take one each
+        w.chunk = ceil_div(ceil_div(stages, want), step) * step;
         w.nsplit = ceil_div(stages, w.chunk);
         w.grid = base * w.nsplit;
         // second pass: keys held in registers serve every row, as long as the workgroups fill the part

@@ -301,24 +301,29 @@ __device__ __forceinline__ void take_norms(const WeighParams &p, float *norm, in
     }
 }
 
-// The weights of a wave's keys, summed over the lanes of a key's 16 rows, into the buffer
-template <class OP, int HELD>
-__device__ __forceinline__ void add_to_buffer(const WeighParams &p, const Keys<OP> &keys, float (&acc)[HELD][OP::NS], int hd,
-                                              int t0, int n_all, int i, int g) {
+// The lane's place in the buffer for stage t of its wave's keys (t >= n_all: there is none):
+// lane (i, g) has that of score i, after the sum over the sixteen lanes of a g; null for
+// lanes beyond, and keys past the last
+template <class OP>
+__device__ __forceinline__ float *place_of(const WeighParams &p, const Keys<OP> &keys, int hd, int t, int n_all, int i, int g) {
+    const int n = t < n_all ? keys.count(t) : 0, key = OP::key_of(i & (OP::NS - 1), g);
+    if (i >= OP::NS || key >= n) return nullptr;
+    return p.weight + (int64_t)hd * p.cap + (keys.is_new(t) ? p.L : 0) + keys.first(t) + key;
+}
+
+// The weights of a stage's keys, of each lane's rows, summed over the lanes of a key's 16
+// rows and added to what the buffer held
+template <class OP>
+__device__ __forceinline__ void add_to(float *place, float held, const float (&acc)[OP::NS], int i) {
+    float mine = 0.f;
 #pragma unroll
-    for (int h = 0; h < HELD; ++h) {
-        const int t = t0 + h;
-        const int n = t < n_all ? keys.count(t) : 0;
-        const int64_t first = (keys.is_new(t) ? p.L : 0) + keys.first(t);
+    for (int e = 0; e < OP::NS; ++e) {
+        float x = acc[e];
 #pragma unroll
-        for (int e = 0; e < OP::NS; ++e) {
-            float x = acc[h][e];
-#pragma unroll
-            for (int d = 1; d < 16; d <<= 1) x += __shfl_xor(x, d);
-            const int key = OP::key_of(e, g);
-            if (i == e && key < n) p.weight[(int64_t)hd * p.cap + first + key] += x;
-        }
+        for (int d = 1; d < 16; d <<= 1) x += __shfl_xor(x, d);
+        mine = i == e ? x : mine;
     }
+    if (place) *place = held + mine;
 }
 
 // block: (group of WAVES stages, kv head), kv head fastest.  The query rows go through LDS
@@ -339,10 +344,12 @@ __global__ __launch_bounds__(256) void weigh_sum_rows_kernel(const WeighParams p
     const uint32_t qa = RG::row_at(i, g);
     const uint64_t q0 = (uint64_t)(uintptr_t)p.q + (uint64_t)hd * G * OP::ROWB;
     typename OP::K k;
-    float acc[1][OP::NS];
+    float acc[OP::NS];
     keys.load(k, t, t < n_all ? keys.count(t) : 0, i, g);
+    float *const place = place_of(p, keys, hd, t, n_all, i, g);
+    const float held = place ? *place : 0.f;      // (asked for here: not a round trip of its own at the end)
 #pragma unroll
-    for (int e = 0; e < OP::NS; ++e) acc[0][e] = 0.f;
+    for (int e = 0; e < OP::NS; ++e) acc[e] = 0.f;
     // This wave's quarter of each stage, rows of the kv head one after the other (past the
     // last: it again): from one stage to the next a row's head goes on by 32 mod G, its
     // token by 32 / G, and one more where the head passes the group's last.
@@ -381,7 +388,7 @@ __global__ __launch_bounds__(256) void weigh_sum_rows_kernel(const WeighParams p
             OP::scores(k, q, s);
             if constexpr (NEW) mask<OP>(s, (r0 + rr + 16 * part + i) / G - (int)keys.first(t), g);
 #pragma unroll
-            for (int e = 0; e < OP::NS; ++e) acc[0][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c2, -nm));
+            for (int e = 0; e < OP::NS; ++e) acc[e] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c2, -nm));
         }
     };
     for (int r0 = 0; r0 < rows; r0 += ROWS_AT_ONCE) {
@@ -405,7 +412,7 @@ __global__ __launch_bounds__(256) void weigh_sum_rows_kernel(const WeighParams p
         if (keys.is_new(t)) walk(std::true_type{});
         else walk(std::false_type{});
     }
-    add_to_buffer<OP, 1>(p, keys, acc, hd, t, n_all, i, g);
+    add_to<OP>(place, held, acc, i);
 }
 
 // The same with the query rows straight from memory
@@ -421,10 +428,12 @@ __global__ __launch_bounds__(256) void weigh_sum_kernel(const WeighParams p) {
     const int t0 = ((int)(blockIdx.x / p.n_kv_heads) * WAVES + wave) * HELD;
     const float c2 = p.scale_log2;
     typename OP::K k[HELD];
-    float acc[HELD][OP::NS];
+    float acc[HELD][OP::NS], *place[HELD], held[HELD];
 #pragma unroll
     for (int h = 0; h < HELD; ++h) {
         keys.load(k[h], t0 + h, t0 + h < n_all ? keys.count(t0 + h) : 0, i, g);
+        place[h] = place_of(p, keys, hd, t0 + h, n_all, i, g);
+        held[h] = place[h] ? *place[h] : 0.f;
 #pragma unroll
         for (int e = 0; e < OP::NS; ++e) acc[h][e] = 0.f;
     }
@@ -464,7 +473,8 @@ __global__ __launch_bounds__(256) void weigh_sum_kernel(const WeighParams p) {
             q = next;
         }
     }
-    add_to_buffer<OP, HELD>(p, keys, acc, hd, t0, n_all, i, g);
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) add_to<OP>(place[h], held[h], acc[h], i);
 }
 
 template <class E, int D>

@@ -50,6 +50,11 @@ WEIGH = [
     (BF16, Q, 33, 65), (F16, (8, 8, 128), 7, 129), (BF16, (12, 3, 128), 5, 200), (BF16, (64, 8, 128), 200, 300),
     (BF16, (128, 2, 128), 20, 70), (BF16, (16, 2, 64), 3, 511), (F16, (8, 2, 64), 40, 5), (F32, Q, 1, 100),
     (F32, (16, 2, 64), 19, 77), (F32, (6, 3, 128), 50, 0),
+    # query rows of a kv head where the passes take other tiles, and one more
+    (BF16, (8, 8, 128), 16, 300), (BF16, (8, 8, 128), 17, 300), (F16, (8, 8, 64), 32, 300), (F16, (8, 8, 64), 33, 300),
+    (BF16, (8, 8, 64), 64, 200), (BF16, (8, 8, 64), 65, 200), (BF16, (4, 4, 128), 128, 777), (BF16, (4, 4, 128), 129, 777),
+    (F16, (2, 2, 64), 1024, 100), (F16, (2, 2, 64), 1025, 100), (F32, (2, 2, 64), 1025, 20), (BF16, (1, 1, 64), 300, 5000),
+    (F32, (64, 64, 64), 2, 1100), (F32, (64, 64, 64), 2, 900), (BF16, (4096, 4096, 64), 1, 40), (BF16, (4096, 1, 64), 2, 40),
 ]
 
 
@@ -110,6 +115,11 @@ EVICT = [
     (1023, 500, 0, 0, "equal"), (1025, 500, 1, 0, "zeros"), (5000, 1250, 4, 24, "normal"), (4096, 4000, 0, 1, "ties"),
     (3333, 1000, 2, 2, "odd"), (20000, 5000, 4, 128, "normal"), (70001, 30000, 0, 0, "normal"),
     (500, 100, 0, 0, "tiny"), (1000, 200, 4, 3, "tiny"), (1000, 900, 4, 3, "tiny"), (40000, 100, 0, 5, "tiny"),
+    (1000, 300, 4, 3, "negative"), (5000, 4000, 0, 0, "negative"), (40000, 30000, 0, 0, "negative"), (3333, 1800, 2, 2, "odd"),
+    (3333, 2500, 2, 2, "odd"), (3333, 3330, 2, 2, "odd"), (50000, 40000, 2, 2, "odd"), (2048, 700, 0, 0, "normal"),
+    (2049, 700, 0, 0, "normal"), (8192, 2100, 5, 64, "normal"), (8193, 2100, 5, 64, "normal"), (32768, 3000, 1, 63, "normal"),
+    (32769, 3000, 1, 63, "normal"), (32768, 32768, 0, 0, "ties"), (32768, 32767, 0, 0, "equal"), (32769, 32768, 0, 1, "equal"),
+    (3000, 2990, 2000, 980, "normal"), (3000, 2980, 2000, 980, "normal"),
 ]
 
 
@@ -121,6 +131,8 @@ def evict_weights(kind, Hkv, cap, g):
         w = torch.full((Hkv, cap), 0.25)
     elif kind == "zeros":
         w[torch.rand((Hkv, cap), generator=g) < 0.8] = 0.0
+    elif kind == "negative":
+        w = -w
     elif kind == "tiny":       # the type's least weights among zeros
         w = torch.randint(1, 60, (Hkv, cap), generator=g) * 2.0 ** -149
         w[torch.rand((Hkv, cap), generator=g) < 0.7] = 0.0
