@@ -44,6 +44,16 @@ struct Ring16 {
             dma16_s(base, off, lds + at);
         }
     }
+    // The same of KEYS rows that follow each other: offsets that are the same for every stage
+    template <bool IS_V>
+    __device__ static __forceinline__ void load_all(uint64_t base, const unsigned char *lds, int wave, int lane) {
+#pragma unroll
+        for (int x = 0; x < LOADS; ++x) {
+            const int at = (wave * LOADS + x) * 1024;
+            const int row = at / ROWB + lane / CH;
+            dma16_s(base, (uint32_t)(row * ROWB) + 16u * (uint32_t)((lane & (CH - 1)) ^ swz<IS_V>(row)), lds + at);
+        }
+    }
     // lane (i, g)'s LDS offset of chunk g of row i (swz has a row's last four bits: the same
     // 16 rows further, at + 16 ROWB); chunk 4 ks + g lies at this ^ 64 ks
     __device__ static __forceinline__ uint32_t row_at(int i, int g) { return (uint32_t)(i * ROWB + 16 * (g ^ swz<false>(i))); }

@@ -85,14 +85,19 @@ __device__ __forceinline__ void take_rows(const SharedParams &p, Rows<OP, RT> &R
     }
 }
 
+struct Nothing {
+    __device__ __forceinline__ void operator()() const {}
+};
+
 // The scores of a stage of n cached keys become weights 2^(c2 s - m).  NB: operands of
 // OP::KEYS keys in the stage.
 // The reference m need not be the maximum: it moves there when a weight exceeds what the
 // operand and the fp32 sums hold (OP::too_large, seen in the operands' bits, so that no
 // maximum is taken otherwise), and weights below it lose nothing, floating as they are.
-template <class OP, int RT, int NB>
+// among(): work that does not depend on it, to be issued among the exponentials.
+template <class OP, int RT, int NB, class AMONG>
 __device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][NB][OP::NS], typename OP::P (&w)[RT][NB], int n,
-                                             float c2, int g) {
+                                             float c2, int g, AMONG among) {
     if (n < NB * OP::KEYS) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
@@ -117,6 +122,7 @@ __device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][NB]
             }
         return OP::too_large(peak);
     };
+    among();
     if (__ballot(weights())) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
@@ -206,7 +212,7 @@ struct ByKeys {
             __builtin_amdgcn_sched_barrier(0);
             OP::load_k(k, r.k(t + STEP), OP::ROWB, i, g);
             __builtin_amdgcn_sched_barrier(0);
-            softmax_step<OP, RT, 1>(R, s, w, r.count(t), c2, g);
+            softmax_step<OP, RT, 1>(R, s, w, r.count(t), c2, g, Nothing());
             OP::template accumulate<RT>(v, w, R.o);
             __builtin_amdgcn_sched_barrier(0);
             OP::load_v(v, r.v(t + STEP), OP::ROWB, i, g);
@@ -284,49 +290,36 @@ __device__ __forceinline__ void join(const SharedParams &p, Rows<OP, RT> &R, flo
 }
 
 // ---- by rows
-// One stage from LDS
+// Scores of a stage's keys, from LDS
 template <class OP, class RG, int RT>
-__device__ __forceinline__ void row_stage(Rows<OP, RT> &R, const unsigned char *ks_, const unsigned char *vs_, uint32_t ka,
-                                          uint32_t va, int n, float c2, int g) {
-    constexpr int NB = RG::KEYS / OP::KEYS;
-    float s[RT][NB][OP::NS];
-    typename OP::P w[RT][NB];
+__device__ __forceinline__ void row_scores(const Rows<OP, RT> &R, const unsigned char *ks_, uint32_t ka, float (&s)[RT][1][OP::NS]) {
+    static_assert(RG::KEYS == OP::KEYS, "one operand's keys in a stage");
+    f32x4 a[RT][2];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        f32x4 a[RT][2];
+    for (int ks = 0; ks < OP::NK; ++ks)
 #pragma unroll
-        for (int ks = 0; ks < OP::NK; ++ks)
+        for (int h = 0; h < 2; ++h) {
+            const u32x4 k = RG::row_frag(ks_, ka, h, ks);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const u32x4 k = RG::row_frag(ks_, ka, 2 * b + h, ks);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-                    a[rt][h] = OP::mfma(k, R.q[rt].f[ks], ks ? a[rt][h] : (f32x4){0.f, 0.f, 0.f, 0.f});
-            }
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int e = 0; e < OP::NS; ++e) s[rt][b][e] = a[rt][e >> 2][e & 3];
-    }
-    softmax_step<OP, RT, NB>(R, s, w, n, c2, g);
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int t = 0; t < OP::NT; ++t) {
-            const u32x4 v = RG::col_frag(vs_ + b * OP::KEYS * OP::ROWB, va, t);
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) R.o[rt][t] = OP::mfma(v, w[rt][b].f, R.o[rt][t]);
+            for (int rt = 0; rt < RT; ++rt)
+                a[rt][h] = OP::mfma(k, R.q[rt].f[ks], ks ? a[rt][h] : (f32x4){0.f, 0.f, 0.f, 0.f});
         }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int e = 0; e < OP::NS; ++e) s[rt][0][e] = a[rt][e >> 2][e & 3];
 }
 
 // The stages of `nkeys` cached rows at kb / vb, in SLOTS slots of LDS: one is read while the
 // others are on their way.  begin() asks for the first; the caller takes its rows
 // meanwhile, and run() first waits for all of it: loads that the compiler knows of must
 // not be on their way when the loop begins, or it waits for every load in it.
-constexpr int SLOTS = 3;
+constexpr int SLOTS = 4;
 
 template <class OP, class RG, int RT>
 struct ByRows {
+    static_assert(SLOTS % 2 == 0, "two sets of scores take turns");
+    using Scores = float[RT][1][OP::NS];
     uint64_t kb, vb;
     int64_t nkeys;
     unsigned char *lds;
@@ -335,31 +328,68 @@ struct ByRows {
         const uint64_t off = (uint64_t)t * RG::KEYS * OP::ROWB;
         const int n = stage_rows<RG::KEYS>(nkeys, t);
         unsigned char *to = lds + slot * 2 * RG::HALF;
-        RG::template load<false>(kb + off, OP::ROWB, n, to, wave, lane);
-        RG::template load<true>(vb + off, OP::ROWB, n, to + RG::HALF, wave, lane);
+        if (n == RG::KEYS) {
+            RG::template load_all<false>(kb + off, to, wave, lane);
+            RG::template load_all<true>(vb + off, to + RG::HALF, wave, lane);
+        } else {
+            RG::template load<false>(kb + off, OP::ROWB, n, to, wave, lane);
+            RG::template load<true>(vb + off, OP::ROWB, n, to + RG::HALF, wave, lane);
+        }
     }
     __device__ __forceinline__ void begin(uint64_t kb_, uint64_t vb_, int64_t nkeys_, unsigned char *lds_, int wave_, int lane_) {
         kb = kb_; vb = vb_; nkeys = nkeys_; lds = lds_; wave = wave_; lane = lane_;
         nst = (int)((nkeys + RG::KEYS - 1) / RG::KEYS);
-        for (int t = 0; t < SLOTS - 1 && t < nst; ++t) load(t, t);
+#pragma unroll
+        for (int t = 0; t < SLOTS - 1; ++t)
+            if (t < nst) load(t, t);
+    }
+    // Stage t, in slot SLOT: its scores s become weights, while the matrix units make those of
+    // the next stage
+    template <int SLOT>
+    __device__ __forceinline__ void stage(Rows<OP, RT> &R, int t, Scores &s, Scores &next, float c2, uint32_t ka, uint32_t va,
+                                          int g) const {
+        // this wave's part of stage t + 1 has landed (the SLOTS - 3 behind it may be on their
+        // way); behind the barrier everybody's has, and nobody reads the slot of stage t - 1
+        // any more
+        if (t + SLOTS - 2 < nst) wait_vmcnt<(SLOTS - 3) * 2 * RG::LOADS>();
+        else wait_vmcnt<0>();
+        barrier_lds();
+        if (t + SLOTS - 1 < nst) load(t + SLOTS - 1, (SLOT + SLOTS - 1) % SLOTS);
+        const unsigned char *vs = lds + SLOT * 2 * RG::HALF + RG::HALF;
+        const unsigned char *k1 = lds + (SLOT + 1) % SLOTS * 2 * RG::HALF;      // (behind the last stage: anything, not used)
+        typename OP::P w[RT][1];
+        constexpr int NT = OP::NT;
+        u32x4 v[NT];      // half of it is asked for here, half when the weights' registers are free
+        softmax_step<OP, RT, 1>(R, s, w, stage_rows<RG::KEYS>(nkeys, t), c2, g, [&]() {
+            row_scores<OP, RG, RT>(R, k1, ka, next);
+#pragma unroll
+            for (int u = 0; u < NT / 2; ++u) v[u] = RG::col_frag(vs, va, u);
+        });
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = NT / 2; u < NT; ++u) v[u] = RG::col_frag(vs, va, u);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < OP::NT; ++u)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) R.o[rt][u] = OP::mfma(v[u], w[rt][0].f, R.o[rt][u]);
+    }
+    template <int SLOT>
+    __device__ __forceinline__ void stages(Rows<OP, RT> &R, int t, Scores &s, Scores &next, float c2, uint32_t ka, uint32_t va,
+                                           int g) const {
+        if (t >= nst) return;
+        stage<SLOT>(R, t, s, next, c2, ka, va, g);
+        if constexpr (SLOT + 1 < SLOTS) stages<SLOT + 1>(R, t + 1, next, s, c2, ka, va, g);
     }
     __device__ __forceinline__ void run(Rows<OP, RT> &R, float c2) const {
         const int i = lane & 15, g = lane >> 4;
         const uint32_t ka = RG::row_at(i, g), va = RG::col_at(i, g);
+        if (nst == 0) return;
         wait_vmcnt<0>();
-        int slot = 0;
-        for (int t = 0; t < nst; ++t) {
-            // this wave's part of stage t has landed (the SLOTS - 2 behind it may be on their
-            // way); behind the barrier everybody's has, and nobody reads the slot of stage
-            // t - 1 any more
-            if (t + SLOTS - 2 < nst) wait_vmcnt<(SLOTS - 2) * 2 * RG::LOADS>();
-            else wait_vmcnt<0>();
-            barrier_lds();
-            if (t + SLOTS - 1 < nst) load(t + SLOTS - 1, slot == 0 ? SLOTS - 1 : slot - 1);
-            const unsigned char *st = lds + slot * 2 * RG::HALF;
-            row_stage<OP, RG, RT>(R, st, st + RG::HALF, ka, va, stage_rows<RG::KEYS>(nkeys, t), c2, g);
-            slot = slot == SLOTS - 1 ? 0 : slot + 1;
-        }
+        barrier_lds();
+        Scores s, next;
+        row_scores<OP, RG, RT>(R, lds, ka, s);
+        for (int t = 0; t < nst; t += SLOTS) stages<0>(R, t, s, next, c2, ka, va, g);
     }
 };
 
@@ -565,7 +595,7 @@ __device__ __forceinline__ void new_item(const SharedParams &p, uint32_t x, int 
 
 // PW, OW: the ways of prefix and own items
 template <class OP, int PW, int OW>
-__global__ __launch_bounds__(256, OP::ELT == 2 ? 3 : 2) void shared_kernel(const SharedParams p) {
+__global__ __launch_bounds__(256, 2) void shared_kernel(const SharedParams p) {
     constexpr int LP = lds_bytes<OP, PW>(), LO = lds_bytes<OP, OW>();
     __shared__ __attribute__((aligned(1024))) unsigned char lds[LP > LO ? LP : LO];
     const int lane = threadIdx.x & 63;
