@@ -1,4 +1,4 @@
-// attn_ring.hpp -- stages of 32 or 64 K (or V, or Q) rows that the four waves of a workgroup
+// attn_ring.hpp -- stages of 32 K (or V, or Q) rows that the four waves of a workgroup
 // share in LDS, 16-bit elements.  Shared by shared.hip and weigh.hip.
 //
 // Fragments loaded straight from memory (attn_direct.hpp) take 16 rows' lines at each
@@ -17,12 +17,11 @@
 namespace kvr {
 namespace dev {
 
-// KEYS_: rows of a stage, 32 or 64
-template <class E, int D, int KEYS_ = 32>
+template <class E, int D>
 struct Ring16 {
     using OP = Op16<E, D>;
     static constexpr int ROWB = D * 2, CH = D / 8, NK = D / 32, NT = D / 16;
-    static constexpr int KEYS = KEYS_, HALF = KEYS * ROWB;      // one operand's rows of a stage
+    static constexpr int KEYS = 32, HALF = KEYS * ROWB;      // one operand's rows of a stage
     static constexpr int LOADS = HALF / 4096;                // wave-wide 1 KB loads of a wave for them
 
     template <bool IS_V>

@@ -18,8 +18,6 @@
 //             stages go through LDS once for all four (attn_ring.hpp)
 // A new item is one wave's.  Each item's partial (M, l, O) is a record of the workspace.
 // The lengths are read on the device: a captured graph serves every step of a decode.
-#include <type_traits>
-
 #include "attn_ring.hpp"
 #include "readers_internal.hpp"
 
@@ -33,7 +31,7 @@ constexpr int WAVES = 4;
 // 16-bit operations of both ways
 template <class E, int D>
 struct Op : Op16<E, D> {
-    using Ring = Ring16<E, D, 32>;
+    using Ring = Ring16<E, D>;
 };
 
 template <class OP, int RT>

@@ -479,7 +479,7 @@ __global__ __launch_bounds__(256) void weigh_sum_kernel(const WeighParams p) {
 
 template <class E, int D>
 struct Op : Op16<E, D> {
-    using Ring = Ring16<E, D, 32>;
+    using Ring = Ring16<E, D>;
 };
 
 template <class OP>
