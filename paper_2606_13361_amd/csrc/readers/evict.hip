@@ -15,9 +15,13 @@
 //   evict_kernel (up to kHeldRows rows)  one launch.  Every workgroup of a kv head holds
 //           all its keys in registers, finds T by itself, and copies its share of the
 //           kept rows: no second launch, no list in memory.
+//           8192 of 32768 rows (67 MB): 26.4 us, of which the copy is 7 and the search about
+//           14: weights 1.6, keys 1, histogram 2.6, its bin 1.3, the bin's keys 2.2 and
+//           their ranks 1.1, counts and places 2.5.  945 of 3798: 8.4 us, 512 of 1024: 6.2 us.
 //   evict_select_kernel, evict_copy_kernel (longer caches)  one workgroup per kv head
 //           reads the weights again for each histogram and writes the list of kept
-//           rows; the copy is a launch of its own.
+//           rows; the copy is a launch of its own.  8192 of 40000 rows: 34 + 13 us, of 131072:
+//           96 + 14 us.
 #include "readers_internal.hpp"
 
 namespace kvr {

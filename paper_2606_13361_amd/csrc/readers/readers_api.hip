@@ -38,7 +38,13 @@ int64_t way_rows(int way) { return way > kByRows ? 64 * (way - kByRows) : 16 * w
 // 128, 256 and 512 took 11.0, 10.6 and 14.4 us with 3774 keys and 9 readers, and a merge
 // of more records.
 constexpr int64_t kMinKeysByKeys = 128, kMinKeysByRows = 256, kMinOwnKeys = 512;
-constexpr int64_t kMaxOwnSplits = 16;
+constexpr int64_t kMaxOwnSplits = 32;      // 16000 own rows of one reader: 4, 16, 32 splits 23 (8000 rows), 15.5 and 14.7 us
+// Prefix rows x keys from which a wave (fp32: an item) takes two tiles of query rows, which
+// reads each key half as often, but leaves fewer items.  16-bit, one and two tiles: 256 rows of
+// 3774 keys 18.6 + 4.0 and 19.6 + 5.5 us (items, merge), 128 of 3774 13.7 and 15.2, 68 of 32768
+// 42.6 and 35.0, 256 of 16384 42.8 and 33.8.  fp32: 120 of 945 6.1 and 8.1, 128 of 3774 33.8
+// and 34.3, 64 of 16384 69.8 and 53.5.
+constexpr int64_t kWork2 = 3 << 19, kWork2F32 = 1 << 19;
 // A call of at most this many stages of prefix and own rows is one launch (kAlone), not the
 // items' and the merge's.  With 64 own rows, 2 readers: 8.3 us instead of 5.8 + 3.2 and the
 // gap between them at 255 keys, 10.3 instead of 5.8 + 3.1 at 512 (and one launch less to
@@ -65,8 +71,9 @@ bool plan_shared(const kvr_desc *d, int64_t L, int64_t n, int64_t S, int64_t tca
     if (s.rows > 0) {
         const int64_t rows_p = n * S * G, rows_o = S * G;
         const bool f32 = d->dtype == KVR_F32;
-        s.pw = rows_p <= 16 ? 1 : f32 ? 2 : kByRows + (rows_p <= 64 ? 1 : 2);
-        s.ow = rows_o <= 16 ? 1 : f32 ? 2 : kByRows + 1;
+        if (f32) s.pw = rows_p > 16 && rows_p * L > kWork2F32 ? 2 : 1;
+        else s.pw = rows_p <= 16 ? 1 : kByRows + (rows_p > 64 && rows_p * L > kWork2 ? 2 : 1);
+        s.ow = rows_o <= 16 || s.pw == 1 ? 1 : f32 ? 2 : kByRows + 1;
         s.p_tiles = ceil_div(rows_p, way_rows(s.pw));
         s.t_tiles = ceil_div(rows_o, way_rows(s.ow));
         int64_t want = 0;
@@ -99,6 +106,12 @@ bool plan_shared(const kvr_desc *d, int64_t L, int64_t n, int64_t S, int64_t tca
 }
 
 // ---- weigh
+// First pass.  16-bit, direct and by rows: 16 query rows of a kv head over 16384 keys 9.9 and
+// 10.6 us, over 3774 4.3 and 5.2, 20 rows 13.2 and 10.8.  By rows, two and four tiles a wave:
+// 512 rows of 16384 keys 28.6 and 25.9, 256 of 16384 16.9 and 17.1, 512 of 3774 11.4 and 12.7.
+// fp32, one and two tiles: 16 rows of 4096 keys 6.6 and 7.9, 32 of 4096 10.8 and 9.0, 96 of
+// 16384 66 and 50.
+constexpr int64_t kStages4 = 256;
 constexpr int64_t kJoinAlone = 1024;   // splits x rows of a kv head from which they are joined once for all
 
 struct WeighPlan {
@@ -115,9 +128,10 @@ bool plan_weigh(const kvr_desc *d, int64_t L, int64_t S, WeighPlan *out) {
     if (L > kMaxRows || S > kMaxRows / G || L + S > kMaxRows) return false;
     if (S > 0) {
         const int64_t rows = S * G;
-        w.way = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 || d->dtype == KVR_F32 ? 4 : kByRows + (rows <= 128 ? 2 : 4);
-        const int64_t base = ceil_div(rows, way_rows(w.way)) * d->n_kv_heads;
         const int64_t stages = ceil_div(L, stage_keys(d)) + ceil_div(S, stage_keys(d));
+        const bool f32 = d->dtype == KVR_F32;
+        w.way = rows <= 16 ? 1 : f32 ? 2 : kByRows + (rows > 256 && stages > kStages4 ? 4 : 2);
+        const int64_t base = ceil_div(rows, way_rows(w.way)) * d->n_kv_heads;
         int64_t want = ceil_div(2 * kCus, base);
         const int64_t most = ceil_div(stages, kWaves);
         if (want > most) want = most;
@@ -125,8 +139,10 @@ bool plan_weigh(const kvr_desc *d, int64_t L, int64_t S, WeighPlan *out) {
         w.chunk = ceil_div(ceil_div(stages, want), step) * step;
         w.nsplit = ceil_div(stages, w.chunk);
         w.grid = base * w.nsplit;
-        // second pass: keys held in registers serve every row, as long as the workgroups fill the part
-        w.held = d->dtype == KVR_F32 && ceil_div(stages, kWaves * 2) * d->n_kv_heads >= 2 * kCus ? 2 : 1;
+        // second pass in fp32: two stages held halve the reads of the query rows, as long as
+        // the workgroups fill the part.  One and two: 24 rows of 16384 keys 69 and 49 us, of
+        // 4096 23.8 and 21.1, of 1000 9.2 and 12.0.
+        w.held = f32 && ceil_div(stages, kWaves * 2) * d->n_kv_heads >= kCus ? 2 : 1;
         if (w.grid > kMaxGrid || ceil_div(stages, kWaves) * d->n_kv_heads > kMaxGrid) return false;
         w.join = w.nsplit * rows > kJoinAlone;
         w.norm_at = want * d->n_kv_heads * rows * 2 * (int64_t)sizeof(float);

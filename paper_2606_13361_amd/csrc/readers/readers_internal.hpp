@@ -50,9 +50,9 @@ struct WeighParams {
     int32_t nsplit, chunk;   // key splits of the first pass, of `chunk` stages each
     float scale_log2;
 };
-// way of the first pass: 1, 2, 4: the four waves share that many 16-row tiles and split the
-// keys; kByRows + 2, + 4: each wave has that many of its own (16-bit only).  held: key stages
-// that a wave of the second pass holds, 1 or 2
+// way of the first pass: 1, 2: the four waves share that many 16-row tiles and split the keys
+// (2: fp32 only); kByRows + 2, + 4: each wave has that many of its own (16-bit only).  held: key
+// stages that a wave of the second pass holds, 1 or 2 (fp32 only)
 hipError_t launch_weigh(const WeighParams &p, int head_dim, int dtype, int way, int held, hipStream_t s);
 
 // The cache of the rows with the most weight (evict.hip)

@@ -87,8 +87,9 @@ hipError_t launch_weigh(const WeighParams &p, int, int dtype, int way, int held,
     if ((size_t)p.nsplit * p.n_kv_heads * rows * 8 > g_ws_given) BAD("weigh workspace");
     const int64_t per = way > kByRows ? 64 * (way - kByRows) : 16 * way;
     if ((rows + per - 1) / per * p.nsplit * p.n_kv_heads > 0x7fffffff) BAD("weigh grid");
-    const bool direct = way == 1 || way == 2 || way == 4, ring = dtype != KVR_F32 && (way == kByRows + 2 || way == kByRows + 4);
-    if ((!direct && !ring) || (held != 1 && held != 2)) BAD("weigh way %d %d", way, held);
+    const bool f32 = dtype == KVR_F32;
+    const bool direct = way == 1 || (f32 && way == 2), ring = !f32 && (way == kByRows + 2 || way == kByRows + 4);
+    if ((!direct && !ring) || (held != 1 && (held != 2 || !f32))) BAD("weigh way %d %d", way, held);
     return hipErrorUnknown;
 }
 hipError_t launch_evict(const EvictParams &p, hipStream_t) {

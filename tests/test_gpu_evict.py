@@ -54,7 +54,7 @@ WEIGH = [
     (BF16, (8, 8, 128), 16, 300), (BF16, (8, 8, 128), 17, 300), (F16, (8, 8, 64), 32, 300), (F16, (8, 8, 64), 33, 300),
     (BF16, (8, 8, 64), 64, 200), (BF16, (8, 8, 64), 65, 200), (BF16, (4, 4, 128), 128, 777), (BF16, (4, 4, 128), 129, 777),
     (F16, (2, 2, 64), 1024, 100), (F16, (2, 2, 64), 1025, 100), (F32, (2, 2, 64), 1025, 20), (BF16, (1, 1, 64), 300, 5000),
-    (F32, (64, 64, 64), 2, 1100), (F32, (64, 64, 64), 2, 900), (BF16, (4096, 4096, 64), 1, 40), (BF16, (4096, 1, 64), 2, 40),
+    (BF16, (2, 1, 128), 129, 8200), (F16, (4, 1, 64), 70, 8300), (F32, (64, 64, 64), 2, 1100), (F32, (64, 64, 64), 2, 900), (BF16, (4096, 4096, 64), 1, 40), (BF16, (4096, 1, 64), 2, 40),
 ]
 
 

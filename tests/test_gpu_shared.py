@@ -147,6 +147,12 @@ PARITY = [
     (BF16, Q, 4, 1, 700, [1, 2, 3, 4], 30), (BF16, Q, 16, 1, 700, list(range(16)), 30), (BF16, Q, 17, 1, 700, list(range(17)), 30),
     (BF16, Q, 32, 1, 700, list(range(32)), 40), (BF16, Q, 33, 1, 700, list(range(33)), 40),
     (F32, (8, 8, 64), 16, 1, 300, list(range(16)), 30), (F32, (8, 8, 64), 33, 1, 300, list(range(33)), 40),
+    # as many rows and keys as two row tiles at a time need: 16-bit, own rows by keys and by rows; fp32
+    (BF16, (4, 1, 128), 64, 1, 6300, list(range(64)), 70), (BF16, (4, 1, 128), 32, 1, 12321, [7] * 32, 9),
+    (BF16, (4, 1, 128), 33, 1, 12000, [7] * 33, 9), (F16, (4, 1, 64), 40, 1, 9999, list(range(40)), 50),
+    (BF16, (4, 1, 128), 9, 8, 5600, [0, 1, 600, 31, 32, 33, -1, 64, 100], 700),
+    (F32, (8, 1, 64), 16, 2, 2100, list(range(16)), 20), (F32, (8, 1, 64), 11, 3, 2000, [5 * i for i in range(11)], 60),
+    (F32, (4, 1, 128), 35, 1, 3800, [3] * 35, 9),
     (BF16, (4096, 4096, 64), 1, 1, 5, [3], 8), (F16, (4096, 1, 64), 1, 1, 5, [3], 8),      # the most heads
 ]
 
