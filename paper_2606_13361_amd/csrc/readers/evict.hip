@@ -182,7 +182,10 @@ __device__ __forceinline__ uint32_t find(Search<BITS> &s, uint32_t pick, uint32_
         return T;
     }
     each([&](uint32_t k) {
-        if (k >> TOP == T >> TOP && k != kZero) s.few[atomicAdd(&s.n_few, 1u)] = k;      // (the least weights share zero's bin)
+        if (k >> TOP == T >> TOP && k != kZero) {      // (the least weights share zero's bin)
+            const uint32_t at = atomicAdd(&s.n_few, 1u);
+            if (at < kFew) s.few[at] = k;      // always, unless the weights change during the call
+        }
     });
     __syncthreads();
     // the keys above a key (low half) and equal to it (high half), by four threads
@@ -408,7 +411,7 @@ __global__ __launch_bounds__(256) void evict_copy_kernel(const EvictParams p) {
         const int64_t r = x >> p.chunk_bits;
         const int hd = (int)(r / p.n_keep);
         const int64_t to = r - (int64_t)hd * p.n_keep;
-        const int32_t from = p.list[r];
+        const int32_t from = (int32_t)min((uint32_t)p.list[r], (uint32_t)p.L - 1);      // (also if the weights change during the call)
         const int64_t src = (((int64_t)hd * p.cap + from) << p.chunk_bits) + c;
         const int64_t dst = (((int64_t)hd * p.cap_out + to) << p.chunk_bits) + c;
         const u32x4 k = ((const u32x4 *)p.kc)[src], v = ((const u32x4 *)p.vc)[src];
