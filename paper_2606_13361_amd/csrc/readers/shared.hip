@@ -503,6 +503,14 @@ __device__ __forceinline__ void own_item(const SharedParams &p, uint32_t x, unsi
     const int chunk = ((it.len + p.nt - 1) / p.nt + KEYS - 1) / KEYS * KEYS;
     const int64_t kb = min((int64_t)split * chunk, (int64_t)it.len);
     it.nkeys = min((int64_t)chunk, it.len - kb);
+    if (it.nkeys == 0) {      // its rows' sums alone: the merge takes no output from a record with none
+        const int r = tile * rows_of(WAY) + (int)threadIdx.x;
+        if (threadIdx.x < rows_of(WAY) && r < p.S * p.group) {
+            const int tk = r / p.group, at = (rd * p.S + tk) * p.n_q_heads + it.hd * p.group + (r - tk * p.group);
+            *record_ml<OP>(p, p.np + split, at) = make_float2(-1e30f, 0.f);
+        }
+        return;
+    }
     const uint64_t off = (((uint64_t)rd * p.n_kv_heads + it.hd) * p.tcap + kb) * OP::ROWB;
     it.k = (uint64_t)(uintptr_t)p.kt + off;
     it.v = (uint64_t)(uintptr_t)p.vt + off;
@@ -705,6 +713,9 @@ __global__ __launch_bounds__(64 * MERGE_WAVES) void shared_merge_kernel(const Sh
                 w[s] = *(const float2 *)(ml + r * p.rows * 2);
             }
         }
+#pragma unroll
+        for (int s = 0; s < BATCH; ++s)
+            if (w[s].y == 0.f) x[s] = (f32x4){0.f, 0.f, 0.f, 0.f};      // no keys: what is there is no output
         float mx = M;
 #pragma unroll
         for (int s = 0; s < BATCH; ++s) mx = fmaxf(mx, w[s].x);
