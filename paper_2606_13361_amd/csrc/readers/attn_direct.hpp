@@ -205,24 +205,24 @@ struct Op16 {
     }
     // o[rt][t] += V^T P^T of every tile
     template <int RT>
-    __device__ static __forceinline__ void accumulate(const V &v, const P (&w)[RT][1], f32x4 (&o)[RT][NT]) {
+    __device__ static __forceinline__ void accumulate(const V &v, const P (&w)[RT], f32x4 (&o)[RT][NT]) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const u32x4 a = column(v, t);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) o[rt][t] = mfma(a, w[rt][0].f, o[rt][t]);
+            for (int rt = 0; rt < RT; ++rt) o[rt][t] = mfma(a, w[rt].f, o[rt][t]);
         }
     }
     // the same of key c alone (zeros in the place of the others), for the rows that see it
     template <int RT>
-    __device__ static __forceinline__ void accumulate_key(const V &v, const P (&w)[RT][1], f32x4 (&o)[RT][NT], int c,
+    __device__ static __forceinline__ void accumulate_key(const V &v, const P (&w)[RT], f32x4 (&o)[RT][NT], int c,
                                                           const bool (&sees)[RT], int g) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const u32x4 a = only_key(column(v, t), c, g);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                const f32x4 x = mfma(a, w[rt][0].f, o[rt][t]);
+                const f32x4 x = mfma(a, w[rt].f, o[rt][t]);
                 o[rt][t] = sees[rt] ? x : o[rt][t];
             }
         }
@@ -350,7 +350,7 @@ struct Op32 {
         return ok;
     }
     template <int RT>
-    __device__ static __forceinline__ void accumulate_key(const V &v, const P (&w)[RT][1], f32x4 (&o)[RT][NT], int c,
+    __device__ static __forceinline__ void accumulate_key(const V &v, const P (&w)[RT], f32x4 (&o)[RT][NT], int c,
                                                           const bool (&sees)[RT], int g) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -359,19 +359,19 @@ struct Op32 {
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     const float a = key_of(e, g) == c ? v.r[e][t / 4][t % 4] : 0.f;
-                    const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x4f32(a, w[rt][0].f[e], o[rt][t], 0, 0, 0);
+                    const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x4f32(a, w[rt].f[e], o[rt][t], 0, 0, 0);
                     o[rt][t] = sees[rt] ? x : o[rt][t];
                 }
     }
     template <int RT>
-    __device__ static __forceinline__ void accumulate(const V &v, const P (&w)[RT][1], f32x4 (&o)[RT][NT]) {
+    __device__ static __forceinline__ void accumulate(const V &v, const P (&w)[RT], f32x4 (&o)[RT][NT]) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
-                    o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.r[e][t / 4][t % 4], w[rt][0].f[e], o[rt][t], 0, 0, 0);
+                    o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.r[e][t / 4][t % 4], w[rt].f[e], o[rt][t], 0, 0, 0);
     }
     __device__ static __forceinline__ void put4(void *row, int d, float a, float b, float c, float e) {
         *(f32x4 *)((float *)row + d) = (f32x4){a, b, c, e};

@@ -102,48 +102,40 @@ struct Nothing {
     __device__ __forceinline__ void operator()() const {}
 };
 
-// The scores of a stage of n cached keys become weights 2^(c2 s - m).  NB: operands of
-// OP::KEYS keys in the stage.
+// The scores of a stage of n cached keys become weights 2^(c2 s - m).
 // The reference m need not be the maximum: it moves there when a weight exceeds what the
 // operand and the fp32 sums hold (OP::too_large, seen in the operands' bits, so that no
 // maximum is taken otherwise), and weights below it lose nothing, floating as they are.
 // among(): work that does not depend on it, to be issued among the exponentials.
-template <class OP, int RT, int NB, class AMONG>
-__device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][NB][OP::NS], typename OP::P (&w)[RT][NB], int n,
+template <class OP, int RT, class AMONG>
+__device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][OP::NS], typename OP::P (&w)[RT], int n,
                                              float c2, int g, AMONG among) {
-    if (n < NB * OP::KEYS) {
+    if (n < OP::KEYS) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int e = 0; e < OP::NS; ++e)
-                    if (b * OP::KEYS + OP::key_of(e, g) >= n) s[rt][b][e] = -INFINITY;
+            for (int e = 0; e < OP::NS; ++e)
+                if (OP::key_of(e, g) >= n) s[rt][e] = -INFINITY;
     }
     auto weights = [&]() {
         typename OP::Peak peak = OP::no_peak();
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
+        for (int rt = 0; rt < RT; ++rt) {
+            float p[OP::NS];
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                float p[OP::NS];
-#pragma unroll
-                for (int e = 0; e < OP::NS; ++e)
-                    p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][b][e], c2, -R.m[rt]));
-                OP::weights(w[rt][b], p);
-                OP::raise(peak, w[rt][b]);
-            }
+            for (int e = 0; e < OP::NS; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][e], c2, -R.m[rt]));
+            OP::weights(w[rt], p);
+            OP::raise(peak, w[rt]);
+        }
         return OP::too_large(peak);
     };
     among();
     if (__ballot(weights())) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            float mx = s[rt][0][0];
+            float mx = s[rt][0];
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int e = 0; e < OP::NS; ++e) mx = fmaxf(mx, s[rt][b][e]);
+            for (int e = 0; e < OP::NS; ++e) mx = fmaxf(mx, s[rt][e]);
             mx = quad_max(mx) * c2;
             const float mn = mx > R.m[rt] + OP::kMost ? mx : R.m[rt];      // each row for itself
             const float alpha = __builtin_amdgcn_exp2f(R.m[rt] - mn);
@@ -155,9 +147,7 @@ __device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][NB]
         weights();
     }
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int b = 0; b < NB; ++b) OP::add(R.l[rt], w[rt][b]);
+    for (int rt = 0; rt < RT; ++rt) OP::add(R.l[rt], w[rt]);
 }
 
 // Where row `at` of record `rec` keeps O, and (M, l)
@@ -218,14 +208,14 @@ struct ByKeys {
     __device__ __forceinline__ void run(const RANGE &r, int first, Rows<OP, RT> &R, float c2, int i, int g) {
         const int nst = r.stages();
         for (int t = first; t < nst; t += STEP) {
-            float s[RT][1][OP::NS];
-            typename OP::P w[RT][1];
+            float s[RT][OP::NS];
+            typename OP::P w[RT];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) OP::scores(k, R.q[rt], s[rt][0]);
+            for (int rt = 0; rt < RT; ++rt) OP::scores(k, R.q[rt], s[rt]);
             __builtin_amdgcn_sched_barrier(0);
             OP::load_k(k, r.k(t + STEP), OP::ROWB, i, g);
             __builtin_amdgcn_sched_barrier(0);
-            softmax_step<OP, RT, 1>(R, s, w, r.count(t), c2, g, Nothing());
+            softmax_step<OP, RT>(R, s, w, r.count(t), c2, g, Nothing());
             OP::template accumulate<RT>(v, w, R.o);
             __builtin_amdgcn_sched_barrier(0);
             OP::load_v(v, r.v(t + STEP), OP::ROWB, i, g);
@@ -305,7 +295,7 @@ __device__ __forceinline__ void join(const SharedParams &p, Rows<OP, RT> &R, flo
 // ---- by rows
 // Scores of a stage's keys, from LDS
 template <class OP, class RG, int RT>
-__device__ __forceinline__ void row_scores(const Rows<OP, RT> &R, const unsigned char *ks_, uint32_t ka, float (&s)[RT][1][OP::NS]) {
+__device__ __forceinline__ void row_scores(const Rows<OP, RT> &R, const unsigned char *ks_, uint32_t ka, float (&s)[RT][OP::NS]) {
     static_assert(RG::KEYS == OP::KEYS, "one operand's keys in a stage");
     f32x4 a[RT][2];
 #pragma unroll
@@ -320,19 +310,20 @@ __device__ __forceinline__ void row_scores(const Rows<OP, RT> &R, const unsigned
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int e = 0; e < OP::NS; ++e) s[rt][0][e] = a[rt][e >> 2][e & 3];
+        for (int e = 0; e < OP::NS; ++e) s[rt][e] = a[rt][e >> 2][e & 3];
 }
 
 // The stages of `nkeys` cached rows at kb / vb, in SLOTS slots of LDS: the next stage's keys
-// and one's values are read while the others are on their way.  begin() asks for the first; the caller takes its rows
-// meanwhile, and run() first waits for all of it: loads that the compiler knows of must
-// not be on their way when the loop begins, or it waits for every load in it.
+// and one's values are read while the others are on their way.  begin() asks for the
+// first; the caller takes its rows meanwhile, and run() first waits for all of it: loads
+// that the compiler knows of must not be on their way when the loop begins, or it waits
+// for every load in it.
 constexpr int SLOTS = 4;
 
 template <class OP, class RG, int RT>
 struct ByRows {
     static_assert(SLOTS % 2 == 0, "two sets of scores take turns");
-    using Scores = float[RT][1][OP::NS];
+    using Scores = float[RT][OP::NS];
     uint64_t kb, vb;
     int64_t nkeys;
     unsigned char *lds;
@@ -371,10 +362,10 @@ struct ByRows {
         if (t + SLOTS - 1 < nst) load(t + SLOTS - 1, (SLOT + SLOTS - 1) % SLOTS);
         const unsigned char *vs = lds + SLOT * 2 * RG::HALF + RG::HALF;
         const unsigned char *k1 = lds + (SLOT + 1) % SLOTS * 2 * RG::HALF;      // (behind the last stage: anything, not used)
-        typename OP::P w[RT][1];
+        typename OP::P w[RT];
         constexpr int NT = OP::NT;
         u32x4 v[NT];      // half of it is asked for here, half when the weights' registers are free
-        softmax_step<OP, RT, 1>(R, s, w, stage_rows<RG::KEYS>(nkeys, t), c2, g, [&]() {
+        softmax_step<OP, RT>(R, s, w, stage_rows<RG::KEYS>(nkeys, t), c2, g, [&]() {
             row_scores<OP, RG, RT>(R, k1, ka, next);
 #pragma unroll
             for (int u = 0; u < NT / 2; ++u) v[u] = RG::col_frag(vs, va, u);
@@ -386,7 +377,7 @@ struct ByRows {
 #pragma unroll
         for (int u = 0; u < OP::NT; ++u)
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) R.o[rt][u] = OP::mfma(v[u], w[rt][0].f, R.o[rt][u]);
+            for (int rt = 0; rt < RT; ++rt) R.o[rt][u] = OP::mfma(v[u], w[rt].f, R.o[rt][u]);
     }
     template <int SLOT>
     __device__ __forceinline__ void stages(Rows<OP, RT> &R, int t, Scores &s, Scores &next, float c2, uint32_t ka, uint32_t va,
@@ -500,7 +491,7 @@ __device__ __forceinline__ void own_item(const SharedParams &p, uint32_t x, unsi
     if (split >= p.nt) return;
     it.len = reader_len(p, rd);
     if (it.len < 0) return;
-    const int chunk = ((it.len + p.nt - 1) / p.nt + KEYS - 1) / KEYS * KEYS;
+    const uint32_t chunk = (((uint32_t)it.len + p.nt - 1) / p.nt + KEYS - 1) / KEYS * KEYS;
     const int64_t kb = min((int64_t)split * chunk, (int64_t)it.len);
     it.nkeys = min((int64_t)chunk, it.len - kb);
     if (it.nkeys == 0) {      // its rows' sums alone: the merge takes no output from a record with none
@@ -555,7 +546,7 @@ __device__ __forceinline__ void attend_new(const SharedParams &p, int rd, int hd
                                   (unsigned char *)p.vt + to + (uint64_t)c0 * OP::ROWB, n, i, g);
         __builtin_amdgcn_sched_barrier(0);
         float s[OP::NS];
-        typename OP::P w[1][1];
+        typename OP::P w[1];
         OP::scores(k, R.q[0], s);
         const int lim = min(n - 1, R.tok[0] - c0);
         float mx = -INFINITY;
@@ -574,8 +565,8 @@ __device__ __forceinline__ void attend_new(const SharedParams &p, int rd, int hd
         R.m[0] = mn;
 #pragma unroll
         for (int e = 0; e < OP::NS; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], p.scale_log2, -mn));
-        OP::weights(w[0][0], s);
-        OP::add(R.l[0], w[0][0]);
+        OP::weights(w[0], s);
+        OP::add(R.l[0], w[0]);
         // A value that is no number must not reach the rows before it, whose weight for it is
         // 0: a stage that has one goes key by key, each for the rows that see it.
         if (__ballot(!OP::finite(v)) == 0) {
