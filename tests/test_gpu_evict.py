@@ -226,6 +226,43 @@ def test_weigh_and_evict_in_a_graph():
             assert torch.equal(x.nan_to_num(), y.nan_to_num()), i
 
 
+def test_two_streams_at_once():
+    """Weighing and eviction of two caches on two streams, a workspace each: the bits of one after the other."""
+    S, L, keep = 40, 5000, 1200
+    sets = []
+    for seed in (1, 2):
+        q, k, kc, w, desc = weigh_case(BF16, Q, S, L, seed=seed)
+        kc = kc.nan_to_num().to(DEV)
+        sets.append(dict(desc=desc, q=q.to(DEV), k=k.to(DEV), kc=kc, vc=kc.flip(1).contiguous(), w=w.to(DEV),
+                         ws=kvr.workspace_for_weigh(desc, L, S), ko=torch.zeros((8, keep, 128), dtype=BF16, device=DEV),
+                         vo=torch.zeros((8, keep, 128), dtype=BF16, device=DEV),
+                         ix=torch.zeros((8, keep), dtype=torch.int32, device=DEV)))
+
+    def step(a, stream=None):
+        kvr.kvr_cache_weigh(a["desc"], a["q"], a["k"], a["kc"], L, S, a["w"], a["ws"], stream=stream)
+        kvr.kvr_cache_evict(a["desc"], a["kc"], a["vc"], L + S, a["w"], keep, a["ko"], a["vo"], n_last=S, index=a["ix"],
+                            stream=stream)
+
+    start = [a["w"].clone() for a in sets]
+    for a in sets:
+        for _ in range(3):
+            step(a)
+    want = [{x: a[x].clone() for x in ("w", "ko", "vo", "ix")} for a in sets]
+    for a, w in zip(sets, start):
+        a["w"].copy_(w)
+        for x in ("ko", "vo", "ix"):
+            a[x].zero_()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        for a, s in zip(sets, streams):
+            step(a, s)
+    torch.cuda.synchronize()
+    for a, w in zip(sets, want):
+        for x in w:
+            assert torch.equal(a[x], w[x]), x
+
+
 @pytest.mark.parametrize("dt", [BF16, F16, F32], ids=str)
 def test_a_document_weighed_evicted_and_read_by_many(dt):
     """Prefill with the rotary embedding, weights of its last tokens, a third of the rows
