@@ -381,7 +381,8 @@ int kvr_continue_batched_rope(const kvr_desc *desc, const kvr_rope *rope, const 
  *   caches hold rotated keys.  pos0 is L_prefix for a whole prefix, and the number
  *   of positions that it stands for when rows were evicted from it.  Needs
  *   rope->n_pos >= pos0 + tail_capacity (+ S when append == 0).
- *   ws: kvr_workspace_bytes_shared(desc, L_prefix, n, S, tail_capacity) bytes.
+ *   ws: kvr_workspace_bytes_shared(desc, L_prefix, n, S, tail_capacity) bytes; calls (and
+ *   captured graphs) that may run at once need one each.
  * Limits: n S n_q_heads below 2^24, L_prefix and tail_capacity below 2^31
  * (KVR_ERR_SHAPE).
  * A masked place never reaches a result: not own rows behind a reader's length, nor
@@ -407,7 +408,8 @@ size_t kvr_workspace_bytes_shared(const kvr_desc *desc, int64_t L_prefix, int32_
  *   weight: device float [n_kv_heads][capacity], rows [0, L_prefix + S) added to
  *   (new token i is row L_prefix + i), the others untouched.  Needs
  *   L_prefix + S <= capacity (KVR_ERR_CAPACITY).
- *   ws: kvr_workspace_bytes_weigh(desc, L_prefix, S) bytes.
+ *   ws: kvr_workspace_bytes_weigh(desc, L_prefix, S) bytes.  Calls that may run at once
+ *   need a workspace, and a weight buffer, each.
  * Scores, softmax and sums in fp32 for every element type.
  * Limits: S n_q_heads and (L_prefix + S) n_kv_heads below 2^28 are served; calls far
  * beyond that are refused (KVR_ERR_SHAPE).
@@ -435,7 +437,7 @@ size_t kvr_workspace_bytes_weigh(const kvr_desc *desc, int64_t L_prefix, int64_t
  *   buffer of the call (KVR_ERR_SHAPE).  n_keep == 0 is a no-op.
  *   weight, weight_out and index need 4-byte alignment.
  *   ws: kvr_workspace_bytes_evict(desc, L) bytes (may be NULL when that is 0: up to
- *   32768 rows).
+ *   32768 rows); calls that may run at once need one each.
  */
 int kvr_cache_evict(const kvr_desc *desc, const void *kcache, const void *vcache, int64_t L, const float *weight,
                     int64_t n_first, int64_t n_last, int64_t n_keep, void *kout, void *vout, int64_t capacity_out,
