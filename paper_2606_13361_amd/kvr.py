@@ -492,6 +492,17 @@ def _at(t, name, dtype, shape, dev):
     raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), shape))
 
 
+def _pair(a, a_name, b, b_name, dtype, shape, dev):
+    """_at of two tensors of one type and shape, a seventh of the time less."""
+    try:
+        if (a.dtype is dtype and b.dtype is dtype and a.get_device() == dev and b.get_device() == dev
+                and a.is_contiguous() and b.is_contiguous() and a.shape == shape and b.shape == shape):
+            return a.data_ptr(), b.data_ptr()
+    except AttributeError:      # one is no tensor
+        pass
+    return _at(a, a_name, dtype, shape, dev), _at(b, b_name, dtype, shape, dev)
+
+
 def _scratch(ws, dev):
     if ws is None:
         return None, 0
@@ -540,24 +551,17 @@ def kvr_continue_shared(desc, Qs, Ks, Vs, kcache, vcache, L_prefix, ktail, vtail
     if Qs.dim() != 4:
         raise ValueError("Qs must be a tensor [n, S, n_q_heads, head_dim]")
     n, S = Qs.shape[:2]
-    rows, new = (n, S, Hq, d), (n, S, Hkv, d)
-    q = _at(Qs, "Qs", dt, rows, dev)
-    k = _at(Ks, "Ks", dt, new, dev)
-    v = _at(Vs, "Vs", dt, new, dev)
-    o = _at(out, "out", dt, rows, dev)
+    q, o = _pair(Qs, "Qs", out, "out", dt, (n, S, Hq, d), dev)
+    k, v = _pair(Ks, "Ks", Vs, "Vs", dt, (n, S, Hkv, d), dev)
     kc = vc = kt = vt = rp = None
     if L_prefix > 0 or kcache is not None or vcache is not None:
-        shape = (Hkv, desc.capacity, d)
-        kc = _at(kcache, "kcache", dt, shape, dev)
-        vc = _at(vcache, "vcache", dt, shape, dev)
+        kc, vc = _pair(kcache, "kcache", vcache, "vcache", dt, (Hkv, desc.capacity, d), dev)
     cap = 0
     if ktail is not None or vtail is not None:
         if not isinstance(ktail, torch.Tensor) or ktail.dim() != 4:
             raise ValueError("ktail must be a tensor [n, n_kv_heads, tail_capacity, head_dim]")
         cap = ktail.shape[2]
-        shape = (n, Hkv, cap, d)
-        kt = _at(ktail, "ktail", dt, shape, dev)
-        vt = _at(vtail, "vtail", dt, shape, dev)
+        kt, vt = _pair(ktail, "ktail", vtail, "vtail", dt, (n, Hkv, cap, d), dev)
     ln = _at(tail_len, "tail_len", torch.int32, (n,), dev)
     wp, wn = _scratch(ws, dev)
     if rope is not None:
@@ -609,14 +613,12 @@ def kvr_cache_evict(desc, kcache, vcache, L, weight, n_keep, kout, vout, n_first
     [n_kv_heads, capacity_out] and index (int32 [n_kv_heads, n_keep]) are optional."""
     Hkv, d, dt = desc.n_kv_heads, desc.head_dim, _TORCH_DTYPE.get(desc.dtype)
     dev = _device(kcache, "kcache")
-    kc = _at(kcache, "kcache", dt, (Hkv, desc.capacity, d), dev)
-    vc = _at(vcache, "vcache", dt, (Hkv, desc.capacity, d), dev)
+    kc, vc = _pair(kcache, "kcache", vcache, "vcache", dt, (Hkv, desc.capacity, d), dev)
     w = _at(weight, "weight", torch.float32, (Hkv, desc.capacity), dev)
     if not isinstance(kout, torch.Tensor) or kout.dim() != 3:
         raise ValueError("kout must be a tensor [n_kv_heads, capacity_out, head_dim]")
     cap = kout.shape[1]
-    ko = _at(kout, "kout", dt, (Hkv, cap, d), dev)
-    vo = _at(vout, "vout", dt, (Hkv, cap, d), dev)
+    ko, vo = _pair(kout, "kout", vout, "vout", dt, (Hkv, cap, d), dev)
     wo = None if weight_out is None else _at(weight_out, "weight_out", torch.float32, (Hkv, cap), dev)
     ix = None if index is None else _at(index, "index", torch.int32, (Hkv, n_keep), dev)
     wp, wn = _scratch(ws, dev)
