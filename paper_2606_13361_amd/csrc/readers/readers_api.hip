@@ -32,7 +32,9 @@ int64_t stage_keys(const kvr_desc *d) { return d->dtype == KVR_F32 ? 16 : 32; }
 int64_t way_rows(int way) { return way > kByRows ? 64 * (way - kByRows) : 16 * way; }
 
 // ---- shared
-// Workgroups are as many as there are compute units, as long as each keeps this many keys.
+// Workgroups are as many as there are compute units (256 and 512, items and merge: 2 readers
+// of 32768 keys 27.3 + 4.0 and 27.1 + 5.4 us, 9 of 32768 30.4 + 4.8 and 34.9 + 5.6, 8 readers'
+// 8000 own rows 48.4 + 4.9 and 47.8 + 4.8), as long as each keeps this many keys.
 // Prefix by keys: one stage for each wave; 128 and 256 measured 5.9 and 6.8 us with 255 keys
 // and 2 readers, 9.0 and 11.0 us with 945 keys and 3 readers in fp32.  By rows it is 256:
 // 128, 256 and 512 took 11.0, 10.6 and 14.4 us with 3774 keys and 9 readers, and a merge
@@ -112,6 +114,7 @@ bool plan_shared(const kvr_desc *d, int64_t L, int64_t n, int64_t S, int64_t tca
 // fp32, one and two tiles: 16 rows of 4096 keys 6.6 and 7.9, 32 of 4096 10.8 and 9.0, 96 of
 // 16384 66 and 50.
 constexpr int64_t kStages4 = 256;
+constexpr int64_t kStatsGroups = 2 * kCus;   // workgroups: 512, 768 and 1024 take 44, 48 and 47 us for 512 rows of 32640 keys
 constexpr int64_t kJoinAlone = 1024;   // splits x rows of a kv head from which they are joined once for all
 
 struct WeighPlan {
@@ -132,7 +135,7 @@ bool plan_weigh(const kvr_desc *d, int64_t L, int64_t S, WeighPlan *out) {
         const bool f32 = d->dtype == KVR_F32;
         w.way = rows <= 16 ? 1 : f32 ? 2 : kByRows + (rows > 256 && stages > kStages4 ? 4 : 2);
         const int64_t base = ceil_div(rows, way_rows(w.way)) * d->n_kv_heads;
-        int64_t want = ceil_div(2 * kCus, base);
+        int64_t want = ceil_div(kStatsGroups, base);
         const int64_t most = ceil_div(stages, kWaves);
         if (want > most) want = most;
         const int64_t step = w.way > kByRows ? 1 : kWaves;      // the waves share a stage, or take one each
