@@ -429,6 +429,8 @@ __global__ __launch_bounds__(256) void evict_copy_kernel(const EvictParams p) {
 hipError_t launch_evict(const EvictParams &p, hipStream_t s) {
     if (p.L <= kHeldRows) {
         const dim3 grid((unsigned)(p.n_kv_heads * p.parts)), block(THREADS);
+        // as few keys a thread as hold them: 1024 rows take 6.2, 7.7 and 14.6 us with 2, 8 and 32,
+        // 3798 rows 8.4 and 15.2 with 8 and 32
         if (p.L <= 2 * THREADS) hipLaunchKernelGGL((evict_kernel<2, 12>), grid, block, 0, s, p);
         else if (p.L <= 8 * THREADS) hipLaunchKernelGGL((evict_kernel<8, 12>), grid, block, 0, s, p);
         else hipLaunchKernelGGL((evict_kernel<32, 14>), grid, block, 0, s, p);

@@ -38,9 +38,11 @@ int64_t way_rows(int way) { return way > kByRows ? 64 * (way - kByRows) : 16 * w
 // Prefix by keys: one stage for each wave; 128 and 256 measured 5.9 and 6.8 us with 255 keys
 // and 2 readers, 9.0 and 11.0 us with 945 keys and 3 readers in fp32.  By rows it is 256:
 // 128, 256 and 512 took 11.0, 10.6 and 14.4 us with 3774 keys and 9 readers, and a merge
-// of more records.
+// of more records.  Own rows: 128, 256 and 512 took 11.0, 10.6 and 10.1 us with 9 readers.
 constexpr int64_t kMinKeysByKeys = 128, kMinKeysByRows = 256, kMinOwnKeys = 512;
-constexpr int64_t kMaxOwnSplits = 32;      // 16000 own rows of one reader: 4, 16, 32 splits 23 (8000 rows), 15.5 and 14.7 us
+// 2 readers of 8000 own rows: 4 and 16 splits 23.1 and 14.9 us; one of 16000: 16 and 32 splits
+// 15.5 and 14.7
+constexpr int64_t kMaxOwnSplits = 32;
 // Prefix rows x keys from which a wave (fp32: an item) takes two tiles of query rows, which
 // reads each key half as often, but leaves fewer items.  16-bit, one and two tiles: 256 rows of
 // 3774 keys 18.6 + 4.0 and 19.6 + 5.5 us (items, merge), 128 of 3774 13.7 and 15.2, 68 of 32768
@@ -114,7 +116,8 @@ bool plan_shared(const kvr_desc *d, int64_t L, int64_t n, int64_t S, int64_t tca
 // fp32, one and two tiles: 16 rows of 4096 keys 6.6 and 7.9, 32 of 4096 10.8 and 9.0, 96 of
 // 16384 66 and 50.
 constexpr int64_t kStages4 = 256;
-constexpr int64_t kStatsGroups = 2 * kCus;   // workgroups: 512, 768 and 1024 take 44, 48 and 47 us for 512 rows of 32640 keys
+// Workgroups: 512, 768 and 1024 take 44, 48 and 47 us for 512 rows of 32640 keys
+constexpr int64_t kStatsGroups = 2 * kCus;
 constexpr int64_t kJoinAlone = 1024;   // splits x rows of a kv head from which they are joined once for all
 
 struct WeighPlan {
@@ -156,7 +159,9 @@ bool plan_weigh(const kvr_desc *d, int64_t L, int64_t S, WeighPlan *out) {
 }
 
 // ---- evict
-constexpr int64_t kRowsPerPart = 16;   // at least, of a workgroup that searches on its own
+// Kept rows, at least, of a workgroup that searches on its own: 512 of 1024 rows take 6.2, 6.2
+// and 6.9 us with 4, 16 and 64
+constexpr int64_t kRowsPerPart = 16;
 
 bool overlap(const void *a, size_t na, const void *b, size_t nb) {
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
