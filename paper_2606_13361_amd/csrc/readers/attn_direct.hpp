@@ -158,10 +158,12 @@ struct Op16 {
         constexpr uint32_t one = std::is_same<E, F16>::value ? 0x3c003c00u : 0x3f803f80u;
         l = mfma((u32x4){one, one, one, one}, w.f, l);
     }
-    // The largest weights, two by two: positive floats order as their bits do.  Up to 2^15 in
-    // fp16 (whose largest is just below 2^16), 2^60 in bf16: 2^31 of them, each times a value
-    // of up to 2^35, are less than the largest fp32 sum.
-    static constexpr int kMost = std::is_same<E, F16>::value ? 15 : 60;
+    // The largest weights, two by two: positive floats order as their bits do.  Up to 2^kMost:
+    // 2^15 in fp16 (whose largest is just below 2^16), 2^60 in bf16: 2^31 of them, each times a
+    // value of up to 2^35, are less than the largest fp32 sum.  Where a reference moves, the
+    // largest weight becomes 2^kLift.  fp16 has 14 exponents below 1, and below them bits go:
+    // with the largest weight at 2^12 or more, weights of 2^-26 of it keep all of theirs.
+    static constexpr int kMost = std::is_same<E, F16>::value ? 15 : 60, kLift = std::is_same<E, F16>::value ? 12 : 0;
     typedef uint16_t Peak __attribute__((ext_vector_type(2)));
     __device__ static __forceinline__ Peak no_peak() { return (Peak){0, 0}; }
     __device__ static __forceinline__ void raise(Peak &k, const P &w) {
@@ -336,7 +338,7 @@ struct Op32 {
         for (int e = 0; e < 4; ++e) w.f[e] = p[e];
     }
     __device__ static __forceinline__ void add(L &l, const P &w) { l += (w.f[0] + w.f[1]) + (w.f[2] + w.f[3]); }
-    static constexpr int kMost = 60;
+    static constexpr int kMost = 60, kLift = 0;
     using Peak = float;      // the sum: too large, or no number, if one of them is
     __device__ static __forceinline__ Peak no_peak() { return 0.f; }
     __device__ static __forceinline__ void raise(Peak &k, const P &w) { k += (w.f[0] + w.f[1]) + (w.f[2] + w.f[3]); }

@@ -103,9 +103,9 @@ struct Nothing {
 };
 
 // The scores of a stage of n cached keys become weights 2^(c2 s - m).
-// The reference m need not be the maximum: it moves there when a weight exceeds what the
+// The reference m need not follow the maximum: it moves when a weight exceeds what the
 // operand and the fp32 sums hold (OP::too_large, seen in the operands' bits, so that no
-// maximum is taken otherwise), and weights below it lose nothing, floating as they are.
+// maximum is taken otherwise), to where the largest weight is 2^kLift.
 // among(): work that does not depend on it, to be issued among the exponentials.
 template <class OP, int RT, class AMONG>
 __device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][OP::NS], typename OP::P (&w)[RT], int n,
@@ -137,7 +137,7 @@ __device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][OP:
 #pragma unroll
             for (int e = 0; e < OP::NS; ++e) mx = fmaxf(mx, s[rt][e]);
             mx = quad_max(mx) * c2;
-            const float mn = mx > R.m[rt] + OP::kMost ? mx : R.m[rt];      // each row for itself
+            const float mn = mx > R.m[rt] + OP::kMost ? mx - OP::kLift : R.m[rt];      // each row for itself
             const float alpha = __builtin_amdgcn_exp2f(R.m[rt] - mn);
             R.m[rt] = mn;
             R.l[rt] *= alpha;
@@ -555,7 +555,7 @@ __device__ __forceinline__ void attend_new(const SharedParams &p, int rd, int hd
             s[e] = OP::key_of(e, g) > lim ? -INFINITY : s[e];
             mx = fmaxf(mx, s[e]);
         }
-        const float mn = fmaxf(R.m[0], quad_max(mx) * p.scale_log2);
+        const float mn = fmaxf(R.m[0], quad_max(mx) * p.scale_log2 - OP::kLift);
         if (c0) {
             const float alpha = __builtin_amdgcn_exp2f(R.m[0] - mn);
             R.l[0] *= alpha;
