@@ -158,12 +158,15 @@ struct Op16 {
         constexpr uint32_t one = std::is_same<E, F16>::value ? 0x3c003c00u : 0x3f803f80u;
         l = mfma((u32x4){one, one, one, one}, w.f, l);
     }
-    // The largest weights, two by two: positive floats order as their bits do.  Up to 2^kMost:
-    // 2^15 in fp16 (whose largest is just below 2^16), 2^60 in bf16: 2^31 of them, each times a
-    // value of up to 2^35, are less than the largest fp32 sum.  Where a reference moves, the
-    // largest weight becomes 2^kLift.  fp16 has 14 exponents below 1, and below them bits go:
-    // with the largest weight at 2^12 or more, weights of 2^-26 of it keep all of theirs.
-    static constexpr int kMost = std::is_same<E, F16>::value ? 15 : 60, kLift = std::is_same<E, F16>::value ? 12 : 0;
+    // The largest weights, two by two: positive floats order as their bits do.  Up to 2^kMost;
+    // where a reference moves, the largest weight becomes 2^kLift.
+    //   bf16  up to 1: a sum of weights times values is never larger than the same with the
+    //         maximum as the reference.  2^-118 of the largest weight is a normal number yet.
+    //   fp16  up to 2^15 (the type's largest number is just below 2^16): 2^31 of them, each times
+    //         a value below 2^16, are far below the largest fp32 number.  There are 14 exponents
+    //         below 1, and below them bits go: with the largest weight at 2^12 or more, weights of
+    //         2^-26 of it keep all of theirs.
+    static constexpr int kMost = std::is_same<E, F16>::value ? 15 : 0, kLift = std::is_same<E, F16>::value ? 12 : -8;
     typedef uint16_t Peak __attribute__((ext_vector_type(2)));
     __device__ static __forceinline__ Peak no_peak() { return (Peak){0, 0}; }
     __device__ static __forceinline__ void raise(Peak &k, const P &w) {
@@ -338,11 +341,12 @@ struct Op32 {
         for (int e = 0; e < 4; ++e) w.f[e] = p[e];
     }
     __device__ static __forceinline__ void add(L &l, const P &w) { l += (w.f[0] + w.f[1]) + (w.f[2] + w.f[3]); }
-    static constexpr int kMost = 60, kLift = 0;
+    // as in bf16; the eight weights of two row tiles, of up to 2^kMost each, add up to 1 at most
+    static constexpr int kMost = -3, kLift = -11;
     using Peak = float;      // the sum: too large, or no number, if one of them is
     __device__ static __forceinline__ Peak no_peak() { return 0.f; }
     __device__ static __forceinline__ void raise(Peak &k, const P &w) { k += (w.f[0] + w.f[1]) + (w.f[2] + w.f[3]); }
-    __device__ static __forceinline__ bool too_large(Peak k) { return !(k <= 0x1p60f); }
+    __device__ static __forceinline__ bool too_large(Peak k) { return !(k <= 1.f); }
     __device__ static __forceinline__ bool finite(const V &v) {
         bool ok = true;
 #pragma unroll

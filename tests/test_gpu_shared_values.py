@@ -107,3 +107,18 @@ def test_weights_far_below_one_that_adds_nothing(dt, way, below):
         k, v = {"prefix": (c.kc[:, 0], c.vc[:, 0]), "own": (c.kt[:, :, 0], c.vt[:, :, 0]), "new": (c.k[:, 0], c.v[:, 0])}[place]
         k[..., 0], v[...] = below, 0.0
         c.check()
+
+
+# ------------------------------------------------------------ large values
+@pytest.mark.parametrize("dt,way", [x for x in WAYS if x[0] != F16], ids=lambda x: str(x).replace("torch.", ""))
+def test_large_values_stay_finite(dt, way):
+    """Values of 2^110 and keys that raise their weights by up to 2^55, over which a sum of weights above 1
+    times such values would pass the largest fp32 number."""
+    c = Call(dt, way, seed=1)
+    c.q[..., 0] = 1.0
+    for k in (c.kc, c.kt, c.k.transpose(1, 2)):
+        at = torch.randint(0, 40, k.shape[:-1], generator=c.g) == 0
+        k[..., 0] = torch.where(at, torch.randint(0, 56, k.shape[:-1], generator=c.g).float(), torch.zeros(()))
+    for v in (c.v, c.vc, c.vt):
+        v *= 2.0 ** 110
+    c.check()
