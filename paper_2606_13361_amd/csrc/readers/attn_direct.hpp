@@ -158,24 +158,45 @@ struct Op16 {
         constexpr uint32_t one = std::is_same<E, F16>::value ? 0x3c003c00u : 0x3f803f80u;
         l = mfma((u32x4){one, one, one, one}, w.f, l);
     }
-    // The largest weights, two by two: positive floats order as their bits do.  Up to 2^kMost;
-    // where a reference moves, the largest weight becomes 2^kLift.
-    //   bf16  up to 1: a sum of weights times values is never larger than the same with the
+    // When a row's reference moves, to where the largest weight is 2^kLift.  A weight that holds
+    // much of its row must not be rounded, or results of two orders of keys differ by it: the
+    // largest one so far is a power of two, and one that grows above it moves the reference as
+    // soon as it is more than a third of the sum so far (a quarter of both), or the operand or
+    // the sums do not hold it:
+    //   bf16  above 1: a sum of weights times values is never larger than the same with the
     //         maximum as the reference.  2^-118 of the largest weight is a normal number yet.
-    //   fp16  up to 2^15 (the type's largest number is just below 2^16): 2^31 of them, each times
-    //         a value below 2^16, are far below the largest fp32 number.  There are 14 exponents
-    //         below 1, and below them bits go: with the largest weight at 2^12 or more, weights of
-    //         2^-26 of it keep all of theirs.
-    static constexpr int kMost = std::is_same<E, F16>::value ? 15 : 0, kLift = std::is_same<E, F16>::value ? 12 : -8;
-    typedef uint16_t Peak __attribute__((ext_vector_type(2)));
-    __device__ static __forceinline__ Peak no_peak() { return (Peak){0, 0}; }
-    __device__ static __forceinline__ void raise(Peak &k, const P &w) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) k = __builtin_elementwise_max(k, __builtin_bit_cast(Peak, (uint32_t)w.f[j]));
+    //   fp16  above the type's largest number: 2^31 weights below 2^16, each times a value below
+    //         2^16, are far below the largest fp32 number.  There are 14 exponents below 1, and
+    //         below them bits go: with the largest weight at 2^12 or more, weights of 2^-26 of it
+    //         keep all of theirs.
+    static constexpr int kLift = std::is_same<E, F16>::value ? 12 : -8;
+    static constexpr float kLargest = std::is_same<E, F16>::value ? 0x1p12f : 0x1p-8f;      // 2^kLift
+    typedef uint16_t Pair __attribute__((ext_vector_type(2)));
+    // The weight that a row's must not exceed, in both halves, as the element type truncates
+    // it; positive floats order as their bits do.  (l: the row's sum)
+    using Mark = Pair;
+    __device__ static __forceinline__ Mark mark(const L &l) {
+        const float x = fmaxf(l[0] * (1.f / 3.f), kLargest);
+        if constexpr (std::is_same<E, F16>::value) return __builtin_bit_cast(Pair, __builtin_amdgcn_cvt_pkrtz(x, x));
+        const uint32_t u = __float_as_uint(fminf(x, 1.f));
+        return __builtin_bit_cast(Pair, __builtin_amdgcn_perm(u, u, 0x07060706u));
     }
-    __device__ static __forceinline__ bool too_large(Peak k) {
-        constexpr uint16_t most = std::is_same<E, F16>::value ? (15 + kMost) << 10 : (127 + kMost) << 7;
-        return k[0] > most || k[1] > most;
+    using Peak = Pair;
+    __device__ static __forceinline__ Peak peak(const P &w) {
+        Peak k = __builtin_bit_cast(Peak, (uint32_t)w.f[0]);
+#pragma unroll
+        for (int j = 1; j < 4; ++j) k = __builtin_elementwise_max(k, __builtin_bit_cast(Peak, (uint32_t)w.f[j]));
+        return k;
+    }
+    // one of the lane's weights exceeds the mark
+    __device__ static __forceinline__ bool above(Peak k, Mark t) {
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(k, t)) != 0;
+    }
+    // one of the row's does, the largest of which is top.  A row decides by its own weights and
+    // sum, and a mark made earlier is not larger, so it does not matter which of a tile's rows
+    // asked.
+    __device__ static __forceinline__ bool moves(uint64_t, int, float top, const L &l) {
+        return above(__builtin_bit_cast(Peak, E::pack2(top, top)), mark(l));
     }
     // whether every value of the stage is a number (the exponent's bits are not all set)
     __device__ static __forceinline__ bool finite(const V &v) {
@@ -341,12 +362,19 @@ struct Op32 {
         for (int e = 0; e < 4; ++e) w.f[e] = p[e];
     }
     __device__ static __forceinline__ void add(L &l, const P &w) { l += (w.f[0] + w.f[1]) + (w.f[2] + w.f[3]); }
-    // as in bf16; the eight weights of two row tiles, of up to 2^kMost each, add up to 1 at most
-    static constexpr int kMost = -3, kLift = -11;
-    using Peak = float;      // the sum: too large, or no number, if one of them is
-    __device__ static __forceinline__ Peak no_peak() { return 0.f; }
-    __device__ static __forceinline__ void raise(Peak &k, const P &w) { k += (w.f[0] + w.f[1]) + (w.f[2] + w.f[3]); }
-    __device__ static __forceinline__ bool too_large(Peak k) { return !(k <= 1.f); }
+    // As in bf16, but weights are not rounded: a row's reference moves when the four of one of
+    // its lanes add up to more than 1 (or to no number).
+    static constexpr int kLift = -10;
+    struct Mark {};
+    __device__ static __forceinline__ Mark mark(const L &) { return Mark(); }
+    using Peak = float;
+    __device__ static __forceinline__ Peak peak(const P &w) { return (w.f[0] + w.f[1]) + (w.f[2] + w.f[3]); }
+    __device__ static __forceinline__ bool above(Peak k, Mark) { return !(k <= 1.f); }
+    // lanes: those that are above
+    __device__ static __forceinline__ bool moves(uint64_t lanes, int i, float, const L &) {
+        const uint32_t x = (uint32_t)lanes | (uint32_t)(lanes >> 32);
+        return ((x | x >> 16) >> i & 1) != 0;
+    }
     __device__ static __forceinline__ bool finite(const V &v) {
         bool ok = true;
 #pragma unroll

@@ -55,6 +55,7 @@ struct Rows {
     f32x4 o[RT][OP::NT];
     float m[RT];             // reference of the row (log2 domain)
     typename OP::L l[RT];    // its sum
+    typename OP::Mark t[RT]; // what its weights must not exceed
     int tok[RT];             // the row's token, of its reader's new ones
     int at[RT];              // the row in out, -1: none
 };
@@ -93,6 +94,7 @@ __device__ __forceinline__ void take_rows(const SharedParams &p, Rows<OP, RT> &R
     for (int rt = 0; rt < RT; ++rt) {
         R.m[rt] = -1e30f;
         R.l[rt] = OP::no_sum();
+        R.t[rt] = OP::mark(R.l[rt]);
 #pragma unroll
         for (int t = 0; t < OP::NT; ++t) R.o[rt][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
@@ -103,9 +105,10 @@ struct Nothing {
 };
 
 // The scores of a stage of n cached keys become weights 2^(c2 s - m).
-// The reference m need not follow the maximum: it moves when a weight exceeds what the
-// operand and the fp32 sums hold (OP::too_large, seen in the operands' bits, so that no
-// maximum is taken otherwise), to where the largest weight is 2^kLift.
+// The reference m does not follow the maximum (attn_direct.hpp: when it moves): whether a
+// weight exceeds its row's mark is seen in the operands' bits, no maximum is taken
+// otherwise.  A row's sum grows, its mark only here, so this is entered more often
+// than a reference moves: on rows without peaks, in the first three or four stages.
 // among(): work that does not depend on it, to be issued among the exponentials.
 template <class OP, int RT, class AMONG>
 __device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][OP::NS], typename OP::P (&w)[RT], int n,
@@ -117,37 +120,42 @@ __device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][OP:
             for (int e = 0; e < OP::NS; ++e)
                 if (OP::key_of(e, g) >= n) s[rt][e] = -INFINITY;
     }
-    auto weights = [&]() {
-        typename OP::Peak peak = OP::no_peak();
+    auto weights = [&](int rt) {      // lanes with a weight above their row's mark
+        float p[OP::NS];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            float p[OP::NS];
-#pragma unroll
-            for (int e = 0; e < OP::NS; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][e], c2, -R.m[rt]));
-            OP::weights(w[rt], p);
-            OP::raise(peak, w[rt]);
-        }
-        return OP::too_large(peak);
+        for (int e = 0; e < OP::NS; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][e], c2, -R.m[rt]));
+        OP::weights(w[rt], p);
+        return __ballot(OP::above(OP::peak(w[rt]), R.t[rt]));
     };
     among();
-    if (__ballot(weights())) {
+    uint64_t above[RT], any = 0;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) any |= above[rt] = weights(rt);
+    if (any) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
+            if (!above[rt]) continue;
             float mx = s[rt][0];
 #pragma unroll
             for (int e = 0; e < OP::NS; ++e) mx = fmaxf(mx, s[rt][e]);
-            mx = quad_max(mx) * c2;
-            const float mn = mx > R.m[rt] + OP::kMost ? mx - OP::kLift : R.m[rt];      // each row for itself
+            mx = quad_max(mx);
+            const bool moves = OP::moves(above[rt], threadIdx.x & 15, __builtin_amdgcn_exp2f(__builtin_fmaf(mx, c2, -R.m[rt])), R.l[rt]);
+            if (!__ballot(moves)) continue;
+            const float mn = moves ? mx * c2 - OP::kLift : R.m[rt];      // each row for itself
             const float alpha = __builtin_amdgcn_exp2f(R.m[rt] - mn);
             R.m[rt] = mn;
             R.l[rt] *= alpha;
 #pragma unroll
             for (int t = 0; t < OP::NT; ++t) R.o[rt][t] *= alpha;
+            weights(rt);
         }
-        weights();
     }
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) OP::add(R.l[rt], w[rt]);
+    if (any) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) R.t[rt] = OP::mark(R.l[rt]);
+    }
 }
 
 // Where row `at` of record `rec` keeps O, and (M, l)

@@ -12,6 +12,7 @@ import numpy as np
 import pytest
 import torch
 
+from harness import workloads as W
 from oracle import readers as O
 from paper_2606_13361_amd import kvr
 
@@ -122,3 +123,24 @@ def test_large_values_stay_finite(dt, way):
     for v in (c.v, c.vc, c.vt):
         v *= 2.0 ** 110
     c.check()
+
+
+# ------------------------------------------------------------ the bar between two GPU results
+@pytest.mark.parametrize("kind", ["scaled", "sink", "tile_end", "rising"])
+@pytest.mark.parametrize("n", [1, 12])
+def test_peaky_rows_agree_with_a_prefill(kind, n):
+    """The rows of a prefill of prefix and new tokens, at 2e-3 and one output ulp, the bar that a
+    continuation is held to on these inputs; n readers with the same tokens (12: two row tiles a wave)."""
+    L, S, sh = 1500, 24, W.QWEN
+    q, k, v = (x.to(DEV) for x in W.stress(kind, L + S, sh, seed=3))
+    full = torch.empty_like(q)
+    desc = kvr.make_desc(sh.n_q_heads, sh.n_kv_heads, sh.head_dim, sh.dtype, L + S)
+    kc, vc = (torch.zeros((sh.n_kv_heads, L + S, sh.head_dim), dtype=sh.dtype, device=DEV) for _ in range(2))
+    kvr.kvr_prefill(desc, q, k, v, L + S, full, kc, vc)
+    new = [x[L:].expand(n, *x[L:].shape).contiguous() for x in (q, k, v)]
+    out = torch.empty_like(new[0])
+    kvr.kvr_continue_shared(desc, *new, kc, vc, L, None, None, torch.zeros(n, dtype=torch.int32, device=DEV), out,
+                            kvr.workspace_for_shared(desc, L, n, S, 0))
+    want = full[L:].double().cpu()
+    far = 2e-3 + 2.0 ** -7 * want.abs()
+    assert float(((out.double().cpu() - want).abs() - far).max()) <= 0.0
