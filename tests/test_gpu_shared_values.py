@@ -144,3 +144,20 @@ def test_peaky_rows_agree_with_a_prefill(kind, n):
     want = full[L:].double().cpu()
     far = 2e-3 + 2.0 ** -7 * want.abs()
     assert float(((out.double().cpu() - want).abs() - far).max()) <= 0.0
+
+
+# ------------------------------------------------------------ references that move
+@EACH_WAY
+@pytest.mark.parametrize("seed", [2, 3])
+def test_weights_that_rise_in_late_stages(dt, way, seed):
+    """One key in 32 is 0 to 140 log2 units above the others, in every range, among own and new rows: references move
+    while sums are not zero, partials of very different ones are joined.  Rows of a tile see them at full
+    height, in part, not at all and upside down."""
+    c = Call(dt, way, seed=seed)
+    heights = torch.tensor([0.0, 10.0, 18.0, 40.0, 70.0, 90.0, 139.0, 140.0])
+    for k in (c.kc, c.kt, c.k.transpose(1, 2)):
+        at = torch.randint(0, 32, k.shape[:-1], generator=c.g) == 0
+        k[..., 0] = torch.where(at, heights[torch.randint(0, 8, k.shape[:-1], generator=c.g)], torch.zeros(()))
+    part = torch.tensor([0.0, 0.125, 0.25, 0.5, 1.0, -0.5])
+    c.q[..., 0] = part[torch.randint(0, 6, c.q.shape[:-1], generator=c.g)]
+    c.check()
