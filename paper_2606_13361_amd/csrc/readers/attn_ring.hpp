@@ -31,7 +31,8 @@ struct Ring16 {
         return D == 128 ? row & 15 : (row >> 1) & 7;
     }
     // This wave's quarter of the rows [0, n) (n > 0) of stride_b bytes from base into the
-    // stage at lds; rows past the last repeat it.
+    // stage at lds; rows past the last repeat it.  A key there is masked by its index; a value
+    // has weight 0, and shared.hip clears it, as the last row's may be infinite.
     template <bool IS_V>
     __device__ static __forceinline__ void load(uint64_t base, uint32_t stride_b, int n, const unsigned char *lds, int wave,
                                                 int lane) {

@@ -335,7 +335,7 @@ struct ByRows {
     uint64_t kb, vb;
     int64_t nkeys;
     unsigned char *lds;
-    int nst, wave, lane;
+    int nst, ragged, wave, lane;      // ragged: the stage that ends inside, or -1
     __device__ __forceinline__ void load(int t, int slot) const {
         const uint64_t off = (uint64_t)t * RG::KEYS * OP::ROWB;
         const int n = stage_rows<RG::KEYS>(nkeys, t);
@@ -351,9 +351,19 @@ struct ByRows {
     __device__ __forceinline__ void begin(uint64_t kb_, uint64_t vb_, int64_t nkeys_, unsigned char *lds_, int wave_, int lane_) {
         kb = kb_; vb = vb_; nkeys = nkeys_; lds = lds_; wave = wave_; lane = lane_;
         nst = (int)((nkeys + RG::KEYS - 1) / RG::KEYS);
+        ragged = nkeys % RG::KEYS ? nst - 1 : -1;
 #pragma unroll
         for (int t = 0; t < SLOTS - 1; ++t)
             if (t < nst) load(t, t);
+    }
+    // Zeros in the place of values behind the last key, whose weights are 0: the row that
+    // load() repeats there may hold an infinity.  Between the barrier behind which the stage has
+    // landed and that of the stage itself.
+    __device__ __forceinline__ void clean(int t, int slot) const {
+        const int n = stage_rows<RG::KEYS>(nkeys, t);
+        unsigned char *to = lds + (slot * 2 + 1) * RG::HALF;
+        for (int at = n * OP::ROWB + 16 * (wave * 64 + lane); at < RG::HALF; at += 16 * 64 * WAVES)
+            *(u32x4 *)(to + at) = (u32x4){0u, 0u, 0u, 0u};
     }
     // Stage t, in slot SLOT: its scores s become weights, while the matrix units make those of
     // the next stage.  32768 keys, 256 rows of a kv head: 61 us one after the other, 57.5 so,
@@ -368,6 +378,7 @@ struct ByRows {
         else wait_vmcnt<0>();
         barrier_lds();
         if (t + SLOTS - 1 < nst) load(t + SLOTS - 1, (SLOT + SLOTS - 1) % SLOTS);
+        if (t + 1 == ragged) clean(t + 1, (SLOT + 1) % SLOTS);
         const unsigned char *vs = lds + SLOT * 2 * RG::HALF + RG::HALF;
         const unsigned char *k1 = lds + (SLOT + 1) % SLOTS * 2 * RG::HALF;      // (behind the last stage: anything, not used)
         typename OP::P w[RT];
@@ -400,6 +411,7 @@ struct ByRows {
         if (nst == 0) return;
         wait_vmcnt<0>();
         barrier_lds();
+        if (ragged == 0) clean(0, 0);
         Scores s, next;
         row_scores<OP, RG, RT>(R, lds, ka, s);
         for (int t = 0; t < nst; t += SLOTS) stages<0>(R, t, s, next, c2, ka, va, g);

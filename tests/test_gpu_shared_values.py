@@ -161,3 +161,20 @@ def test_weights_that_rise_in_late_stages(dt, way, seed):
     part = torch.tensor([0.0, 0.125, 0.25, 0.5, 1.0, -0.5])
     c.q[..., 0] = part[torch.randint(0, 6, c.q.shape[:-1], generator=c.g)]
     c.check()
+
+
+# ------------------------------------------------------------ infinities that are seen
+@EACH_WAY
+def test_an_infinite_value_in_the_last_row(dt, way):
+    """Infinite values in the last row of the prefix and of each reader's own rows, where a range ends inside a
+    stage: infinite outputs, of that sign, in those components, and the others as without them."""
+    c = Call(dt, way, seed=4)
+    want = c.run().float()
+    c.vc[:, c.L - 1, 3] = float("inf")
+    c.vc[:, c.L - 1, 33] = -float("inf")
+    for i, ln in enumerate(c.lens):
+        if ln:
+            c.vt[i, :, ln - 1, 7] = -float("inf")
+            want[i, ..., 7] = -float("inf")
+    want[..., 3], want[..., 33] = float("inf"), -float("inf")
+    assert torch.equal(c.run().float(), want)
