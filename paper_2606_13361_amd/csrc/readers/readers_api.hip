@@ -50,12 +50,20 @@ constexpr int64_t kMaxOwnSplits = 32;
 // and 34.3, 64 of 16384 69.8 and 53.5.
 constexpr int64_t kWork2 = 3 << 19, kWork2F32 = 1 << 19;
 // A call of at most this many stages of prefix and own rows is one launch (kAlone), not the
-// items' and the merge's.  With 64 own rows, 2 readers: 8.3 us instead of 5.8 + 3.2 and the
-// gap between them at 255 keys, 10.3 instead of 5.8 + 3.1 at 512 (and one launch less to
-// issue, 3 us of the host's time), 14.1 instead of 5.9 + 3.2 at 1024; 64 readers: 15.3
-// instead of 15.2 + 4.0 at 255.  fp32, 255 keys: 13.1 instead of 8.3 + 3.1 for 2 readers, 26.6
-// instead of 19.3 + 4.1 for 64.
+// items' and the merge's.  Us a call in a graph, and issued one by one (bf16, 32 / 8 heads of
+// 128, one launch and two):
+//     1 reader    10 stages   7.3 and 7.4   10.3 and 13.1     20 stages    9.8 and 7.5    10.4 and 13.0
+//     32 readers  10          7.7 and 12.9  10.3 and 13.3     20          10.3 and 13.4   10.3 and 13.8
+// fp32, 1 reader, 10 stages: 8.9 and 9.6, 10.4 and 13.1; 20: 11.6 and 9.8, 11.7 and 13.1; 32 readers,
+// 10 stages: 9.7 and 13.4, 10.3 and 13.5.
 constexpr int64_t kAloneStages = 20, kAloneStagesF32 = 10;
+// Every reader reads the prefix anew, so there is a bound on stages times workgroups (one a reader
+// and kv head; at head_dim 64 a compute unit holds two, and each needs half the bytes).  32 / 8 heads
+// of 128, 512 workgroups: 13.4 and 14.6 us with 10 stages, 15.5 and 15.0 with 14, 18.5 and 15.8 with
+// 20; 2048: 35.4 and 31.5 with 3, 67 and 36 with 20 (fp32, 512: 17.4 and 18.2 with 10; 2048: 52 and
+// 42 with 3).  16 / 2 heads of 64, 512: 11.5 and 12.9 with 20; 2048: 26.1 and 30.6 with 10, 34.8 and
+// 31.5 with 18.
+constexpr int64_t kAloneWork = 20 * kCus, kAloneWork64 = 4 * kAloneWork;
 
 struct SharedPlan {
     int pw, ow;
@@ -101,7 +109,9 @@ bool plan_shared(const kvr_desc *d, int64_t L, int64_t n, int64_t S, int64_t tca
         s.octs_o = ceil_div(own * s.nt, 8);
         s.octs_n = ceil_div(n * ceil_div(rows_o, 16) * d->n_kv_heads, 8 * kWaves);
         if ((s.octs_p + s.octs_o + s.octs_n) * 8 > kMaxGrid || s.rows > kMaxGrid) return false;
-        if (rows_o <= 16 && ceil_div(L, stage_keys(d)) + ceil_div(tcap, stage_keys(d)) <= (f32 ? kAloneStagesF32 : kAloneStages))
+        const int64_t stages = ceil_div(L, stage_keys(d)) + ceil_div(tcap, stage_keys(d));
+        const int64_t work = (stages > 1 ? stages : 1) * n * d->n_kv_heads;
+        if (rows_o <= 16 && stages <= (f32 ? kAloneStagesF32 : kAloneStages) && work <= (d->head_dim == 64 ? kAloneWork64 : kAloneWork))
             s.pw = kAlone;
         s.ws_bytes = (size_t)(want + s.nt + 1) * (size_t)s.rows * (d->head_dim + 2) * sizeof(float);
     }
