@@ -383,8 +383,8 @@ int kvr_continue_batched_rope(const kvr_desc *desc, const kvr_rope *rope, const 
  *   rope->n_pos >= pos0 + tail_capacity (+ S when append == 0).
  *   ws: kvr_workspace_bytes_shared(desc, L_prefix, n, S, tail_capacity) bytes; calls (and
  *   captured graphs) that may run at once need one each.
- * Limits: n S n_q_heads below 2^24, L_prefix and tail_capacity below 2^31
- * (KVR_ERR_SHAPE).
+ * Limits: n S n_q_heads below 2^23 is served (more may be, 2^24 is refused), L_prefix and
+ * tail_capacity below 2^31 (KVR_ERR_SHAPE).
  * A masked place never reaches a result: not own rows behind a reader's length, nor
  * a later new token's key or value, whatever they hold.
  */
