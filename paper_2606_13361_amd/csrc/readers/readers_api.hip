@@ -161,6 +161,7 @@ bool plan_weigh(const kvr_desc *d, int64_t L, int64_t S, WeighPlan *out) {
         w.held = f32 && ceil_div(stages, kWaves * 2) * d->n_kv_heads >= kCus ? 2 : 1;
         if (w.grid > kMaxGrid || ceil_div(stages, kWaves) * d->n_kv_heads > kMaxGrid) return false;
         w.join = w.nsplit * rows > kJoinAlone;
+        if (w.join && rows * d->n_kv_heads > kMaxGrid * 32) return false;      // (eight lanes a row: 32 a workgroup)
         w.norm_at = want * d->n_kv_heads * rows * 2 * (int64_t)sizeof(float);
         w.ws_bytes = (size_t)w.norm_at + (size_t)d->n_kv_heads * rows * sizeof(float);
     }

@@ -91,7 +91,7 @@ int main() {
                                     fprintf(stderr, "%s: status %d\n", name, st);
                                 }
                             }
-                for (int64_t total : {(int64_t)4096, (int64_t)1 << 20, ((int64_t)1 << 28) - 1})
+                for (int64_t total : {(int64_t)4096, (int64_t)1 << 20, ((int64_t)1 << 28) - 1, ((int64_t)1 << 29) + 4096, (int64_t)1 << 31})
                     for (int64_t L : {(int64_t)0, (int64_t)1, (int64_t)100000, ((int64_t)1 << 28) / h[1] - 1}) {
                         int64_t S = total / h[0];
                         if (S < 1) continue;
