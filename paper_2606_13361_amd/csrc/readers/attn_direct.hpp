@@ -220,7 +220,6 @@ struct Op16 {
             a[j] &= key_of(2 * j, g) == c ? 0xffffu : key_of(2 * j + 1, g) == c ? 0xffff0000u : 0u;
         return a;
     }
-    __device__ static __forceinline__ void rotate8(u32x4 &lo, u32x4 &hi, const float *cs) { rope_rot8<E>(lo, hi, cs); }
     // operand t of V^T: elements t of keys 2j (low half) and 2j + 1 (high half)
     __device__ static __forceinline__ u32x4 column(const V &v, int t) {
         u32x4 a;
