@@ -19,3 +19,10 @@ CASES = [
 def test_many_readers_of_a_short_prefix(case):
     dt, heads, n, L, tcap = case
     run(Batch(dt, heads, n, 1, L, [i % tcap for i in range(n)], tcap, rope_base=1e4, seed=n))
+
+
+@pytest.mark.parametrize("append", [True, False], ids=["append", "keep"])
+@pytest.mark.parametrize("dt,heads", [(BF16, (16, 4, 128)), (F16, (4, 4, 64)), (F32, (4, 2, 64))], ids=str)
+def test_a_long_prompt_of_a_later_turn(dt, heads, append):
+    """Hundreds of new tokens a reader: many row tiles, and stages of new keys that the first of them do not see."""
+    run(Batch(dt, heads, 3, 257, 100, [0, 5, 300], 560, rope_base=1e4), append)
