@@ -33,21 +33,23 @@ int64_t way_rows(int way) { return way > kByRows ? 64 * (way - kByRows) : 16 * w
 
 // ---- shared
 // Workgroups are as many as there are compute units (256 and 512, items and merge: 2 readers
-// of 32768 keys 27.3 + 4.0 and 27.1 + 5.4 us, 9 of 32768 30.4 + 4.8 and 34.9 + 5.6, 8 readers'
-// 8000 own rows 48.4 + 4.9 and 47.8 + 4.8), as long as each keeps this many keys.
-// Prefix by keys: one stage for each wave; 128 and 256 measured 5.9 and 6.8 us with 255 keys
-// and 2 readers, 9.0 and 11.0 us with 945 keys and 3 readers in fp32.  By rows it is 256:
-// 128, 256 and 512 took 11.0, 10.6 and 14.4 us with 3774 keys and 9 readers, and a merge
-// of more records.  Own rows: 128, 256 and 512 took 11.0, 10.6 and 10.1 us with 9 readers.
+// of 32768 keys 26.9 + 4.2 and 27.1 + 5.4 us, 9 of 32768 31.2 + 4.0 and 35.6 + 5.5, 8 readers'
+// 8000 own rows 48.4 + 4.8 and 47.8 + 4.8; 16 x 4 of 16384 35.2 + 6.1 and 36.3 + 9.0, but 64
+// of 32768 without own rows 58.5 + 6.4 and 51.6 + 9.2), as long as each keeps this many keys.
+// Prefix by keys: one stage for each wave; 128 and 256 measured 5.7 and 6.6 us with 255 keys
+// and 2 readers, 6.1 and 7.4 us with 945 keys and 3 readers in fp32.  By rows it is 256:
+// 128, 256 and 512 took 11.6, 11.0 and 13.7 us with 3774 keys and 9 readers, and a merge
+// of more records.  Own rows: 128, 256 and 512 took 11.6, 11.2 and 10.3 us with 9 readers.
 constexpr int64_t kMinKeysByKeys = 128, kMinKeysByRows = 256, kMinOwnKeys = 512;
-// 2 readers of 8000 own rows: 4 and 16 splits 23.1 and 14.9 us; one of 16000: 16 and 32 splits
-// 15.5 and 14.7
+// 2 readers of 8000 own rows: 4 and 16 splits 23.0 and 14.2 us; one of 16000: 16 and 32 splits
+// 14.8 and 13.9
 constexpr int64_t kMaxOwnSplits = 32;
 // Prefix rows x keys from which a wave (fp32: an item) takes two tiles of query rows, which
 // reads each key half as often, but leaves fewer items.  16-bit, one and two tiles: 256 rows of
-// 3774 keys 18.6 + 4.0 and 19.6 + 5.5 us (items, merge), 128 of 3774 13.7 and 15.2, 68 of 32768
-// 42.6 and 35.0, 256 of 16384 42.8 and 33.8.  fp32: 120 of 945 6.1 and 8.1, 128 of 3774 33.8
-// and 34.3, 64 of 16384 69.8 and 53.5.
+// 3774 keys 18.4 + 4.0 and 20.0 + 5.5 us (items, merge), 128 of 3774 13.7 and 16.3, 68 of 32768
+// 41.7 and 35.9, 256 of 16384 42.0 and 35.8.  fp32, 128 rows of 3774 keys 33.8 and 34.3, 64 of
+// 16384 69.8 and 53.5; of head_dim 64, 192 of 945 6.3 and 8.3, 256 of 3774 12.8 and 12.8, 128 of
+// 16384 20.6 and 18.0.
 constexpr int64_t kWork2 = 3 << 19, kWork2F32 = 1 << 19;
 // A call of at most this many stages of prefix and own rows is one launch (kAlone), not the
 // items' and the merge's.  Us a call in a graph, and issued one by one (bf16, 32 / 8 heads of

@@ -21,18 +21,24 @@
 // The lengths are read on the device: a captured graph serves every step of a decode.
 //
 // Measured, items and merge, in us (32 query heads, 8 kv heads, head_dim 128, one MI355X):
-//   64 readers of 32768 keys, 300 .. 1000 own rows   74.5 + 6.1   304 MB of keys and values, 4.1 TB/s
-//   64 readers of 3774 keys, 24 .. 512 own rows      28.3 + 4.1   87 MB, 2.7 TB/s
-//   16 readers x 4 tokens, 16384 keys                32.6 + 6.1   17.4 GFLOP, 0.53 PFLOP/s
-//   9 readers of 3774 keys                           10.4 + 3.8   latency: lengths, rotation, first keys, records
-//   3 readers x 5 tokens, 945 keys, head_dim 64, fp32   6.1 + 3.2   latency
-// By rows, 32768 keys for 256 rows of a kv head take 55.6 us (0.62 PFLOP/s), of which 10 are
-// the launch, the first stage and the records' writes: a SIMD has one prefix wave, whose
-// exponentials and matrix products (34 of 16 clocks a stage) are in order, one after the
-// other; the other place on the SIMD is the own items'.  Twice the workgroups run the
-// loop at the matrix units' rate (53.7 us) but write and merge twice the records (8.8 instead
-// of 6.1 us); eight waves in two teams that join in LDS run it in as much (18.5 us for 16384
-// keys instead of 23), but leave the own items no place: 89 us for the first line.
+//   64 readers of 32768 keys, 300 .. 1000 own rows   75.1 + 6.3   304 MB of keys and values, 4.0 TB/s
+//   64 readers of 3774 keys, 24 .. 512 own rows      26.9 + 4.2   87 MB, 2.8 TB/s
+//   16 readers x 4 tokens, 16384 keys                35.0 + 6.2   17.4 GFLOP, 0.50 PFLOP/s
+//   9 readers of 3774 keys                           10.4 + 3.9   latency: lengths, rotation, first keys, records
+//   3 readers x 5 tokens, 945 keys, head_dim 64, fp32   5.9 + 3.0   latency
+//   8 readers x 256 tokens, 3774 keys, 100 own rows  230 + 33     a later turn's prompt: new items
+//   8 readers x 24 tokens, the same                  30.4 + 7.4
+// By rows, 32768 keys for 256 rows of a kv head take 58.5 us (0.59 PFLOP/s), of which 10 are
+// the launch, the first stage and the records' writes, and 3 references that move in the
+// first stages (55.6 with references that only move far below the maximum, which rounds
+// weights that hold much of their row): a SIMD has one prefix wave, whose exponentials and
+// matrix products (34 of 16 clocks a stage) are in order, one after the other; the other
+// place on the SIMD is the own items'.  Twice the workgroups: 51.6 us, but twice the records to
+// write and merge (9.2 instead of 6.4 us), 36.3 + 9.0 in the third line; eight waves in two
+// teams that join in LDS took 18.5 us for 16384 keys instead of 23, but leave the own items no
+// place: 89 us for the first line.
+// A later turn's prompt is bound by its new items: a wave loads, rotates and takes 16 new keys at
+// a time, one after the other.
 #include "attn_ring.hpp"
 #include "readers_internal.hpp"
 
@@ -366,8 +372,8 @@ struct ByRows {
             *(u32x4 *)(to + at) = (u32x4){0u, 0u, 0u, 0u};
     }
     // Stage t, in slot SLOT: its scores s become weights, while the matrix units make those of
-    // the next stage.  32768 keys, 256 rows of a kv head: 61 us one after the other, 57.5 so,
-    // and 55.6 with half of V asked for before the exponentials.
+    // the next stage.  32768 keys, 256 rows of a kv head, with references that hardly move: 61 us
+    // one after the other, 57.5 so, and 55.6 with half of V asked for before the exponentials.
     template <int SLOT>
     __device__ __forceinline__ void stage(Rows<OP, RT> &R, int t, Scores &s, Scores &next, float c2, uint32_t ka, uint32_t va,
                                           int g) const {

@@ -17,15 +17,20 @@
 // reproducible bit for bit.
 //
 // Measured, in us (32 query heads, 8 kv heads, head_dim 128, one MI355X):
-//   128 rows over 32640 keys   stats 43, norms 4.7, sums 51   17 GFLOP a pass: 0.40 and 0.34 PFLOP/s
-//   24 rows over 16384 keys    11.6 + 3.9 + 12.7               33 MB of keys a pass
-//   1 row over 3774 keys       4.1 + 4.6                       latency
-// Long calls are bound by the exponentials beside the matrix products, at the clock that this
-// load leaves (about 1.9 GHz): 8 products of 16 clocks and 8 exponentials, 8 fused
-// multiplications and 8 additions for 16 rows and 32 keys.  Scores of the next stage made
-// among the exponentials, as in shared.hip, change nothing (45 and 53): a SIMD has two and
-// three waves that do that for each other.  The second pass holds one stage of keys a wave;
-// two, for half the reads of the query rows, took 60 us instead of 55.
+//   128 tokens over 32640 keys   stats 38.8, norms 4.7, sums 46.9   34.2 GFLOP a pass: 0.88 and 0.73 PFLOP/s
+//   24 tokens over 16384 keys    11.0 + 3.9 + 11.7                  33 MB of keys a pass
+//   1 token over 3774 keys       4.0 + 4.6                          latency
+// (Medians of passes that follow each other; the first ones after a pause are 10 % slower.)
+// Long calls are bound by what a wave issues: for 16 rows and 32 keys 8 products of 16 clocks of a
+// SIMD, and beside them, by the counters, 33 vector instructions in the first pass and 45 in the
+// second: 8 exponentials of 16 clocks, 8 fused multiplications and 8 additions of 4, which are
+// the work, and masks, checks of the sums and, in the second pass, the addresses of the query
+// rows.  That is 128 clocks of products and 228 and 276 of the rest; a unit takes about 290 and
+// 350 at 1.9 GHz, more than the larger of the two: the SIMD's two and three waves overlap
+// them in part.
+// Scores of the next stage made among the exponentials, as in shared.hip, changed nothing (45
+// and 53 us for 43 and 52).  The second pass holds one stage of keys a wave; two, for half the
+// reads of the query rows, took 60 us instead of 55.
 #include <type_traits>
 
 #include "attn_ring.hpp"
