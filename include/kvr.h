@@ -447,6 +447,116 @@ int kvr_cache_evict(const kvr_desc *desc, const void *kcache, const void *vcache
 size_t kvr_workspace_bytes_evict(const kvr_desc *desc, int64_t L);
 
 /*
+ * ---- Paged caches: many sequences in the pages of one pool.
+ *
+ * A pool has n_pages pages of page_size rows for each kv head, keys and values alike: row s
+ * of page b, kv head g is the head_dim elements at k (v) + b * page_stride
+ * + (g * page_size + s) * head_dim.  A dense cache [n_kv_heads][capacity][head_dim] is a
+ * pool of one page.  Row j of sequence r is row j % page_size of page
+ * table[r][j / page_size].  Sequences may have pages in common (a shared prefix), as long as
+ * no call writes rows of them for two sequences.
+ *   page_size    a multiple of 16
+ *   page_stride  elements between pages, >= n_kv_heads * page_size * head_dim and a multiple
+ *                of 16 bytes; k and v may be parts of one array
+ *   table        DEVICE int32 [n][max_pages]: read when the work runs, and only where a
+ *                sequence has rows; max_pages * page_size < 2^31
+ * An entry outside [0, n_pages) is no page: nothing is read or written there.
+ * KVR_ERR_SHAPE, KVR_ERR_ALIGN, KVR_ERR_NULL otherwise.  desc->capacity is not used.
+ */
+typedef struct {
+    void *k, *v;
+    int64_t page_stride;
+    int32_t n_pages;
+    int32_t page_size;
+    const int32_t *table;
+    int32_t max_pages;
+    int32_t reserved; /* must be 0 */
+} kvr_pages;
+
+/*
+ * Rows of tokens with strides: head h of token t is the head_dim elements at
+ * data + t * token_stride + h * head_stride (both >= 0 and multiples of 16 bytes).  The q
+ * rows of a fused projection [tokens][(n_q_heads + 2 n_kv_heads) head_dim] have
+ * token_stride (n_q_heads + 2 n_kv_heads) head_dim and head_stride head_dim; a dense cache
+ * [n_kv_heads][capacity][head_dim] has head_dim and capacity * head_dim.  Rows that a call
+ * writes must not overlap (KVR_ERR_SHAPE).
+ */
+typedef struct {
+    void *data;
+    int64_t token_stride, head_stride;
+} kvr_rows;
+
+/*
+ * Head norms and rotation in one pass, for each row x of q and k:
+ *   y = R(pos) (x / sqrt(mean(x^2) + eps) * w)
+ * R as in kvr_rope_apply; fp32, rounded once to the element type.  With norm weights and a
+ * table a row gets the bits that kvr_layer_forward gives it, with a table alone those of
+ * kvr_rope_apply.
+ *   q, q_out: n_q_heads rows a token; k, k_out: n_kv_heads.  Either pair may be NULL.
+ *   q_out may be q, and k_out k (the same data and strides: in place); other overlaps are
+ *   not allowed.
+ *   q_norm, k_norm [head_dim], 16-byte aligned; NULL: no norm of these rows.
+ *   rope: NULL: no rotation.  pos: DEVICE int32 [n_tok], read when the work runs; NULL:
+ *   token t is at pos0 + t.  rope->n_pos >= pos0 + n_tok (KVR_ERR_POSITION); with pos, a
+ *   token whose position has no entry is left out (its rows of q_out and k_out stay as
+ *   they were).
+ * Limits: n_q_heads + n_kv_heads at most 65535, n_tok below 2^29 is served.
+ */
+int kvr_qk_norm_rope(const kvr_desc *desc, const kvr_rope *rope, const kvr_rows *q, const kvr_rows *k, const void *q_norm,
+                     const void *k_norm, float eps, int64_t n_tok, const int32_t *pos, int64_t pos0, const kvr_rows *q_out,
+                     const kvr_rows *k_out, void *stream);
+
+/*
+ * New tokens into a paged cache: the paged form of kvr_cache_append, with the norm and the
+ * rotation of kvr_qk_norm_rope on the way, and the same for the tokens' queries.
+ *   k, v: n_kv_heads rows for each of n_tok tokens; values are copied.
+ *   q, q_out: n_q_heads rows a token, normalized and rotated into q_out (may be q); or both NULL.
+ *   cu_seqlens: DEVICE int32 [n + 1], cu[0] == 0, non-decreasing: sequence r has tokens
+ *   [cu[r], cu[r + 1]); tokens from cu[n] on are padding.  NULL: n_tok == n, one token of
+ *   each sequence.
+ *   len: DEVICE int32 [n], rows that sequence r has: its token i becomes row len[r] + i
+ *   (len itself is the caller's to advance).  Both are read when the work runs: a captured
+ *   graph serves every step of a decode.
+ *   pos: DEVICE int32 [n_tok], the tokens' positions; NULL: their rows (rope->n_pos >=
+ *   max_pages * page_size then, KVR_ERR_POSITION).
+ * A token takes no part, and its rows of q_out and of the pages stay as they were, if its
+ * sequence has len[r] < 0 (an empty slot of the batch), if it is padding, if its row lies
+ * behind the table's last page or in no page of the pool, or if its position has no entry in the
+ * rotary table.  Two tokens of a call must not have the same row of the same page.
+ * Limits: n_q_heads + 2 n_kv_heads at most 65535, n_tok below 2^29 is served.
+ */
+int kvr_paged_append(const kvr_desc *desc, const kvr_pages *pages, const kvr_rope *rope, const kvr_rows *k, const kvr_rows *v,
+                     const kvr_rows *q, const void *q_norm, const void *k_norm, float eps, int32_t n, int64_t n_tok,
+                     const int32_t *cu_seqlens, const int32_t *len, const int32_t *pos, const kvr_rows *q_out, void *stream);
+
+/*
+ * A decode step's attention: one new token of each of n sequences over its pages.
+ *   out[r][h] = softmax_j(scale * q[r][h] . k_j) v_j over rows j < len[r] + n_new of
+ *   sequence r, query head h reading kv head h / G.
+ *   q: n_q_heads rows for each of n tokens (rotated already, as kvr_paged_append leaves
+ *   them); out [n][n_q_heads][head_dim].
+ *   len: DEVICE int32 [n], read when the work runs; n_new >= 0 is added to each: 1 where the
+ *   step's token has been appended and len not yet advanced.
+ *   max_len: no sequence has more rows; at most max_pages * page_size (KVR_ERR_CAPACITY).
+ *   It decides how the work is shared out and the workspace's size, not how much is read.
+ *   ws: kvr_workspace_bytes_paged(desc, n, max_len) bytes, NULL when that is 0; calls (and
+ *   captured graphs) that may run at once need one each.
+ * A sequence with len[r] < 0, or more than max_len rows, takes no part: its rows of out stay
+ * as they were.  Rows in no page of the pool get no weight, whatever the others hold; a
+ * sequence without any other rows, or with no row at all, gets zeros.
+ * Scores, weights and sums in fp32; 16-bit weights enter the second product as two operands,
+ * a cut weight and what the cut left over.  Results are the same bit for bit
+ * for the same lengths of the whole batch.
+ * Limits: n n_q_heads below 2^24 and n n_kv_heads max_len below 2^37 are served (KVR_ERR_SHAPE
+ * far beyond).
+ */
+int kvr_paged_decode(const kvr_desc *desc, const kvr_pages *pages, const kvr_rows *q, int32_t n, const int32_t *len, int32_t n_new,
+                     int64_t max_len, void *out, void *ws, size_t ws_bytes, void *stream);
+
+/* Workspace bytes of kvr_paged_decode; (size_t)-1 for invalid arguments. */
+size_t kvr_workspace_bytes_paged(const kvr_desc *desc, int32_t n, int64_t max_len);
+
+/*
  * Workspace bytes of kvr_continue_rope (n <= 1, total_S = S) and
  * kvr_continue_batched_rope (n >= 2, total_S = cu[n]): the plain
  * continuation's workspace plus room for the rotated rows.  Non-decreasing in

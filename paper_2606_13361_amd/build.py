@@ -35,7 +35,7 @@ def hipcc():
 
 
 def sources():
-    return sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "readers", "*.hip")))
+    return sorted(p for d in ("", "readers", "paged") for p in glob.glob(os.path.join(CSRC, d, "*.hip")))
 
 
 def model_sources():

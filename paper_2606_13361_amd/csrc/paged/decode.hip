@@ -1,0 +1,589 @@
+// decode.hip -- attention of one new token of each sequence over its pages.
+//
+//   out[r, h] = softmax_j(scale q[r, h] . k_j) v_j,  j < len[r] + n_new, j's page in the pool
+//
+// The lengths are read on the device, so the work is shared out there too: the keys of a
+// sequence and kv head are units of 128 (fp32: 64), a stage of 32 (16) for each wave of a
+// workgroup, and the units of the whole batch, one sequence and head after the other, are
+// cut into equal ranges, one for each workgroup.  However ragged the batch, every workgroup
+// reads as much.  A sequence and head that lie in one range are finished there; pieces of
+// one that several ranges share are records (m, l, O) of the workspace, which a second
+// launch joins in their order.
+//
+// A wave's stages go from memory straight to the registers that the matrix instructions read
+// (attn_direct.hpp); a stage's two halves of 16 rows lie in one page each, and a buffer
+// resource ends with a half's last row, so rows behind a sequence's length, and all rows of a
+// page that is not in the pool, read as zeros and touch no memory.  The next stage's keys
+// are asked for when the scores are done, its values when the outputs are, across the
+// ends of sequences too: their pages are looked up a batch of stages ahead.
+//
+// HBM bounds it: 4 G operations for each byte of 16-bit keys and values, G query heads to a kv head.
+#include "paged/paged_internal.hpp"
+#include "readers/attn_direct.hpp"
+
+namespace kvr {
+namespace {
+
+using namespace dev;
+
+constexpr int WAVES = 4;
+
+// The two element kinds: a stage's weights as the second product's operand.  16-bit: the weight
+// cut to the element type and what that left over, rounded, as two operands, so that weights
+// keep 16 bits (fp16: 22) and outputs are off by little more than their own rounding; the
+// products are matrix instructions that wait for memory anyway.  The cut is of a little less
+// than the weight: then the rest is positive where the weight is, and an infinite value stays one.
+template <class OP>
+struct Weights {
+    typename OP::P hi, lo;
+};
+template <class E, int D>
+struct Dec16 : Op16<E, D> {
+    using B = Op16<E, D>;
+    static constexpr int PARTS = 2;
+    // fp16 weights reach down to 2^-14 before they lose bits: the largest is 2^12
+    static constexpr float LIFT = std::is_same<E, F16>::value ? 12.f : 0.f;
+    using W = Weights<B>;
+    // part h of a stage
+    __device__ static __forceinline__ void load_k(typename B::K &k, __amdgpu_buffer_rsrc_t r, int h, int i, int g) {
+#pragma unroll
+        for (int ks = 0; ks < B::NK; ++ks) k.f[h][ks] = buf_load16(r, B::ROWB * i + 16 * g + 64 * ks);
+    }
+    __device__ static __forceinline__ void load_v(typename B::V &v, __amdgpu_buffer_rsrc_t r, int h, int i, int g) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t off = (4 * g + e) * B::ROWB + 2 * B::NT * i;
+            if constexpr (B::NT == 8) v.r[4 * h + e] = buf_load16(r, off);
+            else v.r[4 * h + e] = __builtin_amdgcn_raw_buffer_load_b64(r, (int)off, 0, 0);
+        }
+    }
+    __device__ static __forceinline__ void pack(W &w, const float (&p)[B::NS]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float a = p[2 * j] * (1.f - 0x1p-20f), b = p[2 * j + 1] * (1.f - 0x1p-20f);
+            uint32_t x;
+            if constexpr (std::is_same<E, F16>::value) x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
+            else x = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+            w.hi.f[j] = x;
+            w.lo.f[j] = E::pack2(p[2 * j] - E::lo(x), p[2 * j + 1] - E::hi(x));
+        }
+    }
+    template <int RT>
+    __device__ static __forceinline__ void outputs(const typename B::V &v, const W (&w)[RT], f32x4 (&o)[RT][B::NT]) {
+#pragma unroll
+        for (int t = 0; t < B::NT; ++t) {
+            const u32x4 a = B::column(v, t);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                o[rt][t] = B::mfma(a, w[rt].lo.f, o[rt][t]);
+                o[rt][t] = B::mfma(a, w[rt].hi.f, o[rt][t]);
+            }
+            if (RT > 1 && t % 2) __builtin_amdgcn_sched_barrier(0);      // operands of two at a time
+        }
+    }
+};
+template <int D>
+struct Dec32 : Op32<D> {
+    using B = Op32<D>;
+    static constexpr int PARTS = 1;
+    static constexpr float LIFT = 0.f;
+    using W = typename B::P;
+    __device__ static __forceinline__ void load_k(typename B::K &k, __amdgpu_buffer_rsrc_t r, int, int i, int g) {
+        B::load_k(k, r, B::ROWB, i, g);
+    }
+    __device__ static __forceinline__ void load_v(typename B::V &v, __amdgpu_buffer_rsrc_t r, int, int i, int g) {
+        B::load_v(v, r, B::ROWB, i, g);
+    }
+    __device__ static __forceinline__ void pack(W &w, const float (&p)[B::NS]) { B::weights(w, p); }
+    template <int RT>
+    __device__ static __forceinline__ void outputs(const typename B::V &v, const W (&w)[RT], f32x4 (&o)[RT][B::NT]) {
+        B::template accumulate<RT>(v, w, o);
+    }
+};
+
+// Rows of a sequence that its token sees; -1: the sequence takes no part
+__device__ __forceinline__ int rows_of(const DecodeParams &p, int32_t len) {
+    const int64_t n = (int64_t)len + p.n_new;
+    return len >= 0 && n <= p.max_len ? (int)n : -1;
+}
+// Units of a sequence (of each of its heads): an empty one has one, which finds no keys
+template <int UNIT>
+__device__ __forceinline__ int units_of(int rows) {
+    return rows < 0 ? 0 : rows == 0 ? 1 : (rows + UNIT - 1) / UNIT;
+}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int lane_of(int x, int l) { return __builtin_amdgcn_readlane(x, l); }
+
+// Inclusive sum over the lanes before
+__device__ __forceinline__ int scan(int x, int lane) {
+#pragma unroll
+    for (int b = 1; b < 64; b <<= 1) {
+        const int y = __shfl_up(x, b);
+        x += lane >= b ? y : 0;
+    }
+    return x;
+}
+
+// A batch: consecutive units of one sequence and head, as many as a wave's lanes hold the parts of
+struct Batch {
+    int r, hd;        // sequence; kv head and row tile
+    int rows, units;  // of the sequence
+    int u, n;         // units [u, u + n)
+    int at;           // unit u among the whole batch's
+};
+
+// The places of a batch's parts, one a lane: lane PARTS j + h has part h of the wave's stage of
+// unit u + j, as bytes from the pool's first (< 0: no rows)
+struct Parts {
+    int64_t off;
+};
+
+template <class OP>
+struct Walk {
+    static constexpr int UNIT = OP::KEYS * WAVES, PER = 64 / OP::PARTS;
+    int heads, left;       // units behind the current batch, of the workgroup's
+    int lens_at, lens;     // rows_of 64 sequences, one a lane
+
+    __device__ __forceinline__ void look(const DecodeParams &p, int r, int lane) {
+        lens_at = r;
+        lens = r + lane < p.n ? rows_of(p, p.len[r + lane]) : -1;
+    }
+    __device__ __forceinline__ int rows(const DecodeParams &p, int r, int lane) {
+        if (r - lens_at >= 64) look(p, r, lane);
+        return lane_of(lens, r - lens_at);
+    }
+    __device__ __forceinline__ void take(Batch &b) {
+        b.n = min(min(PER, b.units - b.u), left);
+        left -= b.n;
+    }
+    // (left > 0)
+    __device__ __forceinline__ void next(const DecodeParams &p, Batch &b, int lane) {
+        b.at += b.n;
+        b.u += b.n;
+        if (b.u == b.units) {
+            b.u = 0;
+            if (++b.hd == heads) {
+                b.hd = 0;
+                do {
+                    ++b.r;
+                    b.rows = rows(p, b.r, lane);
+                    b.units = units_of<UNIT>(b.rows);
+                } while (b.units == 0 && b.r + 1 < p.n);
+                if (b.units == 0) left = 0;      // (the lengths are not what they were)
+            }
+        }
+        take(b);
+    }
+    // The workgroup's first batch; false: it has none.  The sequence of its first unit is found by
+    // sums over 64 groups of sequences, then over 64 groups of the right one's, ...
+    __device__ __forceinline__ bool first(const DecodeParams &p, Batch &b, int wg, int64_t &total, int &sharers, int lane) {
+        heads = p.n_kv_heads * p.tiles;
+        if (p.alone) {
+            b.r = wg / heads;
+            b.hd = wg - b.r * heads;
+            look(p, b.r, lane);
+            b.rows = lane_of(lens, 0);
+            b.units = left = units_of<UNIT>(b.rows);
+            b.u = b.at = 0;
+            if (left == 0) return false;
+            total = left;
+            sharers = 1;
+            take(b);
+            return true;
+        }
+        int lo = 0, cnt = p.n, want = 0, mine, sum, step;
+        int64_t before = 0;
+        for (bool top = true;; top = false) {
+            step = (cnt + 63) / 64;
+            mine = 0;
+            if (step == 1) {
+                look(p, lo, lane);
+                mine = lane < cnt ? units_of<UNIT>(lens) : 0;
+            } else {
+                const int r0 = lo + lane * step, r1 = min(r0 + step, lo + cnt);
+                for (int r = r0; r < r1; ++r) mine += units_of<UNIT>(rows_of(p, p.len[r]));
+            }
+            sum = scan(mine, lane);
+            if (top) {
+                total = (int64_t)lane_of(sum, 63) * heads;
+                if (total == 0) return false;
+                sharers = (int)min((int64_t)p.grid, total);
+                if (wg >= sharers) return false;
+                const int64_t u0 = wg * total / sharers;
+                left = (int)((wg + 1) * total / sharers - u0);
+                b.at = (int)u0;
+                want = (int)(u0 / heads);
+            }
+            const uint64_t over = __ballot(before + sum > want);
+            if (over == 0) return false;      // (the lengths are not what they were)
+            const int l = __builtin_ctzll(over);
+            before += lane_of(sum, l) - lane_of(mine, l);
+            const int start = lo + l * step;
+            cnt = min(step, lo + cnt - start);
+            lo = start;
+            if (step == 1) break;
+        }
+        b.r = lo;
+        b.rows = lane_of(lens, lo - lens_at);
+        b.units = units_of<UNIT>(b.rows);
+        const int rest = (int)(b.at - before * heads);
+        b.hd = rest / b.units;
+        b.u = rest - b.hd * b.units;
+        take(b);
+        return true;
+    }
+    __device__ __forceinline__ Parts parts(const DecodeParams &p, const Batch &b, int wave, int lane) const {
+        const int j = lane / OP::PARTS, h = lane % OP::PARTS;
+        const int part = ((b.u + j) * WAVES + wave) * OP::PARTS + h;
+        Parts o;
+        o.off = -1;
+        if (j < b.n && (int64_t)part * 16 < b.rows) {
+            const int at = (int)((part * p.part_mul) >> p.part_shift);
+            const int page = p.table[(int64_t)b.r * p.max_pages + at];
+            if ((uint32_t)page < (uint32_t)p.n_pages)
+                o.off = page * p.page_bytes + (int64_t)(part * 16 - at * p.page_size) * OP::ROWB;
+        }
+        return o;
+    }
+};
+
+// A wave's stage of unit b.u + j: its parts' first rows, and how many there are
+template <class OP>
+struct Stage {
+    int rows[OP::PARTS];
+    uint64_t at[OP::PARTS];      // bytes from the pool's first
+    __device__ __forceinline__ Stage() {      // none
+#pragma unroll
+        for (int h = 0; h < OP::PARTS; ++h) rows[h] = at[h] = 0;
+    }
+    __device__ __forceinline__ Stage(const DecodeParams &p, const Batch &b, const Parts &parts, int j, int wave) {
+        const int64_t head = (int64_t)(b.hd / p.tiles) * p.page_size * OP::ROWB;
+#pragma unroll
+        for (int h = 0; h < OP::PARTS; ++h) {
+            const int l = j * OP::PARTS + h;
+            const uint32_t lo = lane_of((int)parts.off, l);
+            const int hi = lane_of((int)(parts.off >> 32), l);
+            const int part = ((b.u + j) * WAVES + wave) * OP::PARTS + h;
+            rows[h] = hi < 0 ? 0 : min(b.rows - part * 16, 16);
+            at[h] = hi < 0 ? 0 : ((uint64_t)(uint32_t)hi << 32 | lo) + head;
+        }
+    }
+    __device__ __forceinline__ void load_k(const DecodeParams &p, typename OP::K &k, int i, int g) const {
+#pragma unroll
+        for (int h = 0; h < OP::PARTS; ++h) OP::load_k(k, row_rsrc((uint64_t)p.kp + at[h], rows[h], OP::ROWB, OP::ROWB), h, i, g);
+    }
+    __device__ __forceinline__ void load_v(const DecodeParams &p, typename OP::V &v, int i, int g) const {
+#pragma unroll
+        for (int h = 0; h < OP::PARTS; ++h) OP::load_v(v, row_rsrc((uint64_t)p.vp + at[h], rows[h], OP::ROWB, OP::ROWB), h, i, g);
+    }
+};
+
+template <class OP, int RT>
+struct Rows {
+    f32x4 o[RT][OP::NT];
+    float m[RT], l[RT];      // reference (log2 domain); the lane's share of the row's sum
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            m[rt] = -1e30f;
+            l[rt] = 0.f;
+#pragma unroll
+            for (int t = 0; t < OP::NT; ++t) o[rt][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        }
+    }
+};
+
+// Scores become weights 2^(c2 s - m), m the running maximum less LIFT
+template <class OP, int RT>
+__device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][OP::NS], typename OP::W (&w)[RT],
+                                             const int (&rows)[OP::PARTS], float c2, int g) {
+    int all = rows[0];
+#pragma unroll
+    for (int h = 1; h < OP::PARTS; ++h) all += rows[h];
+    if (all < OP::KEYS) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int e = 0; e < OP::NS; ++e)
+                if (4 * g + (e & 3) >= rows[e >> 2]) s[rt][e] = -INFINITY;
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        float mx = s[rt][0];
+#pragma unroll
+        for (int e = 1; e < OP::NS; ++e) mx = fmaxf(mx, s[rt][e]);
+        mx = fmaxf(quad_max(mx) * c2 - OP::LIFT, R.m[rt]);
+        if (__ballot(mx > R.m[rt])) {
+            const float a = __builtin_amdgcn_exp2f(R.m[rt] - mx);
+            R.m[rt] = mx;
+            R.l[rt] *= a;
+#pragma unroll
+            for (int t = 0; t < OP::NT; ++t) R.o[rt][t] *= a;
+        }
+        float p[OP::NS], sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < OP::NS; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][e], c2, -R.m[rt]));
+            sum += p[e];
+        }
+        R.l[rt] += sum;
+        OP::pack(w[rt], p);
+    }
+}
+
+// The query rows of a kv head's tile; past the last one it again, not to be stored
+template <class OP, int RT>
+__device__ __forceinline__ void take_queries(const DecodeParams &p, typename OP::Q (&q)[RT], int r, int hd, int i, int g) {
+    const int kh = hd / p.tiles, row0 = (hd - kh * p.tiles) * 16 * RT;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = min(row0 + 16 * rt + i, p.group - 1);
+        const int64_t at = r * p.q.token + (kh * p.group + row) * p.q.head;
+        OP::load_q(q[rt], (const unsigned char *)p.q.p + at * OP::ELT, g);
+    }
+}
+
+// Where record rec keeps O, and (m, l)
+template <class OP>
+__device__ __forceinline__ float *record_o(const DecodeParams &p, int64_t rec) {
+    return p.ws + rec * p.rows * OP::DIM;
+}
+template <class OP>
+__device__ __forceinline__ float2 *record_ml(const DecodeParams &p, int64_t rec) {
+    return (float2 *)(p.ws + (int64_t)2 * p.grid * p.rows * OP::DIM) + rec * p.rows;
+}
+// The first and the last workgroup of a sequence and head
+template <class OP>
+__device__ __forceinline__ int2 *sharers_of(const DecodeParams &p, int r, int hd) {
+    return (int2 *)(p.ws + (int64_t)2 * p.grid * p.rows * (OP::DIM + 2)) + (int64_t)r * p.n_kv_heads * p.tiles + hd;
+}
+
+// LDS of a join of one row tile: O of every wave, component c of the lane's four apart, then (m, l)
+template <class OP>
+struct Join {
+    static constexpr int NT = OP::NT;
+    f32x4 o[WAVES][4][64][NT / 4];
+    float2 ml[WAVES][64];
+};
+
+template <class OP, int RT>
+__global__ __launch_bounds__(64 * WAVES, RT > 1 ? 1 : 2) void decode_kernel(const DecodeParams p) {
+    constexpr int NT = OP::NT;
+    __shared__ Join<OP> lds;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int i = lane & 15, g = lane >> 4, wg = blockIdx.x;
+    const float c2 = p.scale_log2;
+
+    Walk<OP> walk;
+    Batch b;
+    int64_t total;
+    int sharers;
+    if (!walk.first(p, b, wg, total, sharers, lane)) return;
+    int seg_u = b.u;      // the segment's first unit here
+    Parts at = walk.parts(p, b, wave, lane);
+    typename OP::Q q[RT];
+    typename OP::K k;
+    typename OP::V v;
+    Rows<OP, RT> R;
+    take_queries<OP, RT>(p, q, b.r, b.hd, i, g);
+    Stage<OP> st(p, b, at, 0, wave);
+    st.load_k(p, k, i, g);
+    st.load_v(p, v, i, g);
+    R.clear();
+
+    for (;;) {
+        Batch nb = b;
+        Parts nat = {-1};
+        const bool more = walk.left > 0;
+        const bool seg_end = b.u + b.n == b.units;
+        if (more) {
+            walk.next(p, nb, lane);
+            nat = walk.parts(p, nb, wave, lane);
+        }
+        for (int j = 0; j < b.n; ++j) {
+            float s[RT][OP::NS];
+            typename OP::W w[RT];
+            int rows[OP::PARTS];
+#pragma unroll
+            for (int h = 0; h < OP::PARTS; ++h) rows[h] = st.rows[h];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) OP::scores(k, q[rt], s[rt]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (j + 1 < b.n) st = Stage<OP>(p, b, at, j + 1, wave);
+            else if (!more) st = Stage<OP>();
+            else {
+                st = Stage<OP>(p, nb, nat, 0, wave);
+                if (seg_end) take_queries<OP, RT>(p, q, nb.r, nb.hd, i, g);      // (the last scores with these are done)
+            }
+            st.load_k(p, k, i, g);
+            __builtin_amdgcn_sched_barrier(0);
+            softmax_step<OP, RT>(R, s, w, rows, c2, g);
+            OP::template outputs<RT>(v, w, R.o);
+            __builtin_amdgcn_sched_barrier(0);
+            st.load_v(p, v, i, g);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (seg_end || !more) {
+            const bool whole = seg_end && seg_u == 0;
+            const int kh = b.hd / p.tiles, row0 = (b.hd - kh * p.tiles) * 16 * RT;
+            // a piece that begins its segment is the workgroup's last, its second record
+            const int64_t rec = 2 * (int64_t)wg + (seg_u == 0 ? 1 : 0);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const int row = row0 + 16 * rt + i;
+                const bool on = row < p.group;
+                __syncthreads();      // the join before this one has been read
+                if (on) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int t = 0; t < NT; t += 4)
+                            lds.o[wave][c][lane][t / 4] = (f32x4){R.o[rt][t][c], R.o[rt][t + 1][c], R.o[rt][t + 2][c], R.o[rt][t + 3][c]};
+                }
+                const float l = quad_sum(R.l[rt]);
+                if (on) lds.ml[wave][lane] = make_float2(R.m[rt], l);
+                __syncthreads();
+                if (on) {
+                    float M = -1e30f, L = 0.f;
+                    f32x4 acc[NT / 4];
+#pragma unroll
+                    for (int t = 0; t < NT / 4; ++t) acc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int s = 0; s < WAVES; ++s) M = fmaxf(M, lds.ml[s][lane].x);
+#pragma unroll
+                    for (int s = 0; s < WAVES; ++s) {
+                        const float2 ml = lds.ml[s][lane];
+                        const float a = __builtin_amdgcn_exp2f(ml.x - M);
+                        L = __builtin_fmaf(a, ml.y, L);
+#pragma unroll
+                        for (int t = 0; t < NT / 4; ++t)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[t][e] = __builtin_fmaf(a, lds.o[s][wave][lane][t][e], acc[t][e]);
+                    }
+                    const int d = NT * (4 * g + wave);
+                    if (whole) {
+                        const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;      // no keys: zeros
+                        unsigned char *out = (unsigned char *)p.out + ((int64_t)b.r * p.n_q_heads + kh * p.group + row) * OP::ROWB;
+#pragma unroll
+                        for (int t = 0; t < NT / 4; ++t)
+                            OP::put4(out, d + 4 * t, acc[t][0] * inv, acc[t][1] * inv, acc[t][2] * inv, acc[t][3] * inv);
+                    } else {
+                        float *po = record_o<OP>(p, rec) + (int64_t)(row - row0) * OP::DIM + d;
+#pragma unroll
+                        for (int t = 0; t < NT / 4; ++t) *(f32x4 *)(po + 4 * t) = acc[t];
+                        if (wave == 0 && g == 0) record_ml<OP>(p, rec)[row - row0] = make_float2(M, L);
+                    }
+                }
+            }
+            if (!p.alone && seg_u == 0 && threadIdx.x == 0) {
+                const int64_t last = (int64_t)b.at + b.n - 1 + (b.units - b.u - b.n);      // the segment's last unit
+                *sharers_of<OP>(p, b.r, b.hd) = make_int2(wg, (int)(((last + 1) * sharers - 1) / total));
+            }
+            R.clear();
+            seg_u = nb.u;
+        }
+        if (!more) break;
+        b = nb;
+        at = nat;
+    }
+}
+
+// The records of one sequence and head, joined in their order.  A row's D values are LANES lanes
+// of four; where rows are few, several ways take the records in turn, and their sums are joined.
+template <class OP>
+__global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p) {
+    constexpr int D = OP::DIM, LANES = D / 4, SLOTS = 256 / LANES, BATCH = 4;
+    __shared__ f32x4 sums[256];
+    __shared__ float2 mls[SLOTS];
+    const int heads = p.n_kv_heads * p.tiles;
+    const int r = blockIdx.x / heads, hd = blockIdx.x - r * heads;
+    if (rows_of(p, p.len[r]) < 0) return;
+    int2 wgs = *sharers_of<OP>(p, r, hd);
+    if (wgs.x == wgs.y) return;
+    wgs.x = max(wgs.x, 0);      // (anything, if the lengths are not what they were)
+    wgs.y = min(wgs.y, p.grid - 1);
+    const int kh = hd / p.tiles, row0 = (hd - kh * p.tiles) * p.rows;
+    const int rows = min(p.rows, p.group - row0);
+    const int slot = threadIdx.x / LANES, d = threadIdx.x % LANES * 4;
+    for (int base = 0; base < rows; base += SLOTS) {
+        const int here = min(rows - base, SLOTS), ways = SLOTS / here;
+        const int row = slot % here, way = slot / here;
+        float M = -1e30f, l = 0.f;
+        f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
+        if (way < ways) {
+            for (int s0 = wgs.x + way; s0 <= wgs.y; s0 += ways * BATCH) {
+                f32x4 x[BATCH];
+                float2 w[BATCH];
+                float mx = M;
+#pragma unroll
+                for (int s = 0; s < BATCH; ++s) {
+                    const int wg = s0 + s * ways;
+                    w[s] = make_float2(-1e30f, 0.f);
+                    x[s] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                    if (wg <= wgs.y) {
+                        const int64_t rec = 2 * (int64_t)wg + (wg == wgs.x ? 1 : 0);
+                        x[s] = *(const f32x4 *)(record_o<OP>(p, rec) + (int64_t)(base + row) * D + d);
+                        w[s] = record_ml<OP>(p, rec)[base + row];
+                    }
+                }
+#pragma unroll
+                for (int s = 0; s < BATCH; ++s) mx = fmaxf(mx, w[s].x);
+                const float a = __builtin_amdgcn_exp2f(M - mx);
+                M = mx;
+                l *= a;
+                acc *= a;
+#pragma unroll
+                for (int s = 0; s < BATCH; ++s) {
+                    const float f = __builtin_amdgcn_exp2f(w[s].x - M);
+                    l = __builtin_fmaf(f, w[s].y, l);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(f, x[s][c], acc[c]);
+                }
+            }
+        }
+        if (base) __syncthreads();
+        sums[threadIdx.x] = acc;
+        if (d == 0) mls[slot] = make_float2(M, l);
+        __syncthreads();
+        if (way == 0) {
+            float top = M;
+            for (int s = 1; s < ways; ++s) top = fmaxf(top, mls[s * here + row].x);
+            const float a = __builtin_amdgcn_exp2f(M - top);
+            l *= a;
+            acc *= a;
+            for (int s = 1; s < ways; ++s) {
+                const float2 ml = mls[s * here + row];
+                const float f = __builtin_amdgcn_exp2f(ml.x - top);
+                l = __builtin_fmaf(f, ml.y, l);
+                const f32x4 x = sums[(s * here + row) * LANES + d / 4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(f, x[c], acc[c]);
+            }
+            const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+            const int64_t at = (int64_t)r * p.n_q_heads + kh * p.group + row0 + base + row;
+            OP::put4((unsigned char *)p.out + at * OP::ROWB, d, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+        }
+    }
+}
+
+template <class OP>
+hipError_t launch_op(const DecodeParams &p, hipStream_t s) {
+    const dim3 grid((unsigned)p.grid), block(64 * WAVES);
+    if (p.rows > 16) hipLaunchKernelGGL((decode_kernel<OP, 2>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((decode_kernel<OP, 1>), grid, block, 0, s, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.alone) return e;
+    hipLaunchKernelGGL(decode_merge_kernel<OP>, dim3((unsigned)(p.n * p.n_kv_heads * p.tiles)), dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_decode(const DecodeParams &p, int head_dim, int dtype, hipStream_t s) {
+    if (dtype == KVR_F32) return head_dim == 128 ? launch_op<Dec32<128>>(p, s) : launch_op<Dec32<64>>(p, s);
+    if (dtype == KVR_F16) return head_dim == 128 ? launch_op<Dec16<F16, 128>>(p, s) : launch_op<Dec16<F16, 64>>(p, s);
+    return head_dim == 128 ? launch_op<Dec16<Bf16, 128>>(p, s) : launch_op<Dec16<Bf16, 64>>(p, s);
+}
+
+}  // namespace kvr

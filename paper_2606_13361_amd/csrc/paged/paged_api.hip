@@ -1,0 +1,252 @@
+// paged_api.hip -- host side of kvr_paged_append, kvr_qk_norm_rope and kvr_paged_decode:
+// argument validation (before any HIP call), work planning and workspaces, as kvr_api.hip
+// does for the other entry points.
+#include <math.h>
+#include <string.h>
+
+#include "kvr.h"
+#include "paged/paged_internal.hpp"
+
+namespace kvr {
+namespace {
+
+constexpr int64_t kCus = 256;
+constexpr int64_t kMaxRows = 0x7fffffff;
+constexpr int64_t kMaxStride = (int64_t)1 << 40;      // elements
+constexpr int64_t kMaxExtent = (int64_t)1 << 60;      // elements of an array: bytes in 64 bits
+constexpr int64_t kMaxGrid = ((int64_t)1 << 24) - 1;  // workgroups of a launch: 2^32 threads are too many
+
+// The library's check of a descriptor: an update of no rows ends after it
+int check_desc(const kvr_desc *d) { return kvr_cache_append(d, nullptr, nullptr, 0, nullptr, nullptr, 0, nullptr); }
+
+float eff_scale(const kvr_desc *d) { return d->scale > 0.f ? d->scale : 1.f / sqrtf((float)d->head_dim); }
+int elt_bytes(const kvr_desc *d) { return d->dtype == KVR_F32 ? 4 : 2; }
+
+bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+int to_status(hipError_t e) { return e == hipSuccess ? KVR_OK : KVR_ERR_DEVICE; }
+
+// ---- rows
+// Rows of `heads` heads of n_tok tokens.  Those that are written must not share memory: one token's after
+// the other's, or one head's.
+int check_rows(const kvr_desc *d, const kvr_rows *r, int64_t n_tok, int64_t heads, bool out) {
+    const int64_t D = d->head_dim, by = 16 / elt_bytes(d);
+    if (r->token_stride < 0 || r->head_stride < 0 || r->token_stride > kMaxStride || r->head_stride > kMaxStride) return KVR_ERR_SHAPE;
+    if (r->token_stride > kMaxExtent / n_tok || r->head_stride > kMaxExtent / heads) return KVR_ERR_SHAPE;
+    if (r->token_stride % by || r->head_stride % by) return KVR_ERR_ALIGN;
+    if (!r->data) return KVR_ERR_NULL;
+    if (!aligned(r->data, 16)) return KVR_ERR_ALIGN;
+    if (!out) return KVR_OK;
+    if (heads > 1 && r->head_stride < D) return KVR_ERR_SHAPE;
+    if (n_tok > 1 && r->token_stride < D) return KVR_ERR_SHAPE;
+    if (heads > 1 && n_tok > 1 && r->token_stride < (heads - 1) * r->head_stride + D &&
+        (r->head_stride - D) / r->token_stride < n_tok - 1)
+        return KVR_ERR_SHAPE;
+    return KVR_OK;
+}
+
+RowsAt rows_at(const kvr_rows *r) {
+    RowsAt a = {nullptr, 0, 0};
+    if (r) { a.p = r->data; a.token = r->token_stride; a.head = r->head_stride; }
+    return a;
+}
+
+int check_table(const kvr_rope *rope, int64_t n_pos) {
+    if (!rope) return KVR_OK;
+    if (!rope->cos_sin) return KVR_ERR_NULL;
+    if (rope->n_pos < n_pos) return KVR_ERR_POSITION;
+    return aligned(rope->cos_sin, 16) ? KVR_OK : KVR_ERR_ALIGN;
+}
+
+// Workgroups of a few tokens each: as many as fill the compute units several times over, as long as
+// one has rows for each of its threads.
+int run_rows(const kvr_desc *d, RowsParams &p, void *stream) {
+    const int64_t per = (int64_t)p.n_q + p.n_k + p.n_v;
+    if (per > kRowsMost) return KVR_ERR_SHAPE;
+    int64_t tokens = ceil_div(p.n_tok, 8 * kCus);
+    if (tokens > kRowTokens) tokens = kRowTokens;
+    if (tokens > kRowsMost / per) tokens = kRowsMost / per;
+    const int64_t grid = ceil_div(p.n_tok, tokens);
+    if (grid > kMaxGrid) return KVR_ERR_SHAPE;
+    p.tokens = (int32_t)tokens;
+    p.by_rows = (uint32_t)((((uint64_t)1 << 32) + per - 1) / per);
+    return to_status(launch_rows(p, d->head_dim, d->dtype, grid, (hipStream_t)stream));
+}
+
+// ---- pages
+int check_pages(const kvr_desc *d, const kvr_pages *g) {
+    if (!g) return KVR_ERR_NULL;
+    if (g->reserved != 0 || g->n_pages < 0 || g->max_pages < 0) return KVR_ERR_SHAPE;
+    if (g->page_size <= 0 || g->page_size % 16) return KVR_ERR_SHAPE;
+    if (g->max_pages > kMaxRows / g->page_size) return KVR_ERR_SHAPE;
+    const int64_t page = (int64_t)d->n_kv_heads * d->head_dim;
+    if (page > kMaxStride / g->page_size) return KVR_ERR_SHAPE;
+    if (g->page_stride < page * g->page_size || g->page_stride > kMaxStride) return KVR_ERR_SHAPE;
+    if (g->n_pages > 0 && g->page_stride > kMaxExtent / g->n_pages) return KVR_ERR_SHAPE;
+    if (g->page_stride % (16 / elt_bytes(d))) return KVR_ERR_ALIGN;
+    return KVR_OK;
+}
+int check_page_pointers(const kvr_pages *g) {
+    if (g->n_pages > 0 && (!g->k || !g->v)) return KVR_ERR_NULL;
+    if (g->max_pages > 0 && !g->table) return KVR_ERR_NULL;
+    return aligned(g->k, 16) && aligned(g->v, 16) && aligned(g->table, 4) ? KVR_OK : KVR_ERR_ALIGN;
+}
+
+// ---- decode
+// Two workgroups a compute unit
+constexpr int64_t kSharers = 2 * kCus;
+// Units up to which a sequence and head is one workgroup's and nothing is joined
+constexpr int64_t kAloneUnits = 4;
+
+struct DecodePlan {
+    int64_t tiles, rows, grid;
+    bool alone;
+    size_t ws_bytes;
+};
+
+bool plan_decode(const kvr_desc *d, int64_t n, int64_t max_len, DecodePlan *out) {
+    DecodePlan s;
+    memset(&s, 0, sizeof s);
+    const int64_t G = d->n_q_heads / d->n_kv_heads, unit = d->dtype == KVR_F32 ? kUnitKeysF32 : kUnitKeys;
+    s.rows = G < 32 ? G : 32;
+    s.tiles = ceil_div(G, 32);
+    if (n > kMaxGrid / d->n_kv_heads / s.tiles || n > kMaxRows / d->n_q_heads) return false;
+    const int64_t heads = n * d->n_kv_heads * s.tiles;
+    const int64_t units = max_len > 0 ? ceil_div(max_len, unit) : 1;
+    if (heads > 0 && units > kMaxRows / heads) return false;
+    s.alone = units <= kAloneUnits;
+    s.grid = s.alone ? heads : units * heads < kSharers ? units * heads : kSharers;
+    if (!s.alone) s.ws_bytes = (size_t)(2 * s.grid * s.rows * (d->head_dim + 2)) * sizeof(float) + (size_t)heads * 8;
+    *out = s;
+    return true;
+}
+
+}  // namespace
+}  // namespace kvr
+
+using namespace kvr;
+
+extern "C" {
+
+int kvr_qk_norm_rope(const kvr_desc *desc, const kvr_rope *rope, const kvr_rows *q, const kvr_rows *k, const void *q_norm,
+                     const void *k_norm, float eps, int64_t n_tok, const int32_t *pos, int64_t pos0, const kvr_rows *q_out,
+                     const kvr_rows *k_out, void *stream) {
+    int st = check_desc(desc);
+    if (st) return st;
+    if (n_tok < 0 || n_tok > kMaxRows || !(eps >= 0.f) || isinf(eps)) return KVR_ERR_SHAPE;
+    if (rope && !pos && (pos0 < 0 || pos0 > kMaxStride)) return KVR_ERR_POSITION;
+    if (n_tok == 0) return KVR_OK;
+    if ((!q && !k) || !q != !q_out || !k != !k_out) return KVR_ERR_NULL;
+    if ((q_norm && !q) || (k_norm && !k)) return KVR_ERR_NULL;
+    if (q && ((st = check_rows(desc, q, n_tok, desc->n_q_heads, false)) || (st = check_rows(desc, q_out, n_tok, desc->n_q_heads, true)))) return st;
+    if (k && ((st = check_rows(desc, k, n_tok, desc->n_kv_heads, false)) || (st = check_rows(desc, k_out, n_tok, desc->n_kv_heads, true)))) return st;
+    if ((st = check_table(rope, pos ? 1 : pos0 + n_tok))) return st;
+    if (!aligned(q_norm, 16) || !aligned(k_norm, 16) || !aligned(pos, 4)) return KVR_ERR_ALIGN;
+
+    RowsParams p;
+    memset(&p, 0, sizeof p);
+    p.q = rows_at(q); p.k = rows_at(k); p.qo = rows_at(q_out); p.ko = rows_at(k_out);
+    p.qn = q_norm; p.kn = k_norm;
+    p.eps = eps;
+    if (rope) { p.cs = rope->cos_sin; p.n_pos = rope->n_pos; }
+    p.pos = pos;
+    p.pos0 = pos0;
+    p.n_tok = n_tok;
+    p.n_q = q ? desc->n_q_heads : 0;
+    p.n_k = k ? desc->n_kv_heads : 0;
+    return run_rows(desc, p, stream);
+}
+
+int kvr_paged_append(const kvr_desc *desc, const kvr_pages *pages, const kvr_rope *rope, const kvr_rows *k, const kvr_rows *v,
+                     const kvr_rows *q, const void *q_norm, const void *k_norm, float eps, int32_t n, int64_t n_tok,
+                     const int32_t *cu_seqlens, const int32_t *len, const int32_t *pos, const kvr_rows *q_out, void *stream) {
+    int st = check_desc(desc);
+    if (st) return st;
+    if ((st = check_pages(desc, pages))) return st;
+    if (n < 0 || n_tok < 0 || n_tok > kMaxRows || (!cu_seqlens && n_tok != n) || !(eps >= 0.f) || isinf(eps)) return KVR_ERR_SHAPE;
+    if (n == 0 || n_tok == 0) return KVR_OK;
+    if (!k || !v || !len || !q != !q_out || (q_norm && !q)) return KVR_ERR_NULL;
+    if ((st = check_page_pointers(pages))) return st;
+    if ((st = check_rows(desc, k, n_tok, desc->n_kv_heads, false)) || (st = check_rows(desc, v, n_tok, desc->n_kv_heads, false))) return st;
+    if (q && ((st = check_rows(desc, q, n_tok, desc->n_q_heads, false)) || (st = check_rows(desc, q_out, n_tok, desc->n_q_heads, true)))) return st;
+    if ((st = check_table(rope, pos ? 1 : (int64_t)pages->max_pages * pages->page_size))) return st;
+    if (!aligned(q_norm, 16) || !aligned(k_norm, 16)) return KVR_ERR_ALIGN;
+    if (!aligned(cu_seqlens, 4) || !aligned(len, 4) || !aligned(pos, 4)) return KVR_ERR_ALIGN;
+    if (pages->n_pages == 0 || pages->max_pages == 0) return KVR_OK;      // no token has a place
+
+    RowsParams p;
+    memset(&p, 0, sizeof p);
+    p.q = rows_at(q); p.k = rows_at(k); p.v = rows_at(v); p.qo = rows_at(q_out);
+    p.qn = q_norm; p.kn = k_norm;
+    p.eps = eps;
+    if (rope) { p.cs = rope->cos_sin; p.n_pos = rope->n_pos; }
+    p.pos = pos;
+    p.kp = (unsigned char *)pages->k; p.vp = (unsigned char *)pages->v;
+    p.page_bytes = pages->page_stride * elt_bytes(desc);
+    p.table = pages->table; p.cu = cu_seqlens; p.len = len;
+    p.n_pages = pages->n_pages;
+    p.page_size = pages->page_size;
+    p.max_pages = pages->max_pages;
+    p.n_seq = n;
+    p.n_tok = n_tok;
+    p.n_q = q ? desc->n_q_heads : 0;
+    p.n_k = p.n_v = desc->n_kv_heads;
+    return run_rows(desc, p, stream);
+}
+
+size_t kvr_workspace_bytes_paged(const kvr_desc *desc, int32_t n, int64_t max_len) {
+    DecodePlan s;
+    if (check_desc(desc) != KVR_OK || n < 0 || max_len < 0 || max_len > kMaxRows) return (size_t)-1;
+    return plan_decode(desc, n, max_len, &s) ? s.ws_bytes : (size_t)-1;
+}
+
+int kvr_paged_decode(const kvr_desc *desc, const kvr_pages *pages, const kvr_rows *q, int32_t n, const int32_t *len, int32_t n_new,
+                     int64_t max_len, void *out, void *ws, size_t ws_bytes, void *stream) {
+    int st = check_desc(desc);
+    if (st) return st;
+    if ((st = check_pages(desc, pages))) return st;
+    if (n < 0 || n_new < 0 || max_len < 0 || max_len > kMaxRows) return KVR_ERR_SHAPE;
+    if (max_len > (int64_t)pages->max_pages * pages->page_size) return KVR_ERR_CAPACITY;
+    DecodePlan plan;
+    if (!plan_decode(desc, n, max_len, &plan)) return KVR_ERR_SHAPE;
+    if (n == 0) return KVR_OK;
+    if (!q || !out || !len) return KVR_ERR_NULL;
+    if ((st = check_rows(desc, q, n, desc->n_q_heads, false))) return st;
+    if ((st = check_page_pointers(pages))) return st;
+    if (!aligned(out, 16) || !aligned(ws, 16) || !aligned(len, 4)) return KVR_ERR_ALIGN;
+    if (plan.ws_bytes && (!ws || ws_bytes < plan.ws_bytes)) return KVR_ERR_WORKSPACE;
+
+    DecodeParams p;
+    memset(&p, 0, sizeof p);
+    p.q = rows_at(q);
+    p.out = out;
+    p.kp = (const unsigned char *)pages->k; p.vp = (const unsigned char *)pages->v;
+    p.page_bytes = pages->page_stride * elt_bytes(desc);
+    p.table = pages->table; p.len = len;
+    p.ws = (float *)ws;
+    p.n = n;
+    p.n_new = n_new;
+    p.max_len = (int32_t)max_len;
+    p.n_pages = pages->n_pages;
+    p.page_size = pages->page_size;
+    p.max_pages = pages->max_pages;
+    p.n_q_heads = desc->n_q_heads;
+    p.n_kv_heads = desc->n_kv_heads;
+    p.group = desc->n_q_heads / desc->n_kv_heads;
+    p.tiles = (int32_t)plan.tiles;
+    p.rows = (int32_t)plan.rows;
+    p.grid = (int32_t)plan.grid;
+    p.alone = plan.alone ? 1 : 0;
+    // part / (parts of a page), exact for the parts of 2^31 rows: with 2^b parts or more, ceil(2^(32 + b) / parts)
+    // is less than 2^b too large in 2^(32 + b), and a part is below 2^28
+    const uint64_t parts = pages->page_size / 16;
+    int bits = 0;
+    while (((uint64_t)1 << bits) < parts) ++bits;
+    p.part_shift = 32 + bits;
+    p.part_mul = (((uint64_t)1 << p.part_shift) + parts - 1) / parts;
+    p.scale_log2 = eff_scale(desc) * 1.4426950408889634f;
+    return to_status(launch_decode(p, desc->head_dim, desc->dtype, (hipStream_t)stream));
+}
+
+}  // extern "C"

@@ -30,7 +30,8 @@ EXPORTS = ("kvr_prefill", "kvr_continue", "kvr_continue_append", "kvr_continue_n
            "kvr_rope_table", "kvr_rope_apply", "kvr_prefill_rope", "kvr_continue_rope",
            "kvr_continue_batched_rope", "kvr_workspace_bytes_rope",
            "kvr_continue_shared", "kvr_workspace_bytes_shared", "kvr_cache_weigh", "kvr_workspace_bytes_weigh",
-           "kvr_cache_evict", "kvr_workspace_bytes_evict")
+           "kvr_cache_evict", "kvr_workspace_bytes_evict",
+           "kvr_qk_norm_rope", "kvr_paged_append", "kvr_paged_decode", "kvr_workspace_bytes_paged")
 
 _TORCH_DTYPE = {KVR_BF16: torch.bfloat16, KVR_F32: torch.float32, KVR_F16: torch.float16}
 
@@ -44,6 +45,16 @@ class kvr_desc(ctypes.Structure):
 
 class kvr_rope(ctypes.Structure):
     _fields_ = [("cos_sin", ctypes.c_void_p), ("n_pos", ctypes.c_int64)]
+
+
+class kvr_pages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("table", ctypes.c_void_p),
+                ("max_pages", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class kvr_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 class KvrError(RuntimeError):
@@ -104,6 +115,12 @@ def load():
     lib.kvr_cache_evict.argtypes = [D, P, P, I64, P, I64, I64, I64, P, P, I64, P, P, P, SZ, P]
     lib.kvr_workspace_bytes_evict.argtypes = [D, I64]
     lib.kvr_workspace_bytes_evict.restype = SZ
+    G, T = ctypes.POINTER(kvr_pages), ctypes.POINTER(kvr_rows)
+    lib.kvr_qk_norm_rope.argtypes = [D, R, T, T, P, P, ctypes.c_float, I64, P, I64, T, T, P]
+    lib.kvr_paged_append.argtypes = [D, G, R, T, T, T, P, P, ctypes.c_float, I32, I64, P, P, P, T, P]
+    lib.kvr_paged_decode.argtypes = [D, G, T, I32, P, I32, I64, P, P, SZ, P]
+    lib.kvr_workspace_bytes_paged.argtypes = [D, I32, I64]
+    lib.kvr_workspace_bytes_paged.restype = SZ
     lib.kvr_strerror.argtypes = [ctypes.c_int]
     lib.kvr_strerror.restype = ctypes.c_char_p
     lib.kvr_abi_version.argtypes = []
@@ -113,7 +130,8 @@ def load():
               lib.kvr_abi_version, lib.kvr_quantize_cache, lib.kvr_continue_q8, lib.kvr_artifact_save,
               lib.kvr_artifact_load, lib.kvr_rope_table, lib.kvr_rope_apply, lib.kvr_prefill_rope,
               lib.kvr_continue_rope, lib.kvr_continue_batched_rope, lib.kvr_continue_shared,
-              lib.kvr_cache_weigh, lib.kvr_cache_evict):
+              lib.kvr_cache_weigh, lib.kvr_cache_evict, lib.kvr_qk_norm_rope, lib.kvr_paged_append,
+              lib.kvr_paged_decode):
         f.restype = ctypes.c_int
     _lib = lib
     return lib
@@ -625,3 +643,164 @@ def kvr_cache_evict(desc, kcache, vcache, L, weight, n_keep, kout, vout, n_first
     _launch(lambda s: load().kvr_cache_evict(ctypes.byref(desc), kc, vc, int(L), w, int(n_first), int(n_last),
                                              int(n_keep), ko, vo, cap, wo, ix, wp, wn, s),
             "kvr_cache_evict", stream, dev)
+
+
+# ---------------------------------------------------------------- paged caches
+class PagedCache:
+    """Sequences in the pages of a pool: k, v [n_pages, n_kv_heads, page_size, head_dim] and a
+    page table, int32 [n, max_pages], all on one GPU.  A page is contiguous; pages may be any
+    distance apart (k = pool[:, 0], v = pool[:, 1] of [n_pages, 2, ...]).  page_size is a
+    multiple of 16.  Entries of the table that are no page of the pool are skipped; they may
+    change between calls, the tensors may not."""
+
+    def __init__(self, desc, k, v, table):
+        dev, dt = _device(k, "k"), _TORCH_DTYPE.get(desc.dtype)
+        if k.dim() != 4:
+            raise ValueError("k must be a tensor [n_pages, n_kv_heads, page_size, head_dim]")
+        n_pages, ps = k.shape[0], k.shape[2]
+        page = (desc.n_kv_heads, ps, desc.head_dim)
+        inner = (ps * desc.head_dim, desc.head_dim, 1)
+        for t, name in ((k, "k"), (v, "v")):
+            _device(t, name)
+            if t.dtype != dt or t.get_device() != dev or t.shape != (n_pages,) + page:
+                raise ValueError("%s must be a %s tensor %s on GPU %d" % (name, dt, (n_pages,) + page, dev))
+            if any(a != b for a, b, m in zip(t.stride()[1:], inner, page) if m > 1):
+                raise ValueError("the rows of a page of %s must be contiguous" % name)
+        # (the stride of a pool of one page is not used, and may be anything)
+        stride = [t.stride(0) if n_pages > 1 else desc.n_kv_heads * ps * desc.head_dim for t in (k, v)]
+        if stride[0] != stride[1]:
+            raise ValueError("pages of k are %d elements apart, those of v %d" % tuple(stride))
+        if not isinstance(table, torch.Tensor) or table.dim() != 2:
+            raise ValueError("table must be an int32 tensor [n, max_pages]")
+        tp = _at(table, "table", torch.int32, table.shape, dev)
+        self.k, self.v, self.table = k, v, table
+        self.device, self.n, self.reach = dev, table.shape[0], table.shape[1] * ps
+        self.geometry = (desc.n_kv_heads, desc.head_dim, desc.dtype)
+        self._c = kvr_pages(k.data_ptr(), v.data_ptr(), stride[0], n_pages, ps, tp, table.shape[1], 0)
+
+    def c(self, desc):
+        if self.geometry != (desc.n_kv_heads, desc.head_dim, desc.dtype):
+            raise ValueError("the cache has kv heads, head_dim, dtype %s, the descriptor %s"
+                             % (self.geometry, (desc.n_kv_heads, desc.head_dim, desc.dtype)))
+        return ctypes.byref(self._c)
+
+
+def _cache(cache, desc):
+    if not isinstance(cache, PagedCache):
+        raise ValueError("cache must be a PagedCache")
+    return cache.c(desc)
+
+
+def _rows(t, name, dt, shape, dev):
+    """Rows [tokens, heads, head_dim] of any token and head stride."""
+    try:
+        if t.dtype is dt and t.get_device() == dev and t.shape == shape:
+            st, sh, s1 = t.stride()
+            if s1 == 1:
+                return ctypes.byref(kvr_rows(t.data_ptr(), st, sh))
+    except AttributeError:      # no tensor
+        pass
+    _device(t, name)
+    if t.dtype != dt:
+        raise ValueError("%s must be a %s tensor, not %s" % (name, dt, t.dtype))
+    if t.get_device() != dev:
+        raise ValueError("%s is on GPU %d, other tensors of the call on GPU %d" % (name, t.get_device(), dev))
+    if t.shape != shape:
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), shape))
+    raise ValueError("%s: the elements of a row must be contiguous" % name)
+
+
+def _rope_at(rope, desc, dev):
+    if rope is None:
+        return None
+    r = _rope(rope, desc)
+    if rope.cos_sin.get_device() != dev:
+        raise ValueError("rope is on GPU %d, other tensors of the call on GPU %d" % (rope.cos_sin.get_device(), dev))
+    return r
+
+
+def kvr_qk_norm_rope(desc, q, k, q_out=None, k_out=None, rope=None, q_norm=None, k_norm=None, eps=1e-6, pos=None,
+                     pos0=0, stream=None):
+    """Head norms and rotation of rows q [n_tok, n_q_heads, head_dim] and k [n_tok, n_kv_heads,
+    head_dim] (views with any token and head stride; either may be None) into q_out and k_out
+    (default: in place).  q_norm, k_norm: weights [head_dim] or None; rope: a RopeTable or
+    None; pos: int32 GPU tensor [n_tok], or token t is at pos0 + t."""
+    d, dt = desc.head_dim, _TORCH_DTYPE.get(desc.dtype)
+    some = k if q is None else q
+    dev = _device(some, "k" if q is None else "q")
+    if some.dim() != 3:
+        raise ValueError("q and k must be tensors [n_tok, heads, head_dim]")
+    n = some.shape[0]
+    qi = qo = ki = ko = None
+    if q is not None:
+        qi = _rows(q, "q", dt, (n, desc.n_q_heads, d), dev)
+        qo = qi if q_out is None else _rows(q_out, "q_out", dt, (n, desc.n_q_heads, d), dev)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if k is not None:
+        ki = _rows(k, "k", dt, (n, desc.n_kv_heads, d), dev)
+        ko = ki if k_out is None else _rows(k_out, "k_out", dt, (n, desc.n_kv_heads, d), dev)
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    qn = None if q_norm is None else _at(q_norm, "q_norm", dt, (d,), dev)
+    kn = None if k_norm is None else _at(k_norm, "k_norm", dt, (d,), dev)
+    ps = None if pos is None else _at(pos, "pos", torch.int32, (n,), dev)
+    rp = _rope_at(rope, desc, dev)
+    _launch(lambda s: load().kvr_qk_norm_rope(ctypes.byref(desc), rp, qi, ki, qn, kn, eps, n, ps, int(pos0), qo, ko, s),
+            "kvr_qk_norm_rope", stream, dev)
+
+
+def kvr_paged_append(desc, cache, k, v, length, rope=None, cu_seqlens=None, pos=None, q=None, q_out=None, q_norm=None,
+                     k_norm=None, eps=1e-6, stream=None):
+    """New tokens' keys and values k, v [n_tok, n_kv_heads, head_dim] (views with any token and
+    head stride) into the pages of a PagedCache, the keys normalized (k_norm) and rotated
+    (rope); their queries q [n_tok, n_q_heads, head_dim] likewise into q_out (default: in
+    place).  length: int32 GPU tensor [n], rows that each sequence has; cu_seqlens: int32 GPU
+    tensor [n + 1] of the packed tokens' sequences (None: one token each); pos: int32 GPU
+    tensor [n_tok] of positions (None: the rows)."""
+    d, dt = desc.head_dim, _TORCH_DTYPE.get(desc.dtype)
+    pages = _cache(cache, desc)
+    dev, n = cache.device, cache.n
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError("k must be a tensor [n_tok, n_kv_heads, head_dim]")
+    T = k.shape[0]
+    ki = _rows(k, "k", dt, (T, desc.n_kv_heads, d), dev)
+    vi = _rows(v, "v", dt, (T, desc.n_kv_heads, d), dev)
+    qi = qo = None
+    if q is not None:
+        qi = _rows(q, "q", dt, (T, desc.n_q_heads, d), dev)
+        qo = qi if q_out is None else _rows(q_out, "q_out", dt, (T, desc.n_q_heads, d), dev)
+    elif q_out is not None or q_norm is not None:
+        raise ValueError("q_out or q_norm without q")
+    qn = None if q_norm is None else _at(q_norm, "q_norm", dt, (d,), dev)
+    kn = None if k_norm is None else _at(k_norm, "k_norm", dt, (d,), dev)
+    ln = _at(length, "length", torch.int32, (n,), dev)
+    cu = None if cu_seqlens is None else _at(cu_seqlens, "cu_seqlens", torch.int32, (n + 1,), dev)
+    ps = None if pos is None else _at(pos, "pos", torch.int32, (T,), dev)
+    rp = _rope_at(rope, desc, dev)
+    _launch(lambda s: load().kvr_paged_append(ctypes.byref(desc), pages, rp, ki, vi, qi, qn, kn, eps, n, T, cu, ln, ps, qo, s),
+            "kvr_paged_append", stream, dev)
+
+
+def kvr_workspace_bytes_paged(desc, n, max_len):
+    return _bytes(load().kvr_workspace_bytes_paged(ctypes.byref(desc), int(n), int(max_len)))
+
+
+def workspace_for_paged(desc, n, max_len, device="cuda"):
+    """Allocate (with torch) the workspace of kvr_paged_decode."""
+    return torch.empty(kvr_workspace_bytes_paged(desc, n, max_len), dtype=torch.uint8, device=device)
+
+
+def kvr_paged_decode(desc, cache, q, length, out, ws=None, n_new=0, max_len=None, stream=None):
+    """Attention of one token of each sequence, q [n, n_q_heads, head_dim] (a view with any
+    token and head stride), into out, over rows [0, length + n_new) of a PagedCache.  length: int32 GPU tensor [n]; max_len: no sequence
+    has more rows (default: all that the page table holds)."""
+    pages = _cache(cache, desc)
+    dev, n = cache.device, cache.n
+    dt, shape = _TORCH_DTYPE.get(desc.dtype), (n, desc.n_q_heads, desc.head_dim)
+    qi, o = _rows(q, "q", dt, shape, dev), _at(out, "out", dt, shape, dev)
+    ln = _at(length, "length", torch.int32, (n,), dev)
+    wp, wn = _scratch(ws, dev)
+    most = int(cache.reach if max_len is None else max_len)
+    _launch(lambda s: load().kvr_paged_decode(ctypes.byref(desc), pages, qi, n, ln, int(n_new), most, o, wp, wn, s),
+            "kvr_paged_decode", stream, dev)
