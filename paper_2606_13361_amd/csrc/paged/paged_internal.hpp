@@ -29,11 +29,11 @@ struct RowsParams {
     int32_t n_pages, page_size, max_pages, n_seq;
     int64_t n_tok;
     int32_t n_q, n_k, n_v;
-    int32_t tokens;          // of a workgroup, at most kRowTokens
-    uint32_t by_rows;        // ceil(2^32 / (n_q + n_k + n_v))
+    int32_t tokens;          // of a wave, one after the other, at most 64
+    int32_t parts;           // waves that share a token's rows
+    int32_t part_rows;       // rows of one of them
 };
-constexpr int kRowTokens = 64;
-constexpr int kRowsMost = 65535;   // rows of a workgroup's tokens: by_rows divides them exactly
+constexpr int kRowWaves = 4;       // of a workgroup
 hipError_t launch_rows(const RowsParams &p, int head_dim, int dtype, int64_t grid, hipStream_t s);
 
 // kvr_paged_decode

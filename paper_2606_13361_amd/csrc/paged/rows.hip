@@ -8,11 +8,19 @@
 // the rotation needs no exchange and a row's sum of squares goes over the D elt / 32
 // lanes next to each other that share it.  The sums are added in the order of every
 // kernel that normalizes heads (pair_sq), and values are rounded as those that rotate
-// rows round them, so that a key has the same bits from each.  A workgroup takes a few
-// tokens: their places are worked out by a thread each while the first rows are on
-// their way.
+// rows round them, so that a key has the same bits from each.
 //
-// HBM bounds it.
+// A wave takes rows of one token at a time: its cosines and sines are read once, and up to
+// BATCH rows of a lane are on their way at once.  The places of the wave's tokens are worked
+// out by a lane each, while the first rows are on their way.
+//
+// HBM bounds it (a 1 GB copy reaches 5.1 TB/s).  bf16, 32 / 8 heads of 128, read and written:
+//   32768 tokens' norms and rotation 127 us, 5.4 TB/s
+//   32 prompts, 32767 tokens, into pages 171 us, 4.7 TB/s; 3774 tokens' keys and values 9.3 us
+// Rows of the next tokens that are not on their way while these are worked out are hidden by
+// other waves: 3 rows a lane (4 waves a SIMD) and 6 (3 waves) took 181 and 198 us for the prompts,
+// 66 and 74 us for 32768 tokens' keys and values.  Written rows bypass the caches as far as
+// a hint does that: 3774 tokens 10.9 us without, the norms 136.
 #include "attn_common.hpp"
 #include "paged/paged_internal.hpp"
 
@@ -21,8 +29,8 @@ namespace {
 
 using namespace dev;
 
-constexpr int NT = 256;
-constexpr int BATCH = 2;      // rows of a thread that are on their way at once
+constexpr int WAVES = kRowWaves;
+constexpr int BATCH = 3;      // rows of a lane that are on their way at once
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -108,101 +116,128 @@ struct Place {
     int64_t slot;      // < 0: the token takes no part
     int64_t pos;
 };
+__device__ __forceinline__ int64_t lane_of(int64_t x, int l) {
+    const uint32_t lo = __builtin_amdgcn_readlane((int)x, l), hi = __builtin_amdgcn_readlane((int)(x >> 32), l);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
 
+// How many of cu[1 .. n] are at most t (they are in order): 64 of them at a time
+__device__ __forceinline__ int ended(const int32_t *cu, int n, int64_t t, int lane) {
+    int lo = 0, cnt = n;
+    while (cnt > 0) {
+        const int step = (cnt + 63) / 64;
+        const int at = (lane + 1) * step;
+        const int c = __popcll(__ballot(at <= cnt && cu[lo + min(at, cnt)] <= t));      // whole steps that ended
+        lo += c * step;
+        cnt = min(step - 1, cnt - c * step);
+    }
+    return lo;
+}
+
+// The places of tokens t0 .. t0 + n - 1 (at most 64), one a lane
 template <bool PAGED>
-__device__ __forceinline__ Place place_of(const RowsParams &p, int64_t t, const int32_t *cu_lds, int row_bytes) {
+__device__ __forceinline__ Place places_of(const RowsParams &p, int64_t t0, int n, int row_bytes, int lane) {
+    const int64_t t = t0 + lane;
     Place o;
-    o.slot = 0;
-    o.pos = p.pos ? (int64_t)p.pos[t] : p.pos0 + t;
+    o.slot = -1;
+    o.pos = 0;
+    int r = lane < n ? 0 : p.n_seq;
     if constexpr (PAGED) {
-        const Place none = {-1, 0};
-        int r = (int)t;
-        int64_t first = t;
         if (p.cu) {
-            // sequences that end at t or before
-            int lo = 0, hi = p.n_seq;
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                const int32_t end = p.n_seq <= NT ? cu_lds[mid + 1] : p.cu[mid + 1];
-                if (end <= t) lo = mid + 1; else hi = mid;
+            const int r0 = ended(p.cu, p.n_seq, t0, lane);
+            const int64_t end = r0 + 1 + lane <= p.n_seq ? (int64_t)p.cu[r0 + 1 + lane] : (int64_t)1 << 40;
+            for (int j = 0; j < n; ++j) {
+                int c = r0 + __popcll(__ballot(end <= t0 + j));
+                if (c == r0 + 64) c = ended(p.cu, p.n_seq, t0 + j, lane);      // (a row of sequences without tokens)
+                if (lane == j) r = c;
             }
-            r = lo;
-            if (r == p.n_seq) return none;
-            first = p.n_seq <= NT ? cu_lds[r] : p.cu[r];
-            if (first < 0 || first > t) return none;
+        } else if (lane < n) {
+            r = (int)t;
         }
+    }
+    if (lane >= n || (PAGED && r >= p.n_seq)) return o;
+    o.pos = p.pos ? (int64_t)p.pos[t] : p.pos0 + t;
+    int64_t slot = 0;
+    if constexpr (PAGED) {
+        const int64_t first = p.cu ? p.cu[r] : t;
         const int32_t len = p.len[r];
-        if (len < 0) return none;
+        if (first < 0 || first > t || len < 0) return o;
         const int64_t row = (int64_t)len + (t - first);
-        if (row >= (int64_t)p.max_pages * p.page_size) return none;
+        if (row >= (int64_t)p.max_pages * p.page_size) return o;
         const int32_t at = (int32_t)row / p.page_size;
         const int32_t page = p.table[(int64_t)r * p.max_pages + at];
-        if ((uint32_t)page >= (uint32_t)p.n_pages) return none;
+        if ((uint32_t)page >= (uint32_t)p.n_pages) return o;
         if (!p.pos) o.pos = row;
-        o.slot = page * p.page_bytes + (int64_t)((int32_t)row - at * p.page_size) * row_bytes;
+        slot = page * p.page_bytes + (int64_t)((int32_t)row - at * p.page_size) * row_bytes;
     }
-    if (p.cs && (o.pos < 0 || o.pos >= p.n_pos)) o.slot = -1;
+    if (!p.cs || (o.pos >= 0 && o.pos < p.n_pos)) o.slot = slot;
     return o;
 }
 
 template <class T, int D, bool PAGED>
-__global__ __launch_bounds__(NT) void rows_kernel(const RowsParams p) {
+__global__ __launch_bounds__(64 * WAVES) void rows_kernel(const RowsParams p) {
     using EL = Elt<T>;
-    constexpr int N = EL::N, LANES = D / (2 * N), ROWS = NT / LANES, ROWB = D * EL::BYTES;
-    __shared__ Place places[kRowTokens];
-    __shared__ int32_t cu_lds[NT + 1];
-    const int tid = threadIdx.x;
-    const int c = chunk_of<LANES>(tid % LANES);
-    const int per = p.n_q + p.n_k + p.n_v;
-    const int64_t t0 = (int64_t)blockIdx.x * p.tokens;
-    const int nt = (int)min((int64_t)p.tokens, p.n_tok - t0);
-    const int total = nt * per;
+    constexpr int N = EL::N, LANES = D / (2 * N), ROWS = 64 / LANES, ROWB = D * EL::BYTES;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = chunk_of<LANES>(lane % LANES);
+    const int per = p.n_q + p.n_k + p.n_v, n_qk = p.n_q + p.n_k;
+    const uint32_t id = blockIdx.x * WAVES + wave, group = id / (uint32_t)p.parts;
+    const int64_t t0 = (int64_t)group * p.tokens, t1 = min(t0 + p.tokens, p.n_tok);
+    const int first = (int)(id - group * p.parts) * p.part_rows, last = min(first + p.part_rows, per);
 
-    Chunk x[BATCH];
-    auto load = [&](int r0) {
+    // weights of the lane's elements
+    u32x4 w[2][2];
 #pragma unroll
-        for (int b = 0; b < BATCH; ++b) {
-            const int r = r0 + b * ROWS;
-            if (r >= total) continue;
-            const int tk = (int)__umulhi((uint32_t)r, p.by_rows);
-            int h = r - tk * per;
-            const RowsAt &a = h < p.n_q ? p.q : h < p.n_q + p.n_k ? p.k : p.v;
-            h -= h < p.n_q ? 0 : h < p.n_q + p.n_k ? p.n_q : p.n_q + p.n_k;
-            const unsigned char *s = (const unsigned char *)a.p + ((t0 + tk) * a.token + h * a.head) * EL::BYTES + 16 * c;
-            x[b].lo = *(const u32x4 *)s;
-            x[b].hi = *(const u32x4 *)(s + ROWB / 2);
-        }
-    };
-    load(tid / LANES);
-    if constexpr (PAGED) {
-        if (p.cu && p.n_seq <= NT) {
-            for (int j = tid; j <= p.n_seq; j += NT) cu_lds[j] = p.cu[j];
-            __syncthreads();
-        }
+    for (int i = 0; i < 2; ++i) {
+        const unsigned char *n = (const unsigned char *)(i ? p.kn : p.qn) + 16 * c;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            w[i][h] = (i ? p.kn : p.qn) ? *(const u32x4 *)(n + h * (ROWB / 2)) : (u32x4){0u, 0u, 0u, 0u};
     }
-    if (tid < nt) places[tid] = place_of<PAGED>(p, t0 + tid, cu_lds, ROWB);
-    __syncthreads();
 
-    for (int r0 = tid / LANES; r0 < total; r0 += BATCH * ROWS) {
+    Place at;
+    for (int64_t t = t0; t < t1; ++t) {
+        int64_t slot;
+        float cs[2 * N];
+        for (int r0 = first; r0 < last; r0 += BATCH * ROWS) {
+            Chunk x[BATCH];
 #pragma unroll
-        for (int b = 0; b < BATCH; ++b) {
-            const int r = r0 + b * ROWS;
-            if (r >= total) continue;      // all lanes of a row alike
-            const int tk = (int)__umulhi((uint32_t)r, p.by_rows);
-            int h = r - tk * per;
-            const Place at = places[tk];
-            if (at.slot < 0) continue;
-            const bool is_q = h < p.n_q, is_v = h >= p.n_q + p.n_k;
-            h -= is_q ? 0 : is_v ? p.n_q + p.n_k : p.n_q;
-            if (!is_v) {
-                const void *nw = is_q ? p.qn : p.kn;
-                const float *cs = p.cs ? p.cs + at.pos * D + 2 * N * c : nullptr;
-                if (nw) {
+            for (int b = 0; b < BATCH; ++b) {
+                if (r0 + b * ROWS >= last) break;
+                const int r = min(r0 + b * ROWS + lane / LANES, last - 1);
+                const RowsAt &a = r < p.n_q ? p.q : r < n_qk ? p.k : p.v;
+                const int h = r - (r < p.n_q ? 0 : r < n_qk ? p.n_q : n_qk);
+                const unsigned char *s = (const unsigned char *)a.p + (t * a.token + h * a.head) * EL::BYTES + 16 * c;
+                x[b].lo = *(const u32x4 *)s;
+                x[b].hi = *(const u32x4 *)(s + ROWB / 2);
+            }
+            if (r0 == first) {
+                if (t == t0) at = places_of<PAGED>(p, t0, (int)(t1 - t0), ROWB, lane);
+                slot = lane_of(at.slot, (int)(t - t0));
+                if (slot < 0) break;
+                if (p.cs) {
+                    const float *s = p.cs + lane_of(at.pos, (int)(t - t0)) * D + 2 * N * c;
+#pragma unroll
+                    for (int j = 0; j < 2 * N; ++j) cs[j] = s[j];
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                if (r0 + b * ROWS >= last) break;
+                const int r = r0 + b * ROWS + lane / LANES;
+                const bool is_q = r < p.n_q, is_v = r >= n_qk;
+                const bool norm = !is_v && (is_q ? p.qn : p.kn);
+                Chunk y = x[b];
+                if (p.cs && __ballot(!is_v && !norm)) {
+                    EL::rotate(y, cs);
+                    if (norm || is_v) y = x[b];
+                }
+                if (__ballot(norm)) {
                     float a[N], e[N], s[N], wa[N], we[N];
                     EL::widen(x[b].lo, a);
                     EL::widen(x[b].hi, e);
-                    EL::widen(*(const u32x4 *)((const unsigned char *)nw + 16 * c), wa);
-                    EL::widen(*(const u32x4 *)((const unsigned char *)nw + ROWB / 2 + 16 * c), we);
+                    EL::widen(is_q ? w[0][0] : w[1][0], wa);
+                    EL::widen(is_q ? w[0][1] : w[1][1], we);
 #pragma unroll
                     for (int j = 0; j < N; ++j) s[j] = pair_sq(a[j], e[j]);
                     const float inv = 1.0f / sqrtf(row_sum<LANES, N>(s) / (float)D + p.eps);
@@ -211,35 +246,34 @@ __global__ __launch_bounds__(NT) void rows_kernel(const RowsParams p) {
                         a[j] = a[j] * inv * wa[j];
                         e[j] = e[j] * inv * we[j];
                     }
-                    if (cs) {
+                    if (p.cs) {
 #pragma unroll
                         for (int j = 0; j < N; ++j) {
-                            const float y = a[j], z = e[j];
-                            rope_rot(y, z, cs[2 * j], cs[2 * j + 1], a[j], e[j]);
+                            const float f = a[j], g = e[j];
+                            rope_rot(f, g, cs[2 * j], cs[2 * j + 1], a[j], e[j]);
                         }
                     }
-                    x[b].lo = EL::narrow(a);
-                    x[b].hi = EL::narrow(e);
-                } else if (cs) {
-                    EL::rotate(x[b], cs);
+                    const u32x4 lo = EL::narrow(a), hi = EL::narrow(e);
+                    if (norm) { y.lo = lo; y.hi = hi; }
                 }
+                if (r >= last) continue;
+                const int h = r - (is_q ? 0 : is_v ? n_qk : p.n_q);
+                unsigned char *d;
+                if (PAGED && !is_q)
+                    d = (is_v ? p.vp : p.kp) + slot + (int64_t)h * p.page_size * ROWB;
+                else
+                    d = (unsigned char *)(is_q ? p.qo.p : p.ko.p) +
+                        (t * (is_q ? p.qo.token : p.ko.token) + h * (is_q ? p.qo.head : p.ko.head)) * EL::BYTES;
+                __builtin_nontemporal_store(y.lo, (u32x4 *)(d + 16 * c));
+                __builtin_nontemporal_store(y.hi, (u32x4 *)(d + ROWB / 2 + 16 * c));
             }
-            unsigned char *d;
-            if (PAGED && !is_q)
-                d = (is_v ? p.vp : p.kp) + at.slot + (int64_t)h * p.page_size * ROWB;
-            else
-                d = (unsigned char *)(is_q ? p.qo.p : p.ko.p) +
-                    ((t0 + tk) * (is_q ? p.qo.token : p.ko.token) + h * (is_q ? p.qo.head : p.ko.head)) * EL::BYTES;
-            *(u32x4 *)(d + 16 * c) = x[b].lo;
-            *(u32x4 *)(d + ROWB / 2 + 16 * c) = x[b].hi;
         }
-        load(r0 + BATCH * ROWS);
     }
 }
 
 template <class T>
 hipError_t launch_t(const RowsParams &p, int head_dim, int64_t grid, hipStream_t s) {
-    const dim3 g((unsigned)grid), b(NT);
+    const dim3 g((unsigned)grid), b(64 * WAVES);
     if (p.kp) {
         if (head_dim == 128) hipLaunchKernelGGL((rows_kernel<T, 128, true>), g, b, 0, s, p);
         else hipLaunchKernelGGL((rows_kernel<T, 64, true>), g, b, 0, s, p);
