@@ -26,7 +26,7 @@ namespace {
 
 using namespace dev;
 
-constexpr int WAVES = 4;
+constexpr int SHARED_WAVES = 4, ALONE_WAVES = 8;
 
 // The two element kinds: a stage's weights as the second product's operand.  16-bit: the weight
 // cut to the element type and what that left over, rounded, as two operands, so that weights
@@ -139,7 +139,7 @@ struct Parts {
     int64_t off;
 };
 
-template <class OP>
+template <class OP, int WAVES>
 struct Walk {
     static constexpr int UNIT = OP::KEYS * WAVES, PER = 64 / OP::PARTS;
     int heads, left;       // units behind the current batch, of the workgroup's
@@ -249,7 +249,7 @@ struct Walk {
 };
 
 // A wave's stage of unit b.u + j: its parts' first rows, and how many there are
-template <class OP>
+template <class OP, int WAVES>
 struct Stage {
     int rows[OP::PARTS];
     uint64_t at[OP::PARTS];      // bytes from the pool's first
@@ -360,22 +360,23 @@ __device__ __forceinline__ int2 *sharers_of(const DecodeParams &p, int r, int hd
 }
 
 // LDS of a join of one row tile: O of every wave, component c of the lane's four apart, then (m, l)
-template <class OP>
+template <class OP, int WAVES>
 struct Join {
     static constexpr int NT = OP::NT;
     f32x4 o[WAVES][4][64][NT / 4];
     float2 ml[WAVES][64];
 };
 
-template <class OP, int RT>
+template <class OP, int RT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, RT > 1 ? 1 : 2) void decode_kernel(const DecodeParams p) {
     constexpr int NT = OP::NT;
-    __shared__ Join<OP> lds;
+    using St = Stage<OP, WAVES>;
+    __shared__ Join<OP, WAVES> lds;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int i = lane & 15, g = lane >> 4, wg = blockIdx.x;
     const float c2 = p.scale_log2;
 
-    Walk<OP> walk;
+    Walk<OP, WAVES> walk;
     Batch b;
     int64_t total;
     int sharers;
@@ -387,7 +388,7 @@ __global__ __launch_bounds__(64 * WAVES, RT > 1 ? 1 : 2) void decode_kernel(cons
     typename OP::V v;
     Rows<OP, RT> R;
     take_queries<OP, RT>(p, q, b.r, b.hd, i, g);
-    Stage<OP> st(p, b, at, 0, wave);
+    St st(p, b, at, 0, wave);
     st.load_k(p, k, i, g);
     st.load_v(p, v, i, g);
     R.clear();
@@ -410,10 +411,10 @@ __global__ __launch_bounds__(64 * WAVES, RT > 1 ? 1 : 2) void decode_kernel(cons
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) OP::scores(k, q[rt], s[rt]);
             __builtin_amdgcn_sched_barrier(0);
-            if (j + 1 < b.n) st = Stage<OP>(p, b, at, j + 1, wave);
-            else if (!more) st = Stage<OP>();
+            if (j + 1 < b.n) st = St(p, b, at, j + 1, wave);
+            else if (!more) st = St();
             else {
-                st = Stage<OP>(p, nb, nat, 0, wave);
+                st = St(p, nb, nat, 0, wave);
                 if (seg_end) take_queries<OP, RT>(p, q, nb.r, nb.hd, i, g);      // (the last scores with these are done)
             }
             st.load_k(p, k, i, g);
@@ -444,7 +445,7 @@ __global__ __launch_bounds__(64 * WAVES, RT > 1 ? 1 : 2) void decode_kernel(cons
                 const float l = quad_sum(R.l[rt]);
                 if (on) lds.ml[wave][lane] = make_float2(R.m[rt], l);
                 __syncthreads();
-                if (on) {
+                if (on && wave < 4) {
                     float M = -1e30f, L = 0.f;
                     f32x4 acc[NT / 4];
 #pragma unroll
@@ -489,92 +490,87 @@ __global__ __launch_bounds__(64 * WAVES, RT > 1 ? 1 : 2) void decode_kernel(cons
     }
 }
 
-// The records of one sequence and head, joined in their order.  A row's D values are LANES lanes
-// of four; where rows are few, several ways take the records in turn, and their sums are joined.
+// The records of one query row, joined in an order that the lengths fix: several ways take them in
+// turn, LANES lanes of four values each, and their sums are joined.
 template <class OP>
 __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p) {
-    constexpr int D = OP::DIM, LANES = D / 4, SLOTS = 256 / LANES, BATCH = 4;
+    constexpr int D = OP::DIM, LANES = D / 4, WAYS = 256 / LANES, BATCH = 4;
     __shared__ f32x4 sums[256];
-    __shared__ float2 mls[SLOTS];
-    const int heads = p.n_kv_heads * p.tiles;
-    const int r = blockIdx.x / heads, hd = blockIdx.x - r * heads;
-    if (rows_of(p, p.len[r]) < 0) return;
-    int2 wgs = *sharers_of<OP>(p, r, hd);
-    if (wgs.x == wgs.y) return;
+    __shared__ float2 mls[WAYS];
+    const int r = blockIdx.x / p.n_q_heads, h = blockIdx.x - r * p.n_q_heads;
+    const int kh = h / p.group, tile = (h - kh * p.group) / p.rows, row = h - kh * p.group - tile * p.rows;
+    int2 wgs = *sharers_of<OP>(p, r, kh * p.tiles + tile);
+    if (rows_of(p, p.len[r]) < 0 || wgs.x == wgs.y) return;
     wgs.x = max(wgs.x, 0);      // (anything, if the lengths are not what they were)
     wgs.y = min(wgs.y, p.grid - 1);
-    const int kh = hd / p.tiles, row0 = (hd - kh * p.tiles) * p.rows;
-    const int rows = min(p.rows, p.group - row0);
-    const int slot = threadIdx.x / LANES, d = threadIdx.x % LANES * 4;
-    for (int base = 0; base < rows; base += SLOTS) {
-        const int here = min(rows - base, SLOTS), ways = SLOTS / here;
-        const int row = slot % here, way = slot / here;
-        float M = -1e30f, l = 0.f;
-        f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
-        if (way < ways) {
-            for (int s0 = wgs.x + way; s0 <= wgs.y; s0 += ways * BATCH) {
-                f32x4 x[BATCH];
-                float2 w[BATCH];
-                float mx = M;
+    const int way = threadIdx.x / LANES, d = threadIdx.x % LANES * 4;
+    float M = -1e30f, l = 0.f;
+    f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int s0 = wgs.x + way; s0 <= wgs.y; s0 += WAYS * BATCH) {
+        f32x4 x[BATCH];
+        float2 w[BATCH];
+        float mx = M;
 #pragma unroll
-                for (int s = 0; s < BATCH; ++s) {
-                    const int wg = s0 + s * ways;
-                    w[s] = make_float2(-1e30f, 0.f);
-                    x[s] = (f32x4){0.f, 0.f, 0.f, 0.f};
-                    if (wg <= wgs.y) {
-                        const int64_t rec = 2 * (int64_t)wg + (wg == wgs.x ? 1 : 0);
-                        x[s] = *(const f32x4 *)(record_o<OP>(p, rec) + (int64_t)(base + row) * D + d);
-                        w[s] = record_ml<OP>(p, rec)[base + row];
-                    }
-                }
-#pragma unroll
-                for (int s = 0; s < BATCH; ++s) mx = fmaxf(mx, w[s].x);
-                const float a = __builtin_amdgcn_exp2f(M - mx);
-                M = mx;
-                l *= a;
-                acc *= a;
-#pragma unroll
-                for (int s = 0; s < BATCH; ++s) {
-                    const float f = __builtin_amdgcn_exp2f(w[s].x - M);
-                    l = __builtin_fmaf(f, w[s].y, l);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(f, x[s][c], acc[c]);
-                }
+        for (int s = 0; s < BATCH; ++s) {
+            const int wg = s0 + s * WAYS;
+            w[s] = make_float2(-1e30f, 0.f);
+            x[s] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            if (wg <= wgs.y) {
+                const int64_t rec = 2 * (int64_t)wg + (wg == wgs.x ? 1 : 0);
+                x[s] = *(const f32x4 *)(record_o<OP>(p, rec) + (int64_t)row * D + d);
+                w[s] = record_ml<OP>(p, rec)[row];
             }
         }
-        if (base) __syncthreads();
-        sums[threadIdx.x] = acc;
-        if (d == 0) mls[slot] = make_float2(M, l);
-        __syncthreads();
-        if (way == 0) {
-            float top = M;
-            for (int s = 1; s < ways; ++s) top = fmaxf(top, mls[s * here + row].x);
-            const float a = __builtin_amdgcn_exp2f(M - top);
-            l *= a;
-            acc *= a;
-            for (int s = 1; s < ways; ++s) {
-                const float2 ml = mls[s * here + row];
-                const float f = __builtin_amdgcn_exp2f(ml.x - top);
-                l = __builtin_fmaf(f, ml.y, l);
-                const f32x4 x = sums[(s * here + row) * LANES + d / 4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(f, x[c], acc[c]);
-            }
-            const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-            const int64_t at = (int64_t)r * p.n_q_heads + kh * p.group + row0 + base + row;
-            OP::put4((unsigned char *)p.out + at * OP::ROWB, d, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+        for (int s = 0; s < BATCH; ++s) mx = fmaxf(mx, w[s].x);
+        const float a = __builtin_amdgcn_exp2f(M - mx);
+        M = mx;
+        l *= a;
+        acc *= a;
+#pragma unroll
+        for (int s = 0; s < BATCH; ++s) {
+            const float f = __builtin_amdgcn_exp2f(w[s].x - M);
+            l = __builtin_fmaf(f, w[s].y, l);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(f, x[s][c], acc[c]);
         }
     }
+    sums[threadIdx.x] = acc;
+    if (d == 0) mls[way] = make_float2(M, l);
+    __syncthreads();
+    if (way) return;
+    float top = M;
+#pragma unroll
+    for (int s = 1; s < WAYS; ++s) top = fmaxf(top, mls[s].x);
+    const float a = __builtin_amdgcn_exp2f(M - top);
+    l *= a;
+    acc *= a;
+#pragma unroll
+    for (int s = 1; s < WAYS; ++s) {
+        const float2 ml = mls[s];
+        const float f = __builtin_amdgcn_exp2f(ml.x - top);
+        l = __builtin_fmaf(f, ml.y, l);
+        const f32x4 x = sums[s * LANES + threadIdx.x];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(f, x[c], acc[c]);
+    }
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+    OP::put4((unsigned char *)p.out + ((int64_t)r * p.n_q_heads + h) * OP::ROWB, d, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
 }
 
 template <class OP>
 hipError_t launch_op(const DecodeParams &p, hipStream_t s) {
-    const dim3 grid((unsigned)p.grid), block(64 * WAVES);
-    if (p.rows > 16) hipLaunchKernelGGL((decode_kernel<OP, 2>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((decode_kernel<OP, 1>), grid, block, 0, s, p);
+    const dim3 grid((unsigned)p.grid);
+    if (p.alone) {
+        if (p.rows > 16) hipLaunchKernelGGL((decode_kernel<OP, 2, ALONE_WAVES>), grid, dim3(64 * ALONE_WAVES), 0, s, p);
+        else hipLaunchKernelGGL((decode_kernel<OP, 1, ALONE_WAVES>), grid, dim3(64 * ALONE_WAVES), 0, s, p);
+        return hipGetLastError();
+    }
+    if (p.rows > 16) hipLaunchKernelGGL((decode_kernel<OP, 2, SHARED_WAVES>), grid, dim3(64 * SHARED_WAVES), 0, s, p);
+    else hipLaunchKernelGGL((decode_kernel<OP, 1, SHARED_WAVES>), grid, dim3(64 * SHARED_WAVES), 0, s, p);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.alone) return e;
-    hipLaunchKernelGGL(decode_merge_kernel<OP>, dim3((unsigned)(p.n * p.n_kv_heads * p.tiles)), dim3(256), 0, s, p);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(decode_merge_kernel<OP>, dim3((unsigned)(p.n * p.n_q_heads)), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 

@@ -122,7 +122,7 @@ bool plan_decode(const kvr_desc *d, int64_t n, int64_t max_len, DecodePlan *out)
     const int64_t G = d->n_q_heads / d->n_kv_heads, unit = d->dtype == KVR_F32 ? kUnitKeysF32 : kUnitKeys;
     s.rows = G < 32 ? G : 32;
     s.tiles = ceil_div(G, 32);
-    if (n > kMaxGrid / d->n_kv_heads / s.tiles || n > kMaxRows / d->n_q_heads) return false;
+    if (n > kMaxGrid / d->n_kv_heads / s.tiles || n > kMaxGrid / d->n_q_heads) return false;
     const int64_t heads = n * d->n_kv_heads * s.tiles;
     const int64_t units = max_len > 0 ? ceil_div(max_len, unit) : 1;
     if (heads > 0 && units > kMaxRows / heads) return false;
