@@ -553,7 +553,8 @@ int kvr_paged_append(const kvr_desc *desc, const kvr_pages *pages, const kvr_rop
 int kvr_paged_decode(const kvr_desc *desc, const kvr_pages *pages, const kvr_rows *q, int32_t n, const int32_t *len, int32_t n_new,
                      int64_t max_len, void *out, void *ws, size_t ws_bytes, void *stream);
 
-/* Workspace bytes of kvr_paged_decode; (size_t)-1 for invalid arguments. */
+/* Workspace bytes of kvr_paged_decode: non-decreasing in max_len; (size_t)-1 for invalid
+ * arguments. */
 size_t kvr_workspace_bytes_paged(const kvr_desc *desc, int32_t n, int64_t max_len);
 
 /*

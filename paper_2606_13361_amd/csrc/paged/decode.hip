@@ -3,8 +3,8 @@
 //   out[r, h] = softmax_j(scale q[r, h] . k_j) v_j,  j < len[r] + n_new, j's page in the pool
 //
 // The lengths are read on the device, so the work is shared out there too: the keys of a
-// sequence and kv head are units of 128 (fp32: 64), a stage of 32 (16) for each wave of a
-// workgroup, and the units of the whole batch, one sequence and head after the other, are
+// sequence and kv head are units, a stage of 32 (fp32: 16) for each wave of a workgroup,
+// and the units of the whole batch, one sequence and head after the other, are
 // cut into equal ranges, one for each workgroup.  However ragged the batch, every workgroup
 // reads as much.  A sequence and head that lie in one range are finished there; pieces of
 // one that several ranges share are records (m, l, O) of the workspace, which a second
@@ -15,7 +15,8 @@
 // resource ends with a half's last row, so rows behind a sequence's length, and all rows of a
 // page that is not in the pool, read as zeros and touch no memory.  The next stage's keys
 // are asked for when the scores are done, its values when the outputs are, across the
-// ends of sequences too: their pages are looked up a batch of stages ahead.
+// ends of sequences too: its pages are looked up another stage ahead, with scalar loads, which
+// do not wait behind the keys and values that are on their way.
 //
 // HBM bounds it: 4 G operations for each byte of 16-bit keys and values, G query heads to a kv head.
 #include "paged/paged_internal.hpp"
@@ -26,7 +27,6 @@ namespace {
 
 using namespace dev;
 
-constexpr int SHARED_WAVES = 4, ALONE_WAVES = 8;
 
 // The two element kinds: a stage's weights as the second product's operand.  16-bit: the weight
 // cut to the element type and what that left over, rounded, as two operands, so that weights
@@ -116,35 +116,59 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 __device__ __forceinline__ int lane_of(int x, int l) { return __builtin_amdgcn_readlane(x, l); }
 
 // Inclusive sum over the lanes before
-__device__ __forceinline__ int scan(int x, int lane) {
-#pragma unroll
-    for (int b = 1; b < 64; b <<= 1) {
-        const int y = __shfl_up(x, b);
-        x += lane >= b ? y : 0;
-    }
+__device__ __forceinline__ int scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // row_shr 1, 2, 4, 8: within 16 lanes
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // the sums of rows 0 and 2 to 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // of the first two to the others
     return x;
 }
 
-// A batch: consecutive units of one sequence and head, as many as a wave's lanes hold the parts of
-struct Batch {
+// `total` units cut into ranges of nearly one length, the longer ones first
+struct Cut {
+    int total, n, each, more;      // ranges; units of one; how many have one unit more
+    __device__ __forceinline__ int start(int w) const { return w * each + min(w, more); }
+    __device__ __forceinline__ int range_of(int u) const {
+        const int longer = more * (each + 1);
+        return u < longer ? u / (each + 1) : more + (u - longer) / each;
+    }
+};
+
+// Memory that no kernel of the call writes, read with scalar loads
+template <class T>
+__device__ __forceinline__ T scalar(const T *x) {
+    return *(const __attribute__((address_space(4))) T *)(uintptr_t)x;
+}
+
+// A unit of one sequence and head, and the wave's stage of it
+struct Unit {
     int r, hd;        // sequence; kv head and row tile
     int rows, units;  // of the sequence
-    int u, n;         // units [u, u + n)
-    int at;           // unit u among the whole batch's
+    int u;
+    int page, part;   // the stage's first part: entry of the page table, and which of the page's
+    __device__ __forceinline__ bool last() const { return u + 1 == units; }
 };
 
-// The places of a batch's parts, one a lane: lane PARTS j + h has part h of the wave's stage of
-// unit u + j, as bytes from the pool's first (< 0: no rows)
-struct Parts {
-    int64_t off;
-};
-
+// The workgroup's units, one after the other
 template <class OP, int WAVES>
 struct Walk {
-    static constexpr int UNIT = OP::KEYS * WAVES, PER = 64 / OP::PARTS;
-    int heads, left;       // units behind the current batch, of the workgroup's
+    static constexpr int UNIT = OP::KEYS * WAVES, PARTS = UNIT / 16;      // keys, and parts of 16, of a unit
+    int heads, left;       // units behind the one returned last
     int lens_at, lens;     // rows_of 64 sequences, one a lane
+    int page0, part0;      // of the wave's stage of a sequence's first unit
+    int pages, parts;      // from one unit to the next
 
+    __device__ __forceinline__ Walk(const DecodeParams &p, int wave) {
+        heads = p.n_kv_heads * p.tiles;
+        page_of(p, wave * OP::PARTS, page0, part0);
+        page_of(p, PARTS, pages, parts);
+    }
+    __device__ __forceinline__ static void page_of(const DecodeParams &p, int part, int &page, int &rest) {
+        page = (int)((part * p.part_mul) >> p.part_shift);
+        rest = part - page * (p.page_size >> 4);
+    }
     __device__ __forceinline__ void look(const DecodeParams &p, int r, int lane) {
         lens_at = r;
         lens = r + lane < p.n ? rows_of(p, p.len[r + lane]) : -1;
@@ -153,16 +177,13 @@ struct Walk {
         if (r - lens_at >= 64) look(p, r, lane);
         return lane_of(lens, r - lens_at);
     }
-    __device__ __forceinline__ void take(Batch &b) {
-        b.n = min(min(PER, b.units - b.u), left);
-        left -= b.n;
-    }
     // (left > 0)
-    __device__ __forceinline__ void next(const DecodeParams &p, Batch &b, int lane) {
-        b.at += b.n;
-        b.u += b.n;
-        if (b.u == b.units) {
+    __device__ __forceinline__ void next(const DecodeParams &p, Unit &b, int lane) {
+        --left;
+        if (b.last()) {
             b.u = 0;
+            b.page = page0;
+            b.part = part0;
             if (++b.hd == heads) {
                 b.hd = 0;
                 do {
@@ -170,30 +191,34 @@ struct Walk {
                     b.rows = rows(p, b.r, lane);
                     b.units = units_of<UNIT>(b.rows);
                 } while (b.units == 0 && b.r + 1 < p.n);
-                if (b.units == 0) left = 0;      // (the lengths are not what they were)
+                if (b.units == 0) b.units = 1, left = 0;      // (the lengths are not what they were)
+            }
+        } else {
+            ++b.u;
+            b.page += pages;
+            b.part += parts;
+            if (b.part >= p.page_size >> 4) {
+                b.part -= p.page_size >> 4;
+                ++b.page;
             }
         }
-        take(b);
     }
-    // The workgroup's first batch; false: it has none.  The sequence of its first unit is found by
-    // sums over 64 groups of sequences, then over 64 groups of the right one's, ...
-    __device__ __forceinline__ bool first(const DecodeParams &p, Batch &b, int wg, int64_t &total, int &sharers, int lane) {
-        heads = p.n_kv_heads * p.tiles;
+    // The workgroup's first unit, and the `at` of it among all; false: it has none.  The sequence is found
+    // by sums over 64 groups of sequences, then over 64 groups of the right one's, ...
+    __device__ __forceinline__ bool first(const DecodeParams &p, Unit &b, int &at, int wg, Cut &cut, int wave, int lane) {
         if (p.alone) {
             b.r = wg / heads;
             b.hd = wg - b.r * heads;
-            look(p, b.r, lane);
-            b.rows = lane_of(lens, 0);
-            b.units = left = units_of<UNIT>(b.rows);
-            b.u = b.at = 0;
-            if (left == 0) return false;
-            total = left;
-            sharers = 1;
-            take(b);
+            b.rows = rows_of(p, scalar(p.len + b.r));
+            b.units = units_of<UNIT>(b.rows);
+            if (b.units == 0) return false;
+            b.u = at = 0;
+            b.page = page0;
+            b.part = part0;
+            left = b.units - 1;
             return true;
         }
-        int lo = 0, cnt = p.n, want = 0, mine, sum, step;
-        int64_t before = 0;
+        int lo = 0, cnt = p.n, want = 0, before = 0, mine, sum, step;
         for (bool top = true;; top = false) {
             step = (cnt + 63) / 64;
             mine = 0;
@@ -204,16 +229,16 @@ struct Walk {
                 const int r0 = lo + lane * step, r1 = min(r0 + step, lo + cnt);
                 for (int r = r0; r < r1; ++r) mine += units_of<UNIT>(rows_of(p, p.len[r]));
             }
-            sum = scan(mine, lane);
+            sum = scan(mine);
             if (top) {
-                total = (int64_t)lane_of(sum, 63) * heads;
-                if (total == 0) return false;
-                sharers = (int)min((int64_t)p.grid, total);
-                if (wg >= sharers) return false;
-                const int64_t u0 = wg * total / sharers;
-                left = (int)((wg + 1) * total / sharers - u0);
-                b.at = (int)u0;
-                want = (int)(u0 / heads);
+                cut.total = lane_of(sum, 63) * heads;
+                cut.n = min(p.grid, cut.total);
+                if (wg >= cut.n) return false;
+                cut.each = cut.total / cut.n;
+                cut.more = cut.total - cut.each * cut.n;
+                at = cut.start(wg);
+                left = cut.start(wg + 1) - at - 1;
+                want = at / heads;
             }
             const uint64_t over = __ballot(before + sum > want);
             if (over == 0) return false;      // (the lengths are not what they were)
@@ -227,28 +252,31 @@ struct Walk {
         b.r = lo;
         b.rows = lane_of(lens, lo - lens_at);
         b.units = units_of<UNIT>(b.rows);
-        const int rest = (int)(b.at - before * heads);
+        const int rest = at - before * heads;
         b.hd = rest / b.units;
         b.u = rest - b.hd * b.units;
-        take(b);
+        page_of(p, (b.u * WAVES + wave) * OP::PARTS, b.page, b.part);
         return true;
-    }
-    __device__ __forceinline__ Parts parts(const DecodeParams &p, const Batch &b, int wave, int lane) const {
-        const int j = lane / OP::PARTS, h = lane % OP::PARTS;
-        const int part = ((b.u + j) * WAVES + wave) * OP::PARTS + h;
-        Parts o;
-        o.off = -1;
-        if (j < b.n && (int64_t)part * 16 < b.rows) {
-            const int at = (int)((part * p.part_mul) >> p.part_shift);
-            const int page = p.table[(int64_t)b.r * p.max_pages + at];
-            if ((uint32_t)page < (uint32_t)p.n_pages)
-                o.off = page * p.page_bytes + (int64_t)(part * 16 - at * p.page_size) * OP::ROWB;
-        }
-        return o;
     }
 };
 
-// A wave's stage of unit b.u + j: its parts' first rows, and how many there are
+// What the page table says for a stage's parts.  Asked for two stages ahead.
+template <class OP, int WAVES>
+struct Pages {
+    int page[OP::PARTS];
+    __device__ __forceinline__ void ask(const DecodeParams &p, const Unit &b, int wave) {
+        const int key = (b.u * WAVES + wave) * OP::KEYS;
+        int at = b.page, part = b.part;
+#pragma unroll
+        for (int h = 0; h < OP::PARTS; ++h) {
+            // (a part without rows has no entry of its own)
+            page[h] = scalar(p.table + (int64_t)b.r * p.max_pages + (key + 16 * h < b.rows ? at : 0));
+            if (++part == p.page_size >> 4) part = 0, ++at;
+        }
+    }
+};
+
+// A wave's stage of a unit: its parts' first rows, and how many there are
 template <class OP, int WAVES>
 struct Stage {
     int rows[OP::PARTS];
@@ -257,16 +285,17 @@ struct Stage {
 #pragma unroll
         for (int h = 0; h < OP::PARTS; ++h) rows[h] = at[h] = 0;
     }
-    __device__ __forceinline__ Stage(const DecodeParams &p, const Batch &b, const Parts &parts, int j, int wave) {
-        const int64_t head = (int64_t)(b.hd / p.tiles) * p.page_size * OP::ROWB;
+    __device__ __forceinline__ Stage(const DecodeParams &p, const Unit &b, const Pages<OP, WAVES> &pages, int wave) {
+        const uint64_t first = (uint64_t)(b.hd / p.tiles) * (uint32_t)p.page_size;
+        const int key = (b.u * WAVES + wave) * OP::KEYS;
+        int part = b.part;
 #pragma unroll
         for (int h = 0; h < OP::PARTS; ++h) {
-            const int l = j * OP::PARTS + h;
-            const uint32_t lo = lane_of((int)parts.off, l);
-            const int hi = lane_of((int)(parts.off >> 32), l);
-            const int part = ((b.u + j) * WAVES + wave) * OP::PARTS + h;
-            rows[h] = hi < 0 ? 0 : min(b.rows - part * 16, 16);
-            at[h] = hi < 0 ? 0 : ((uint64_t)(uint32_t)hi << 32 | lo) + head;
+            const int n = min(b.rows - (key + 16 * h), 16);
+            const bool there = n > 0 && (uint32_t)pages.page[h] < (uint32_t)p.n_pages;
+            rows[h] = there ? n : 0;
+            at[h] = there ? (uint64_t)pages.page[h] * (uint64_t)p.page_bytes + (first + 16 * (uint32_t)part) * OP::ROWB : 0;
+            if (++part == p.page_size >> 4) part = 0;
         }
     }
     __device__ __forceinline__ void load_k(const DecodeParams &p, typename OP::K &k, int i, int g) const {
@@ -359,7 +388,7 @@ __device__ __forceinline__ int2 *sharers_of(const DecodeParams &p, int r, int hd
     return (int2 *)(p.ws + (int64_t)2 * p.grid * p.rows * (OP::DIM + 2)) + (int64_t)r * p.n_kv_heads * p.tiles + hd;
 }
 
-// LDS of a join of one row tile: O of every wave, component c of the lane's four apart, then (m, l)
+// LDS of a join of one row tile by a workgroup's waves: O, component c of the lane's four apart, and (m, l)
 template <class OP, int WAVES>
 struct Join {
     static constexpr int NT = OP::NT;
@@ -371,61 +400,62 @@ template <class OP, int RT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, RT > 1 ? 1 : 2) void decode_kernel(const DecodeParams p) {
     constexpr int NT = OP::NT;
     using St = Stage<OP, WAVES>;
-    __shared__ Join<OP, WAVES> lds;
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : uniform(threadIdx.x >> 6);
     const int i = lane & 15, g = lane >> 4, wg = blockIdx.x;
     const float c2 = p.scale_log2;
 
-    Walk<OP, WAVES> walk;
-    Batch b;
-    int64_t total;
-    int sharers;
-    if (!walk.first(p, b, wg, total, sharers, lane)) return;
-    int seg_u = b.u;      // the segment's first unit here
-    Parts at = walk.parts(p, b, wave, lane);
+    Walk<OP, WAVES> walk(p, wave);
+    Unit b, n1, n2;       // this unit, the next, the one after it
+    Pages<OP, WAVES> p1, p2;
+    Cut cut;
+    int at;
+    if (!walk.first(p, b, at, wg, cut, wave, lane)) return;
+    p1.ask(p, b, wave);
     typename OP::Q q[RT];
     typename OP::K k;
     typename OP::V v;
     Rows<OP, RT> R;
     take_queries<OP, RT>(p, q, b.r, b.hd, i, g);
-    St st(p, b, at, 0, wave);
+    St st(p, b, p1, wave);
     st.load_k(p, k, i, g);
     st.load_v(p, v, i, g);
+    n1 = b;
+    bool more = walk.left > 0;
+    if (more) {
+        walk.next(p, n1, lane);
+        p1.ask(p, n1, wave);
+    }
+    int seg_u = b.u;      // the segment's first unit here
     R.clear();
 
     for (;;) {
-        Batch nb = b;
-        Parts nat = {-1};
-        const bool more = walk.left > 0;
-        const bool seg_end = b.u + b.n == b.units;
-        if (more) {
-            walk.next(p, nb, lane);
-            nat = walk.parts(p, nb, wave, lane);
-        }
-        for (int j = 0; j < b.n; ++j) {
-            float s[RT][OP::NS];
-            typename OP::W w[RT];
-            int rows[OP::PARTS];
+        float s[RT][OP::NS];
+        typename OP::W w[RT];
+        int rows[OP::PARTS];
 #pragma unroll
-            for (int h = 0; h < OP::PARTS; ++h) rows[h] = st.rows[h];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) OP::scores(k, q[rt], s[rt]);
-            __builtin_amdgcn_sched_barrier(0);
-            if (j + 1 < b.n) st = St(p, b, at, j + 1, wave);
-            else if (!more) st = St();
-            else {
-                st = St(p, nb, nat, 0, wave);
-                if (seg_end) take_queries<OP, RT>(p, q, nb.r, nb.hd, i, g);      // (the last scores with these are done)
-            }
-            st.load_k(p, k, i, g);
-            __builtin_amdgcn_sched_barrier(0);
-            softmax_step<OP, RT>(R, s, w, rows, c2, g);
-            OP::template outputs<RT>(v, w, R.o);
-            __builtin_amdgcn_sched_barrier(0);
-            st.load_v(p, v, i, g);
-            __builtin_amdgcn_sched_barrier(0);
+        for (int h = 0; h < OP::PARTS; ++h) rows[h] = st.rows[h];
+        if (more) st = St(p, n1, p1, wave);
+        else st = St();
+        n2 = n1;
+        const bool more2 = walk.left > 0;
+        if (more2) {
+            walk.next(p, n2, lane);
+            p2.ask(p, n2, wave);
         }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) OP::scores(k, q[rt], s[rt]);
+        __builtin_amdgcn_sched_barrier(0);
+        st.load_k(p, k, i, g);
+        __builtin_amdgcn_sched_barrier(0);
+        softmax_step<OP, RT>(R, s, w, rows, c2, g);
+        OP::template outputs<RT>(v, w, R.o);
+        __builtin_amdgcn_sched_barrier(0);
+        st.load_v(p, v, i, g);
+        __builtin_amdgcn_sched_barrier(0);
+        const bool seg_end = b.last();
         if (seg_end || !more) {
+            if (more) take_queries<OP, RT>(p, q, n1.r, n1.hd, i, g);
             const bool whole = seg_end && seg_u == 0;
             const int kh = b.hd / p.tiles, row0 = (b.hd - kh * p.tiles) * 16 * RT;
             // a piece that begins its segment is the workgroup's last, its second record
@@ -434,35 +464,10 @@ __global__ __launch_bounds__(64 * WAVES, RT > 1 ? 1 : 2) void decode_kernel(cons
             for (int rt = 0; rt < RT; ++rt) {
                 const int row = row0 + 16 * rt + i;
                 const bool on = row < p.group;
-                __syncthreads();      // the join before this one has been read
-                if (on) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int t = 0; t < NT; t += 4)
-                            lds.o[wave][c][lane][t / 4] = (f32x4){R.o[rt][t][c], R.o[rt][t + 1][c], R.o[rt][t + 2][c], R.o[rt][t + 3][c]};
-                }
                 const float l = quad_sum(R.l[rt]);
-                if (on) lds.ml[wave][lane] = make_float2(R.m[rt], l);
-                __syncthreads();
-                if (on && wave < 4) {
-                    float M = -1e30f, L = 0.f;
-                    f32x4 acc[NT / 4];
-#pragma unroll
-                    for (int t = 0; t < NT / 4; ++t) acc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int s = 0; s < WAVES; ++s) M = fmaxf(M, lds.ml[s][lane].x);
-#pragma unroll
-                    for (int s = 0; s < WAVES; ++s) {
-                        const float2 ml = lds.ml[s][lane];
-                        const float a = __builtin_amdgcn_exp2f(ml.x - M);
-                        L = __builtin_fmaf(a, ml.y, L);
-#pragma unroll
-                        for (int t = 0; t < NT / 4; ++t)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[t][e] = __builtin_fmaf(a, lds.o[s][wave][lane][t][e], acc[t][e]);
-                    }
-                    const int d = NT * (4 * g + wave);
+                // c: the component of the lane's four, head-dim indices NT (4 g + c) ..
+                auto put = [&](int c, const f32x4 (&acc)[NT / 4], float M, float L) {
+                    const int d = NT * (4 * g + c);
                     if (whole) {
                         const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;      // no keys: zeros
                         unsigned char *out = (unsigned char *)p.out + ((int64_t)b.r * p.n_q_heads + kh * p.group + row) * OP::ROWB;
@@ -473,37 +478,84 @@ __global__ __launch_bounds__(64 * WAVES, RT > 1 ? 1 : 2) void decode_kernel(cons
                         float *po = record_o<OP>(p, rec) + (int64_t)(row - row0) * OP::DIM + d;
 #pragma unroll
                         for (int t = 0; t < NT / 4; ++t) *(f32x4 *)(po + 4 * t) = acc[t];
-                        if (wave == 0 && g == 0) record_ml<OP>(p, rec)[row - row0] = make_float2(M, L);
+                        if (c == 0 && g == 0) record_ml<OP>(p, rec)[row - row0] = make_float2(M, L);
+                    }
+                };
+                if constexpr (WAVES == 1) {
+                    if (on) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            f32x4 acc[NT / 4];
+#pragma unroll
+                            for (int t = 0; t < NT; t += 4) acc[t / 4] = (f32x4){R.o[rt][t][c], R.o[rt][t + 1][c], R.o[rt][t + 2][c], R.o[rt][t + 3][c]};
+                            put(c, acc, R.m[rt], l);
+                        }
+                    }
+                } else {
+                    __shared__ Join<OP, WAVES> lds;
+                    __syncthreads();      // the join before this one has been read
+                    if (on) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+#pragma unroll
+                            for (int t = 0; t < NT; t += 4)
+                                lds.o[wave][c][lane][t / 4] = (f32x4){R.o[rt][t][c], R.o[rt][t + 1][c], R.o[rt][t + 2][c], R.o[rt][t + 3][c]};
+                        lds.ml[wave][lane] = make_float2(R.m[rt], l);
+                    }
+                    __syncthreads();
+                    if (on && wave < 4) {
+                        float M = -1e30f, L = 0.f;
+                        f32x4 acc[NT / 4];
+#pragma unroll
+                        for (int t = 0; t < NT / 4; ++t) acc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int s = 0; s < WAVES; ++s) M = fmaxf(M, lds.ml[s][lane].x);
+#pragma unroll
+                        for (int s = 0; s < WAVES; ++s) {
+                            const float2 ml = lds.ml[s][lane];
+                            const float a = __builtin_amdgcn_exp2f(ml.x - M);
+                            L = __builtin_fmaf(a, ml.y, L);
+#pragma unroll
+                            for (int t = 0; t < NT / 4; ++t)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) acc[t][e] = __builtin_fmaf(a, lds.o[s][wave][lane][t][e], acc[t][e]);
+                        }
+                        put(wave, acc, M, L);
                     }
                 }
             }
             if (!p.alone && seg_u == 0 && threadIdx.x == 0) {
-                const int64_t last = (int64_t)b.at + b.n - 1 + (b.units - b.u - b.n);      // the segment's last unit
-                *sharers_of<OP>(p, b.r, b.hd) = make_int2(wg, (int)(((last + 1) * sharers - 1) / total));
+                const int last = at + b.units - 1;      // the segment's last unit
+                *sharers_of<OP>(p, b.r, b.hd) = make_int2(wg, whole ? wg : cut.range_of(last));
             }
             R.clear();
-            seg_u = nb.u;
+            at += b.u + 1 - seg_u;      // of the next segment's first unit
+            seg_u = 0;
         }
         if (!more) break;
-        b = nb;
-        at = nat;
+        b = n1;
+        n1 = n2;
+        p1 = p2;
+        more = more2;
     }
 }
 
-// The records of one query row, joined in an order that the lengths fix: several ways take them in
-// turn, LANES lanes of four values each, and their sums are joined.
-template <class OP>
+// The records of ROWS query rows of a sequence and head, joined in an order that the lengths fix:
+// several ways take a row's records in turn, LANES lanes of four values each, and their sums are joined.
+template <class OP, int ROWS>
 __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p) {
-    constexpr int D = OP::DIM, LANES = D / 4, WAYS = 256 / LANES, BATCH = 4;
+    constexpr int D = OP::DIM, LANES = D / 4, WAYS = 256 / LANES / ROWS, BATCH = 4;
     __shared__ f32x4 sums[256];
-    __shared__ float2 mls[WAYS];
-    const int r = blockIdx.x / p.n_q_heads, h = blockIdx.x - r * p.n_q_heads;
-    const int kh = h / p.group, tile = (h - kh * p.group) / p.rows, row = h - kh * p.group - tile * p.rows;
-    int2 wgs = *sharers_of<OP>(p, r, kh * p.tiles + tile);
-    if (rows_of(p, p.len[r]) < 0 || wgs.x == wgs.y) return;
+    __shared__ float2 mls[WAYS * ROWS];
+    const int heads = p.n_kv_heads * p.tiles, groups = (p.rows + ROWS - 1) / ROWS;
+    const int seg = blockIdx.x / groups, r = seg / heads, hd = seg - r * heads;
+    int2 wgs = *sharers_of<OP>(p, r, hd);
+    if (rows_of(p, scalar(p.len + r)) < 0 || wgs.x == wgs.y) return;
     wgs.x = max(wgs.x, 0);      // (anything, if the lengths are not what they were)
     wgs.y = min(wgs.y, p.grid - 1);
-    const int way = threadIdx.x / LANES, d = threadIdx.x % LANES * 4;
+    const int slot = threadIdx.x / LANES, way = slot / ROWS, d = threadIdx.x % LANES * 4;
+    const int kh = hd / p.tiles, row0 = (hd - kh * p.tiles) * p.rows, rows = min(p.rows, p.group - row0);
+    const int at = (blockIdx.x - seg * groups) * ROWS + slot % ROWS, row = min(at, rows - 1);
     float M = -1e30f, l = 0.f;
     f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
     for (int s0 = wgs.x + way; s0 <= wgs.y; s0 += WAYS * BATCH) {
@@ -536,41 +588,44 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p)
         }
     }
     sums[threadIdx.x] = acc;
-    if (d == 0) mls[way] = make_float2(M, l);
+    if (d == 0) mls[slot] = make_float2(M, l);
     __syncthreads();
-    if (way) return;
+    if (way || at >= rows) return;
     float top = M;
 #pragma unroll
-    for (int s = 1; s < WAYS; ++s) top = fmaxf(top, mls[s].x);
+    for (int s = 1; s < WAYS; ++s) top = fmaxf(top, mls[s * ROWS + slot].x);
     const float a = __builtin_amdgcn_exp2f(M - top);
     l *= a;
     acc *= a;
 #pragma unroll
     for (int s = 1; s < WAYS; ++s) {
-        const float2 ml = mls[s];
+        const float2 ml = mls[s * ROWS + slot];
         const float f = __builtin_amdgcn_exp2f(ml.x - top);
         l = __builtin_fmaf(f, ml.y, l);
-        const f32x4 x = sums[s * LANES + threadIdx.x];
+        const f32x4 x = sums[s * ROWS * LANES + threadIdx.x];
 #pragma unroll
         for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(f, x[c], acc[c]);
     }
     const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-    OP::put4((unsigned char *)p.out + ((int64_t)r * p.n_q_heads + h) * OP::ROWB, d, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+    const int64_t to = (int64_t)r * p.n_q_heads + kh * p.group + row0 + row;
+    OP::put4((unsigned char *)p.out + to * OP::ROWB, d, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
 }
 
 template <class OP>
 hipError_t launch_op(const DecodeParams &p, hipStream_t s) {
     const dim3 grid((unsigned)p.grid);
-    if (p.alone) {
-        if (p.rows > 16) hipLaunchKernelGGL((decode_kernel<OP, 2, ALONE_WAVES>), grid, dim3(64 * ALONE_WAVES), 0, s, p);
-        else hipLaunchKernelGGL((decode_kernel<OP, 1, ALONE_WAVES>), grid, dim3(64 * ALONE_WAVES), 0, s, p);
-        return hipGetLastError();
-    }
-    if (p.rows > 16) hipLaunchKernelGGL((decode_kernel<OP, 2, SHARED_WAVES>), grid, dim3(64 * SHARED_WAVES), 0, s, p);
-    else hipLaunchKernelGGL((decode_kernel<OP, 1, SHARED_WAVES>), grid, dim3(64 * SHARED_WAVES), 0, s, p);
+    auto go = [&](auto waves) {
+        constexpr int W = decltype(waves)::value;
+        if (p.rows > 16) hipLaunchKernelGGL((decode_kernel<OP, 2, W>), grid, dim3(64 * W), 0, s, p);
+        else hipLaunchKernelGGL((decode_kernel<OP, 1, W>), grid, dim3(64 * W), 0, s, p);
+    };
+    if (p.waves == 4) go(std::integral_constant<int, 4>());
+    else go(std::integral_constant<int, 1>());
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(decode_merge_kernel<OP>, dim3((unsigned)(p.n * p.n_q_heads)), dim3(256), 0, s, p);
+    if (e != hipSuccess || p.alone) return e;
+    const int segs = p.n * p.n_kv_heads * p.tiles;
+    if (p.merge_rows == 1) hipLaunchKernelGGL((decode_merge_kernel<OP, 1>), dim3((unsigned)(segs * p.rows)), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((decode_merge_kernel<OP, 4>), dim3((unsigned)(segs * ((p.rows + 3) / 4))), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 

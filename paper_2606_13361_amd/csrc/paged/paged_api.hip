@@ -105,13 +105,14 @@ int check_page_pointers(const kvr_pages *g) {
 }
 
 // ---- decode
-// Two workgroups a compute unit
-constexpr int64_t kSharers = 2 * kCus;
-// Units up to which a sequence and head is one workgroup's and nothing is joined
-constexpr int64_t kAloneUnits = 4;
+constexpr int64_t kSharers = 4 * kCus;      // waves that share the units out
+constexpr int64_t kAloneBytes = 160 << 10, kManyHeads = 256, kManyAloneBytes = 512 << 10;
+constexpr int64_t kOneWaveHeads = 2048, kOneWaveBytes = 256 << 10;
+constexpr int64_t kOneWaveStages = 32;
 
 struct DecodePlan {
     int64_t tiles, rows, grid;
+    int waves, merge_rows;
     bool alone;
     size_t ws_bytes;
 };
@@ -119,16 +120,24 @@ struct DecodePlan {
 bool plan_decode(const kvr_desc *d, int64_t n, int64_t max_len, DecodePlan *out) {
     DecodePlan s;
     memset(&s, 0, sizeof s);
-    const int64_t G = d->n_q_heads / d->n_kv_heads, unit = d->dtype == KVR_F32 ? kUnitKeysF32 : kUnitKeys;
+    const int64_t G = d->n_q_heads / d->n_kv_heads, stage = d->dtype == KVR_F32 ? kStageKeysF32 : kStageKeys;
     s.rows = G < 32 ? G : 32;
     s.tiles = ceil_div(G, 32);
     if (n > kMaxGrid / d->n_kv_heads / s.tiles || n > kMaxGrid / d->n_q_heads) return false;
     const int64_t heads = n * d->n_kv_heads * s.tiles;
-    const int64_t units = max_len > 0 ? ceil_div(max_len, unit) : 1;
-    if (heads > 0 && units > kMaxRows / heads) return false;
-    s.alone = units <= kAloneUnits;
-    s.grid = s.alone ? heads : units * heads < kSharers ? units * heads : kSharers;
-    if (!s.alone) s.ws_bytes = (size_t)(2 * s.grid * s.rows * (d->head_dim + 2)) * sizeof(float) + (size_t)heads * 8;
+    const int64_t stages = max_len > 0 ? ceil_div(max_len, stage) : 1;
+    if (heads > 0 && stages > kMaxRows / heads) return false;
+    const int64_t bytes = stages * stage * d->head_dim * elt_bytes(d) * 2;      // of one of them, at most
+    s.alone = bytes <= (heads >= kManyHeads ? kManyAloneBytes : kAloneBytes);
+    if (s.alone) s.waves = heads >= kOneWaveHeads && bytes <= kOneWaveBytes ? 1 : 4;
+    else s.waves = stages <= kOneWaveStages ? 1 : 4;
+    s.merge_rows = heads >= kManyHeads ? 4 : 1;
+    const int64_t units = ceil_div(stages, s.waves) * heads;
+    s.grid = s.alone ? heads : units < kSharers / s.waves ? units : kSharers / s.waves;
+    // (single waves have more records than workgroups of four: room for what a shorter max_len needs, too)
+    const int64_t one = (stages < kOneWaveStages ? stages : kOneWaveStages) * heads, most = one < kSharers ? one : kSharers;
+    const int64_t sharers = heads >= kManyHeads || s.grid > most ? s.grid : most;
+    if (!s.alone) s.ws_bytes = (size_t)(2 * sharers * s.rows * (d->head_dim + 2)) * sizeof(float) + (size_t)heads * 8;
     *out = s;
     return true;
 }
@@ -234,7 +243,8 @@ int kvr_paged_decode(const kvr_desc *desc, const kvr_pages *pages, const kvr_row
     p.out = out;
     p.kp = (const unsigned char *)pages->k; p.vp = (const unsigned char *)pages->v;
     p.page_bytes = pages->page_stride * elt_bytes(desc);
-    p.table = pages->table; p.len = len;
+    p.table = pages->max_pages ? pages->table : len;      // (no rows then: what is read is not used)
+    p.len = len;
     p.ws = (float *)ws;
     p.n = n;
     p.n_new = n_new;
@@ -248,6 +258,8 @@ int kvr_paged_decode(const kvr_desc *desc, const kvr_pages *pages, const kvr_row
     p.tiles = (int32_t)plan.tiles;
     p.rows = (int32_t)plan.rows;
     p.grid = (int32_t)plan.grid;
+    p.waves = plan.waves;
+    p.merge_rows = plan.merge_rows;
     p.alone = plan.alone ? 1 : 0;
     // part / (parts of a page), exact for the parts of 2^31 rows: with 2^b parts or more, ceil(2^(32 + b) / parts)
     // is less than 2^b too large in 2^(32 + b), and a part is below 2^28

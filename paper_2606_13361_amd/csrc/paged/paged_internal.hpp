@@ -50,13 +50,15 @@ struct DecodeParams {
     int32_t tiles;           // of 16 (32) query rows of a kv head
     int32_t rows;            // of a record
     int32_t grid;            // workgroups that share the units
+    int32_t waves;           // of a workgroup
+    int32_t merge_rows;      // query rows of a workgroup that joins records, 1 or 4
     int32_t alone;           // a workgroup takes one sequence and head, nothing is joined
     uint32_t part_shift;     // 16-row parts of a page, as a divisor: (part * part_mul) >> part_shift
     uint64_t part_mul;
     float scale_log2;
 };
-// keys of a unit of work, one stage for each of the workgroup's four waves
-constexpr int kUnitKeys = 128, kUnitKeysF32 = 64;
+// keys of a wave's stage: a unit of work is one for each of the workgroup's 1 or 4 waves
+constexpr int kStageKeys = 32, kStageKeysF32 = 16;
 hipError_t launch_decode(const DecodeParams &p, int head_dim, int dtype, hipStream_t s);
 
 }  // namespace kvr
