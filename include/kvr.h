@@ -475,7 +475,8 @@ typedef struct {
 
 /*
  * Rows of tokens with strides: head h of token t is the head_dim elements at
- * data + t * token_stride + h * head_stride (both >= 0 and multiples of 16 bytes).  The q
+ * data + t * token_stride + h * head_stride (both >= 0 and multiples of 16 bytes; that of a
+ * single token, or head, is not used).  The q
  * rows of a fused projection [tokens][(n_q_heads + 2 n_kv_heads) head_dim] have
  * token_stride (n_q_heads + 2 n_kv_heads) head_dim and head_stride head_dim; a dense cache
  * [n_kv_heads][capacity][head_dim] has head_dim and capacity * head_dim.  Rows that a call

@@ -33,9 +33,12 @@ int to_status(hipError_t e) { return e == hipSuccess ? KVR_OK : KVR_ERR_DEVICE; 
 // the other's, or one head's.
 int check_rows(const kvr_desc *d, const kvr_rows *r, int64_t n_tok, int64_t heads, bool out) {
     const int64_t D = d->head_dim, by = 16 / elt_bytes(d);
-    if (r->token_stride < 0 || r->head_stride < 0 || r->token_stride > kMaxStride || r->head_stride > kMaxStride) return KVR_ERR_SHAPE;
-    if (r->token_stride > kMaxExtent / n_tok || r->head_stride > kMaxExtent / heads) return KVR_ERR_SHAPE;
-    if (r->token_stride % by || r->head_stride % by) return KVR_ERR_ALIGN;
+    const struct { int64_t stride, n; } dims[] = {{r->token_stride, n_tok}, {r->head_stride, heads}};
+    for (const auto &x : dims) {
+        if (x.n <= 1) continue;      // the stride of a single one is not used
+        if (x.stride < 0 || x.stride > kMaxStride || x.stride > kMaxExtent / x.n) return KVR_ERR_SHAPE;
+        if (x.stride % by) return KVR_ERR_ALIGN;
+    }
     if (!r->data) return KVR_ERR_NULL;
     if (!aligned(r->data, 16)) return KVR_ERR_ALIGN;
     if (!out) return KVR_OK;
@@ -105,10 +108,30 @@ int check_page_pointers(const kvr_pages *g) {
 }
 
 // ---- decode
-constexpr int64_t kSharers = 4 * kCus;      // waves that share the units out
-constexpr int64_t kAloneBytes = 160 << 10, kManyHeads = 256, kManyAloneBytes = 512 << 10;
-constexpr int64_t kOneWaveHeads = 2048, kOneWaveBytes = 256 << 10;
+// All in a captured graph, us a call, 16-bit, 32 / 8 heads of 128 where nothing else is said ("16 / 2":
+// heads of 64); a stage is a wave's 16 KB of keys and values (8 KB at 64).
+//
+// Waves that share the units out: as many as ask for this much at once on a compute unit.  32, 64 and
+// 128 KB: one sequence of 32768 rows 33.5, 29.7 and 30.8, 64 of 100 to 4096 125, 105 and 107, of 300 to
+// 32768 829, 754 and 763; 16 / 2, 64 of 100 to 3900 21.2, 20.8 and 22.0.
+constexpr int64_t kAskedBytes = 64 << 10;
+// A sequence and head of at most this many bytes is one workgroup's of four waves, and nothing is joined:
+// 160 KB, more where there are many of them, as far as one long sequence among short ones does not hold the
+// others up for long.  In one launch and shared out: 1 sequence of 250 rows (128 KB) 5.7 and 6.7, 310 6.4
+// and 6.8, 480 7.8 and 7.0; 8 of 20 to 300 7.5 and 8.1, to 480 (240 KB) 8.9 and 8.5; 31 of 10 to 480 10.2
+// and 13.1, 32 of 10 to 980 (496 KB) 18.5 and 20.3, 64 of 100 to 1500 (752 KB) 47.4 and 46.3; 16 / 2, 64 of 10
+// to 900 (232 KB) 9.8 and 11.0; fp32, 8 of 10 to 150 (160 KB) 9.1 and 8.5, 64 of 10 to 480 (480 KB) 34.2 and 33.9.
+constexpr int64_t kAloneBytes = 160 << 10, kAloneMost = 512 << 10, kAloneByHeads = 2 << 10;
+// One wave instead of four, where many of them are short: 128 sequences of 10 to 200 rows 16.7 instead of 18.1, 256
+// 27.3 instead of 30.1, 256 of 10 to 480 (240 KB) 56.6 and 55.4; 64 of 10 to 250 12.5 and 11.3.
+constexpr int64_t kOneWaveHeads = 1024, kOneWaveBytes = 128 << 10;
+// Shared out, ranges of one wave up to this many stages of a sequence, of four beyond (records of which
+// there are fewer): 1 sequence of 480 rows 7.0 and 7.9, 980 (31 stages) 7.6 and 8.6, 1500 8.7 and 8.8, 3774
+// 11.6 and 9.8; 8 of 100 to 980 11.0 and 11.2.
 constexpr int64_t kOneWaveStages = 32;
+// Records are joined a query row a workgroup, or four where there are many: 1 and 4, one sequence of 3774
+// rows 9.8 and 11.7, 16 of 100 to 3980 32.1 and 31.8, 32 56.6 and 56.0, 1000 of 10 to 200 134 and 121.
+constexpr int64_t kMergeHeads = 128;
 
 struct DecodePlan {
     int64_t tiles, rows, grid;
@@ -127,16 +150,18 @@ bool plan_decode(const kvr_desc *d, int64_t n, int64_t max_len, DecodePlan *out)
     const int64_t heads = n * d->n_kv_heads * s.tiles;
     const int64_t stages = max_len > 0 ? ceil_div(max_len, stage) : 1;
     if (heads > 0 && stages > kMaxRows / heads) return false;
-    const int64_t bytes = stages * stage * d->head_dim * elt_bytes(d) * 2;      // of one of them, at most
-    s.alone = bytes <= (heads >= kManyHeads ? kManyAloneBytes : kAloneBytes);
+    const int64_t stage_bytes = stage * d->head_dim * elt_bytes(d) * 2, bytes = stages * stage_bytes;      // of a sequence and head, at most
+    const int64_t waves = kAskedBytes / stage_bytes * kCus;
+    const int64_t by_heads = heads * kAloneByHeads < kAloneMost ? heads * kAloneByHeads : kAloneMost;
+    s.alone = bytes <= (by_heads > kAloneBytes ? by_heads : kAloneBytes);
     if (s.alone) s.waves = heads >= kOneWaveHeads && bytes <= kOneWaveBytes ? 1 : 4;
     else s.waves = stages <= kOneWaveStages ? 1 : 4;
-    s.merge_rows = heads >= kManyHeads ? 4 : 1;
+    s.merge_rows = heads >= kMergeHeads ? 4 : 1;
     const int64_t units = ceil_div(stages, s.waves) * heads;
-    s.grid = s.alone ? heads : units < kSharers / s.waves ? units : kSharers / s.waves;
+    s.grid = s.alone ? heads : units < waves / s.waves ? units : waves / s.waves;
     // (single waves have more records than workgroups of four: room for what a shorter max_len needs, too)
-    const int64_t one = (stages < kOneWaveStages ? stages : kOneWaveStages) * heads, most = one < kSharers ? one : kSharers;
-    const int64_t sharers = heads >= kManyHeads || s.grid > most ? s.grid : most;
+    const int64_t one = (stages < kOneWaveStages ? stages : kOneWaveStages) * heads, most = one < waves ? one : waves;
+    const int64_t sharers = s.grid > most ? s.grid : most;
     if (!s.alone) s.ws_bytes = (size_t)(2 * sharers * s.rows * (d->head_dim + 2)) * sizeof(float) + (size_t)heads * 8;
     *out = s;
     return true;

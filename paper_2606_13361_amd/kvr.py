@@ -675,30 +675,33 @@ class PagedCache:
         tp = _at(table, "table", torch.int32, table.shape, dev)
         self.k, self.v, self.table = k, v, table
         self.device, self.n, self.reach = dev, table.shape[0], table.shape[1] * ps
-        self.geometry = (desc.n_kv_heads, desc.head_dim, desc.dtype)
+        self.kv_heads, self.head_dim, self.dtype = desc.n_kv_heads, desc.head_dim, desc.dtype
         self._c = kvr_pages(k.data_ptr(), v.data_ptr(), stride[0], n_pages, ps, tp, table.shape[1], 0)
 
-    def c(self, desc):
-        if self.geometry != (desc.n_kv_heads, desc.head_dim, desc.dtype):
+    def c(self, kv_heads, head_dim, dtype):
+        if kv_heads != self.kv_heads or head_dim != self.head_dim or dtype != self.dtype:
             raise ValueError("the cache has kv heads, head_dim, dtype %s, the descriptor %s"
-                             % (self.geometry, (desc.n_kv_heads, desc.head_dim, desc.dtype)))
-        return ctypes.byref(self._c)
+                             % ((self.kv_heads, self.head_dim, self.dtype), (kv_heads, head_dim, dtype)))
+        return _byref(self._c)
 
 
-def _cache(cache, desc):
+_byref = ctypes.byref
+
+
+def _cache(cache, kv_heads, head_dim, dtype):
     if not isinstance(cache, PagedCache):
         raise ValueError("cache must be a PagedCache")
-    return cache.c(desc)
+    return cache.c(kv_heads, head_dim, dtype)
 
 
 def _rows(t, name, dt, shape, dev):
-    """Rows [tokens, heads, head_dim] of any token and head stride."""
+    """Rows [tokens, heads, head_dim] of any token and head stride.  One expression where all is well: a
+    small call is bound by its checks on the host."""
     try:
-        if t.dtype is dt and t.get_device() == dev and t.shape == shape:
-            st, sh, s1 = t.stride()
-            if s1 == 1:
-                return ctypes.byref(kvr_rows(t.data_ptr(), st, sh))
-    except AttributeError:      # no tensor
+        st, sh, one = t.stride()
+        if one == 1 and t.dtype is dt and t.shape == shape and t.get_device() == dev:
+            return _byref(kvr_rows(t.data_ptr(), st, sh))
+    except (AttributeError, TypeError, ValueError):      # no tensor, or of another rank
         pass
     _device(t, name)
     if t.dtype != dt:
@@ -708,6 +711,18 @@ def _rows(t, name, dt, shape, dev):
     if t.shape != shape:
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), shape))
     raise ValueError("%s: the elements of a row must be contiguous" % name)
+
+
+def _vector(t, name, dtype, n, dev):
+    """_at of a tensor of n values, or None"""
+    if t is None:
+        return None
+    try:
+        if t.dtype is dtype and t.shape == (n,) and t.get_device() == dev and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:      # no tensor
+        pass
+    return _at(t, name, dtype, (n,), dev)
 
 
 def _rope_at(rope, desc, dev):
@@ -725,7 +740,7 @@ def kvr_qk_norm_rope(desc, q, k, q_out=None, k_out=None, rope=None, q_norm=None,
     head_dim] (views with any token and head stride; either may be None) into q_out and k_out
     (default: in place).  q_norm, k_norm: weights [head_dim] or None; rope: a RopeTable or
     None; pos: int32 GPU tensor [n_tok], or token t is at pos0 + t."""
-    d, dt = desc.head_dim, _TORCH_DTYPE.get(desc.dtype)
+    Hq, Hkv, d, dt = desc.n_q_heads, desc.n_kv_heads, desc.head_dim, _TORCH_DTYPE.get(desc.dtype)
     some = k if q is None else q
     dev = _device(some, "k" if q is None else "q")
     if some.dim() != 3:
@@ -733,20 +748,18 @@ def kvr_qk_norm_rope(desc, q, k, q_out=None, k_out=None, rope=None, q_norm=None,
     n = some.shape[0]
     qi = qo = ki = ko = None
     if q is not None:
-        qi = _rows(q, "q", dt, (n, desc.n_q_heads, d), dev)
-        qo = qi if q_out is None else _rows(q_out, "q_out", dt, (n, desc.n_q_heads, d), dev)
+        qi = _rows(q, "q", dt, (n, Hq, d), dev)
+        qo = qi if q_out is None else _rows(q_out, "q_out", dt, (n, Hq, d), dev)
     elif q_out is not None:
         raise ValueError("q_out without q")
     if k is not None:
-        ki = _rows(k, "k", dt, (n, desc.n_kv_heads, d), dev)
-        ko = ki if k_out is None else _rows(k_out, "k_out", dt, (n, desc.n_kv_heads, d), dev)
+        ki = _rows(k, "k", dt, (n, Hkv, d), dev)
+        ko = ki if k_out is None else _rows(k_out, "k_out", dt, (n, Hkv, d), dev)
     elif k_out is not None:
         raise ValueError("k_out without k")
-    qn = None if q_norm is None else _at(q_norm, "q_norm", dt, (d,), dev)
-    kn = None if k_norm is None else _at(k_norm, "k_norm", dt, (d,), dev)
-    ps = None if pos is None else _at(pos, "pos", torch.int32, (n,), dev)
-    rp = _rope_at(rope, desc, dev)
-    _launch(lambda s: load().kvr_qk_norm_rope(ctypes.byref(desc), rp, qi, ki, qn, kn, eps, n, ps, int(pos0), qo, ko, s),
+    qn, kn = _vector(q_norm, "q_norm", dt, d, dev), _vector(k_norm, "k_norm", dt, d, dev)
+    at, rp = _vector(pos, "pos", torch.int32, n, dev), _rope_at(rope, desc, dev)
+    _launch(lambda s: load().kvr_qk_norm_rope(_byref(desc), rp, qi, ki, qn, kn, eps, n, at, int(pos0), qo, ko, s),
             "kvr_qk_norm_rope", stream, dev)
 
 
@@ -758,27 +771,25 @@ def kvr_paged_append(desc, cache, k, v, length, rope=None, cu_seqlens=None, pos=
     place).  length: int32 GPU tensor [n], rows that each sequence has; cu_seqlens: int32 GPU
     tensor [n + 1] of the packed tokens' sequences (None: one token each); pos: int32 GPU
     tensor [n_tok] of positions (None: the rows)."""
-    d, dt = desc.head_dim, _TORCH_DTYPE.get(desc.dtype)
-    pages = _cache(cache, desc)
-    dev, n = cache.device, cache.n
+    Hkv, d, code = desc.n_kv_heads, desc.head_dim, desc.dtype
+    pages = _cache(cache, Hkv, d, code)
+    dt, dev, n = _TORCH_DTYPE[code], cache.device, cache.n
     if not isinstance(k, torch.Tensor) or k.dim() != 3:
         raise ValueError("k must be a tensor [n_tok, n_kv_heads, head_dim]")
     T = k.shape[0]
-    ki = _rows(k, "k", dt, (T, desc.n_kv_heads, d), dev)
-    vi = _rows(v, "v", dt, (T, desc.n_kv_heads, d), dev)
+    ki, vi = _rows(k, "k", dt, (T, Hkv, d), dev), _rows(v, "v", dt, (T, Hkv, d), dev)
     qi = qo = None
     if q is not None:
-        qi = _rows(q, "q", dt, (T, desc.n_q_heads, d), dev)
-        qo = qi if q_out is None else _rows(q_out, "q_out", dt, (T, desc.n_q_heads, d), dev)
+        shape = (T, desc.n_q_heads, d)
+        qi = _rows(q, "q", dt, shape, dev)
+        qo = qi if q_out is None else _rows(q_out, "q_out", dt, shape, dev)
     elif q_out is not None or q_norm is not None:
         raise ValueError("q_out or q_norm without q")
-    qn = None if q_norm is None else _at(q_norm, "q_norm", dt, (d,), dev)
-    kn = None if k_norm is None else _at(k_norm, "k_norm", dt, (d,), dev)
+    qn, kn = _vector(q_norm, "q_norm", dt, d, dev), _vector(k_norm, "k_norm", dt, d, dev)
     ln = _at(length, "length", torch.int32, (n,), dev)
-    cu = None if cu_seqlens is None else _at(cu_seqlens, "cu_seqlens", torch.int32, (n + 1,), dev)
-    ps = None if pos is None else _at(pos, "pos", torch.int32, (T,), dev)
+    cu, at = _vector(cu_seqlens, "cu_seqlens", torch.int32, n + 1, dev), _vector(pos, "pos", torch.int32, T, dev)
     rp = _rope_at(rope, desc, dev)
-    _launch(lambda s: load().kvr_paged_append(ctypes.byref(desc), pages, rp, ki, vi, qi, qn, kn, eps, n, T, cu, ln, ps, qo, s),
+    _launch(lambda s: load().kvr_paged_append(_byref(desc), pages, rp, ki, vi, qi, qn, kn, eps, n, T, cu, ln, at, qo, s),
             "kvr_paged_append", stream, dev)
 
 
@@ -795,12 +806,13 @@ def kvr_paged_decode(desc, cache, q, length, out, ws=None, n_new=0, max_len=None
     """Attention of one token of each sequence, q [n, n_q_heads, head_dim] (a view with any
     token and head stride), into out, over rows [0, length + n_new) of a PagedCache.  length: int32 GPU tensor [n]; max_len: no sequence
     has more rows (default: all that the page table holds)."""
-    pages = _cache(cache, desc)
-    dev, n = cache.device, cache.n
-    dt, shape = _TORCH_DTYPE.get(desc.dtype), (n, desc.n_q_heads, desc.head_dim)
+    Hkv, d, code = desc.n_kv_heads, desc.head_dim, desc.dtype
+    pages = _cache(cache, Hkv, d, code)
+    dt, dev, n = _TORCH_DTYPE[code], cache.device, cache.n
+    shape = (n, desc.n_q_heads, d)
     qi, o = _rows(q, "q", dt, shape, dev), _at(out, "out", dt, shape, dev)
     ln = _at(length, "length", torch.int32, (n,), dev)
     wp, wn = _scratch(ws, dev)
-    most = int(cache.reach if max_len is None else max_len)
-    _launch(lambda s: load().kvr_paged_decode(ctypes.byref(desc), pages, qi, n, ln, int(n_new), most, o, wp, wn, s),
+    most = cache.reach if max_len is None else int(max_len)
+    _launch(lambda s: load().kvr_paged_decode(_byref(desc), pages, qi, n, ln, int(n_new), most, o, wp, wn, s),
             "kvr_paged_decode", stream, dev)

@@ -160,13 +160,46 @@ def test_ragged_batches(dt, n):
         b.check(t)
 
 
-def test_many_sequences():
+@pytest.mark.parametrize("max_pages", [None, 400], ids=["one_launch", "shared_out"])
+def test_many_sequences(max_pages):
     """More sequences than two rounds of the search take one by one."""
     n = 4500
     rows = [(37 * r) % 29 - 3 for r in range(n)]
     rows[4200] = 1100
-    b = Batch(BF16, (4, 1, 64), 16, rows, seed=1)
+    b = Batch(BF16, (4, 1, 64), 16, rows, seed=1, max_pages=max_pages)
     t = b.gpu()
+    assert (t["ws"].numel() > 0) == (max_pages is not None)
+    b.call(t)
+    b.check(t)
+
+
+# max_len of the ways of a call of 6 sequences of at most 150 rows, by the bytes of a sequence and head: one launch
+# of four waves each, ranges of one wave, ranges of four
+WAYS = {"one_launch": 160, "ranges_of_a_wave": 1024, "ranges_of_four": 3200}
+
+
+@DTYPES
+@pytest.mark.parametrize("heads", [(8, 2, 128), (8, 2, 64), (20, 1, 128), (40, 1, 64)], ids=lambda h: "%d_%d_%d" % h)
+@pytest.mark.parametrize("way", WAYS)
+def test_each_way(dt, heads, way):
+    reach = WAYS[way] // (2 if dt == F32 else 1)
+    rows = [reach // (7 if way == "one_launch" else 3), 150, 0, -1, 33, 64]
+    if way != "one_launch":
+        rows[4] = reach
+    b = Batch(dt, heads, 16, [min(m, reach) for m in rows], seed=reach, max_pages=reach // 16)
+    t = b.gpu()
+    assert (t["ws"].numel() > 0) == (way != "one_launch")
+    b.call(t)
+    b.check(t)
+
+
+@DTYPES
+@pytest.mark.parametrize("heads", [(8, 8, 64), (8, 4, 128), (68, 2, 64)], ids=lambda h: "%d_%d_%d" % h)
+def test_a_wave_for_each_of_many_short_ones(dt, heads):
+    n = 1024 // heads[1] + 3
+    b = Batch(dt, heads, 16, [(r * 13) % 61 - 1 for r in range(n)], seed=2)
+    t = b.gpu()
+    assert t["ws"].numel() == 0
     b.call(t)
     b.check(t)
 
