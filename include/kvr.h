@@ -501,7 +501,7 @@ typedef struct {
  *   token t is at pos0 + t.  rope->n_pos >= pos0 + n_tok (KVR_ERR_POSITION); with pos, a
  *   token whose position has no entry is left out (its rows of q_out and k_out stay as
  *   they were).
- * Limits: n_q_heads + n_kv_heads at most 65535, n_tok below 2^29 is served.
+ * Limits: n_q_heads + n_kv_heads at most 65535, n_tok below 2^26 is served (KVR_ERR_SHAPE).
  */
 int kvr_qk_norm_rope(const kvr_desc *desc, const kvr_rope *rope, const kvr_rows *q, const kvr_rows *k, const void *q_norm,
                      const void *k_norm, float eps, int64_t n_tok, const int32_t *pos, int64_t pos0, const kvr_rows *q_out,
@@ -524,7 +524,8 @@ int kvr_qk_norm_rope(const kvr_desc *desc, const kvr_rope *rope, const kvr_rows 
  * sequence has len[r] < 0 (an empty slot of the batch), if it is padding, if its row lies
  * behind the table's last page or in no page of the pool, or if its position has no entry in the
  * rotary table.  Two tokens of a call must not have the same row of the same page.
- * Limits: n_q_heads + 2 n_kv_heads at most 65535, n_tok below 2^29 is served.
+ * Limits: n_q_heads + 2 n_kv_heads at most 65535, n below 2^24, n_tok below 2^26 is served
+ * (KVR_ERR_SHAPE).
  */
 int kvr_paged_append(const kvr_desc *desc, const kvr_pages *pages, const kvr_rope *rope, const kvr_rows *k, const kvr_rows *v,
                      const kvr_rows *q, const void *q_norm, const void *k_norm, float eps, int32_t n, int64_t n_tok,
@@ -548,8 +549,9 @@ int kvr_paged_append(const kvr_desc *desc, const kvr_pages *pages, const kvr_rop
  * Scores, weights and sums in fp32; 16-bit weights enter the second product as two operands,
  * a cut weight and what the cut left over.  Results are the same bit for bit
  * for the same lengths of the whole batch.
- * Limits: n n_q_heads below 2^24 and n n_kv_heads max_len below 2^37 are served (KVR_ERR_SHAPE
- * far beyond).
+ * out must not overlap the other arguments.
+ * Limits: max_len at most 2^30; n n_q_heads below 2^24 and n n_q_heads max_len below 2^35 are
+ * served (KVR_ERR_SHAPE).
  */
 int kvr_paged_decode(const kvr_desc *desc, const kvr_pages *pages, const kvr_rows *q, int32_t n, const int32_t *len, int32_t n_new,
                      int64_t max_len, void *out, void *ws, size_t ws_bytes, void *stream);

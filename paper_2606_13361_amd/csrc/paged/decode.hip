@@ -19,6 +19,8 @@
 // do not wait behind the keys and values that are on their way.
 //
 // HBM bounds it: 4 G operations for each byte of 16-bit keys and values, G query heads to a kv head.
+#include <float.h>
+
 #include "paged/paged_internal.hpp"
 #include "readers/attn_direct.hpp"
 
@@ -109,7 +111,7 @@ __device__ __forceinline__ int rows_of(const DecodeParams &p, int32_t len) {
 // Units of a sequence (of each of its heads): an empty one has one, which finds no keys
 template <int UNIT>
 __device__ __forceinline__ int units_of(int rows) {
-    return rows < 0 ? 0 : rows == 0 ? 1 : (rows + UNIT - 1) / UNIT;
+    return rows < 0 ? 0 : rows == 0 ? 1 : (rows - 1) / UNIT + 1;
 }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -315,7 +317,7 @@ struct Rows {
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            m[rt] = -1e30f;
+            m[rt] = -FLT_MAX;
             l[rt] = 0.f;
 #pragma unroll
             for (int t = 0; t < OP::NT; ++t) o[rt][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -397,7 +399,7 @@ struct Join {
 };
 
 template <class OP, int RT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, RT > 1 ? 1 : 2) void decode_kernel(const DecodeParams p) {
+__global__ __launch_bounds__(64 * WAVES, 2) void decode_kernel(const DecodeParams p) {
     constexpr int NT = OP::NT;
     using St = Stage<OP, WAVES>;
     const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : uniform(threadIdx.x >> 6);
@@ -504,7 +506,7 @@ __global__ __launch_bounds__(64 * WAVES, RT > 1 ? 1 : 2) void decode_kernel(cons
                     }
                     __syncthreads();
                     if (on && wave < 4) {
-                        float M = -1e30f, L = 0.f;
+                        float M = -FLT_MAX, L = 0.f;
                         f32x4 acc[NT / 4];
 #pragma unroll
                         for (int t = 0; t < NT / 4; ++t) acc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -556,7 +558,7 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p)
     const int slot = threadIdx.x / LANES, way = slot / ROWS, d = threadIdx.x % LANES * 4;
     const int kh = hd / p.tiles, row0 = (hd - kh * p.tiles) * p.rows, rows = min(p.rows, p.group - row0);
     const int at = (blockIdx.x - seg * groups) * ROWS + slot % ROWS, row = min(at, rows - 1);
-    float M = -1e30f, l = 0.f;
+    float M = -FLT_MAX, l = 0.f;
     f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
     for (int s0 = wgs.x + way; s0 <= wgs.y; s0 += WAYS * BATCH) {
         f32x4 x[BATCH];
@@ -565,7 +567,7 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p)
 #pragma unroll
         for (int s = 0; s < BATCH; ++s) {
             const int wg = s0 + s * WAYS;
-            w[s] = make_float2(-1e30f, 0.f);
+            w[s] = make_float2(-FLT_MAX, 0.f);
             x[s] = (f32x4){0.f, 0.f, 0.f, 0.f};
             if (wg <= wgs.y) {
                 const int64_t rec = 2 * (int64_t)wg + (wg == wgs.x ? 1 : 0);

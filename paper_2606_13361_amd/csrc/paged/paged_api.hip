@@ -14,6 +14,7 @@ constexpr int64_t kCus = 256;
 constexpr int64_t kMaxRows = 0x7fffffff;
 constexpr int64_t kMaxStride = (int64_t)1 << 40;      // elements
 constexpr int64_t kMaxExtent = (int64_t)1 << 60;      // elements of an array: bytes in 64 bits
+constexpr int64_t kMaxLen = (int64_t)1 << 30;           // rows of a sequence in decode: 32-bit on the device, with room for a unit
 constexpr int64_t kMaxHeads = 65535;                  // rows of a token
 constexpr int64_t kMaxGrid = ((int64_t)1 << 24) - 1;  // workgroups of a launch: 2^32 threads are too many
 
@@ -209,7 +210,7 @@ int kvr_paged_append(const kvr_desc *desc, const kvr_pages *pages, const kvr_rop
     int st = check_desc(desc);
     if (st) return st;
     if ((st = check_pages(desc, pages))) return st;
-    if (n < 0 || n_tok < 0 || n_tok > kMaxRows || (!cu_seqlens && n_tok != n) || !(eps >= 0.f) || isinf(eps)) return KVR_ERR_SHAPE;
+    if (n < 0 || n > kMaxGrid || n_tok < 0 || n_tok > kMaxRows || (!cu_seqlens && n_tok != n) || !(eps >= 0.f) || isinf(eps)) return KVR_ERR_SHAPE;
     if (n == 0 || n_tok == 0) return KVR_OK;
     if (!k || !v || !len || !q != !q_out || (q_norm && !q)) return KVR_ERR_NULL;
     if ((st = check_page_pointers(pages))) return st;
@@ -242,7 +243,7 @@ int kvr_paged_append(const kvr_desc *desc, const kvr_pages *pages, const kvr_rop
 
 size_t kvr_workspace_bytes_paged(const kvr_desc *desc, int32_t n, int64_t max_len) {
     DecodePlan s;
-    if (check_desc(desc) != KVR_OK || n < 0 || max_len < 0 || max_len > kMaxRows) return (size_t)-1;
+    if (check_desc(desc) != KVR_OK || n < 0 || max_len < 0 || max_len > kMaxLen) return (size_t)-1;
     return plan_decode(desc, n, max_len, &s) ? s.ws_bytes : (size_t)-1;
 }
 
@@ -251,7 +252,7 @@ int kvr_paged_decode(const kvr_desc *desc, const kvr_pages *pages, const kvr_row
     int st = check_desc(desc);
     if (st) return st;
     if ((st = check_pages(desc, pages))) return st;
-    if (n < 0 || n_new < 0 || max_len < 0 || max_len > kMaxRows) return KVR_ERR_SHAPE;
+    if (n < 0 || n_new < 0 || max_len < 0 || max_len > kMaxLen) return KVR_ERR_SHAPE;
     if (max_len > (int64_t)pages->max_pages * pages->page_size) return KVR_ERR_CAPACITY;
     DecodePlan plan;
     if (!plan_decode(desc, n, max_len, &plan)) return KVR_ERR_SHAPE;

@@ -284,6 +284,22 @@ def test_scores_far_apart(dt, reach):
     b.check(t)
 
 
+def test_scores_as_large_as_numbers_go():
+    """All scores are -2^120 or so: the largest of them has all the weight."""
+    b = Batch(F32, (2, 1, 64), 16, [40, 700])
+    b.q.zero_()
+    b.q[:, :, 0] = -2.0 ** 60
+    for r, m in enumerate(b.rows):
+        for j in range(-(-m // 16)):
+            b.kp[b.table[r, j], 0, :, 0] = 2.0 ** 62
+        b.kp[b.table[r, 1], 0, 5, 0] = 2.0 ** 61
+    t = b.gpu()
+    b.call(t)
+    torch.cuda.synchronize()
+    for r in range(2):
+        assert torch.equal(t["out"][r].cpu(), b.vp[b.table[r, 1], 0, 5].expand(2, 64))
+
+
 def test_largest_numbers():
     """A mean of the largest values is finite; an infinity where it has weight shows."""
     for dt, big in ((BF16, 3.3e38), (F16, 65504.0), (F32, 3.4e38)):
@@ -326,6 +342,22 @@ def test_offsets_beyond_32_bits():
     t["cache"] = kvr.PagedCache(b.desc, kp, vp, t["table"])
     b.call(t)
     b.check(t)
+
+
+def test_a_long_sequence():
+    """2^25 rows and some: one page over and over, so that every row counts alike and the mean is the page's.
+    A range has at most 2^25 / 1024 rows, 32 of which are one product: 1024 sums each off by 2^-24, twice,
+    and as many ranges joined; a row more or less is 2^-25."""
+    b = Batch(BF16, (4, 1, 64), 4096, [4096], spare=0)
+    page = int(b.table[0, 0])
+    b.table = torch.full((1, 8193), page, dtype=torch.int32)
+    t = b.gpu()
+    t["len"].fill_(8192 * 4096 + 5)
+    b.call(t)
+    torch.cuda.synchronize()
+    want, mass = P.decode(b.q, b.kp, b.vp, b.table.numpy(), [4096])
+    err = np.abs(P._f64(t["out"]) - want)
+    assert (err <= 1.1 * (2.0 ** -8 * np.abs(want) + mass * 2.0 ** -11)).all()
 
 
 def test_dense_cache_is_a_pool_of_one_page():

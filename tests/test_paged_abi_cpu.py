@@ -101,7 +101,7 @@ def test_pages_missing(lib):
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(n=-1), "SHAPE"), (dict(n_new=-1), "SHAPE"), (dict(most=-1), "SHAPE"), (dict(most=1 << 31), "SHAPE"),
+    (dict(n=-1), "SHAPE"), (dict(n_new=-1), "SHAPE"), (dict(most=-1), "SHAPE"), (dict(most=(1 << 30) + 1), "SHAPE"),
     (dict(n=1 << 24), "SHAPE"), (dict(most=81), "CAPACITY"), (dict(q=None), "NULL"), (dict(q=rows(32, data=None)), "NULL"), (dict(q=rows(32, head=-128)), "SHAPE"), (dict(out=None), "NULL"),
     (dict(ln=None), "NULL"), (dict(q=rows(32, data=MIS)), "ALIGN"), (dict(q=rows(32, token=4100)), "ALIGN"), (dict(out=MIS), "ALIGN"), (dict(ws=MIS), "ALIGN"), (dict(ln=A + 2), "ALIGN"),
 ])
@@ -126,7 +126,7 @@ def test_decode_workspace(lib):
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(n=-1), "SHAPE"), (dict(T=-1), "SHAPE"), (dict(T=1 << 31), "SHAPE"), (dict(cu=None), "SHAPE"), (dict(eps=-1.0), "SHAPE"),
+    (dict(n=-1), "SHAPE"), (dict(n=1 << 24), "SHAPE"), (dict(T=-1), "SHAPE"), (dict(T=1 << 31), "SHAPE"), (dict(cu=None), "SHAPE"), (dict(eps=-1.0), "SHAPE"),
     (dict(eps=float("nan")), "SHAPE"), (dict(eps=float("inf")), "SHAPE"),
     (dict(k=None), "NULL"), (dict(v=None), "NULL"), (dict(ln=None), "NULL"), (dict(q=None), "NULL"), (dict(qo=None), "NULL"),
     (dict(q=None, qo=None), "NULL"),      # norm weights without queries
@@ -167,6 +167,16 @@ def test_heads_that_the_kernels_do_not_count(lib):
     d = desc(n_q_heads=65536, n_kv_heads=1)
     wide = lambda: rows(65536)
     assert norm_rope(lib, d, q=wide(), qo=wide(), k=None, ko=None, kn=None) == kvr.KVR_ERR_SHAPE
+
+
+def test_the_stride_of_a_single_token_or_head_is_not_used(lib):
+    """Negative strides, which are a shape's error where they are used; what is checked behind them is not aligned."""
+    d = desc(n_q_heads=4, n_kv_heads=1)
+    one = lambda token=-3, head=-5: kvr.kvr_rows(A, token, head)
+    key = lambda n, **kw: norm_rope(lib, d, n=n, q=None, qo=None, qn=None, kn=MIS, k=one(**kw), ko=one(**kw))
+    assert decode(lib, d, n=1, q=one(head=128), out=MIS) == kvr.KVR_ERR_ALIGN
+    assert decode(lib, d, n=2, q=one(head=128), out=MIS) == kvr.KVR_ERR_SHAPE
+    assert key(1) == kvr.KVR_ERR_ALIGN and key(2, token=128) == kvr.KVR_ERR_ALIGN and key(2) == kvr.KVR_ERR_SHAPE
 
 
 def test_no_work(lib):
