@@ -47,16 +47,19 @@ struct Dec16 : Op16<E, D> {
     static constexpr float LIFT = std::is_same<E, F16>::value ? 12.f : 0.f;
     using W = Weights<B>;
     // part h of a stage
+    template <int HINT>
     __device__ static __forceinline__ void load_k(typename B::K &k, __amdgpu_buffer_rsrc_t r, int h, int i, int g) {
 #pragma unroll
-        for (int ks = 0; ks < B::NK; ++ks) k.f[h][ks] = buf_load16(r, B::ROWB * i + 16 * g + 64 * ks);
+        for (int ks = 0; ks < B::NK; ++ks)
+            k.f[h][ks] = __builtin_amdgcn_raw_buffer_load_b128(r, B::ROWB * i + 16 * g + 64 * ks, 0, HINT);
     }
+    template <int HINT>
     __device__ static __forceinline__ void load_v(typename B::V &v, __amdgpu_buffer_rsrc_t r, int h, int i, int g) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const uint32_t off = (4 * g + e) * B::ROWB + 2 * B::NT * i;
-            if constexpr (B::NT == 8) v.r[4 * h + e] = buf_load16(r, off);
-            else v.r[4 * h + e] = __builtin_amdgcn_raw_buffer_load_b64(r, (int)off, 0, 0);
+            const int off = (4 * g + e) * B::ROWB + 2 * B::NT * i;
+            if constexpr (B::NT == 8) v.r[4 * h + e] = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, HINT);
+            else v.r[4 * h + e] = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, HINT);
         }
     }
     __device__ static __forceinline__ void pack(W &w, const float (&p)[B::NS]) {
@@ -90,11 +93,21 @@ struct Dec32 : Op32<D> {
     static constexpr int PARTS = 1;
     static constexpr float LIFT = 0.f;
     using W = typename B::P;
+    template <int HINT>
     __device__ static __forceinline__ void load_k(typename B::K &k, __amdgpu_buffer_rsrc_t r, int, int i, int g) {
-        B::load_k(k, r, B::ROWB, i, g);
+#pragma unroll
+        for (int ks = 0; ks < B::NK; ++ks) k.f[ks] = load<HINT>(r, B::ROWB * i + 16 * g + 64 * ks);
     }
+    template <int HINT>
     __device__ static __forceinline__ void load_v(typename B::V &v, __amdgpu_buffer_rsrc_t r, int, int i, int g) {
-        B::load_v(v, r, B::ROWB, i, g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int j = 0; j < B::NT / 4; ++j) v.r[e][j] = load<HINT>(r, B::ROWB * (4 * g + e) + 4 * B::NT * i + 16 * j);
+    }
+    template <int HINT>
+    __device__ static __forceinline__ f32x4 load(__amdgpu_buffer_rsrc_t r, int off) {
+        return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, HINT));
     }
     __device__ static __forceinline__ void pack(W &w, const float (&p)[B::NS]) { B::weights(w, p); }
     template <int RT>
@@ -300,13 +313,17 @@ struct Stage {
             if (++part == p.page_size >> 4) part = 0;
         }
     }
+    template <int HINT>
     __device__ __forceinline__ void load_k(const DecodeParams &p, typename OP::K &k, int i, int g) const {
 #pragma unroll
-        for (int h = 0; h < OP::PARTS; ++h) OP::load_k(k, row_rsrc((uint64_t)p.kp + at[h], rows[h], OP::ROWB, OP::ROWB), h, i, g);
+        for (int h = 0; h < OP::PARTS; ++h)
+            OP::template load_k<HINT>(k, row_rsrc((uint64_t)p.kp + at[h], rows[h], OP::ROWB, OP::ROWB), h, i, g);
     }
+    template <int HINT>
     __device__ __forceinline__ void load_v(const DecodeParams &p, typename OP::V &v, int i, int g) const {
 #pragma unroll
-        for (int h = 0; h < OP::PARTS; ++h) OP::load_v(v, row_rsrc((uint64_t)p.vp + at[h], rows[h], OP::ROWB, OP::ROWB), h, i, g);
+        for (int h = 0; h < OP::PARTS; ++h)
+            OP::template load_v<HINT>(v, row_rsrc((uint64_t)p.vp + at[h], rows[h], OP::ROWB, OP::ROWB), h, i, g);
     }
 };
 
@@ -398,20 +415,16 @@ struct Join {
     float2 ml[WAVES][64];
 };
 
-template <class OP, int RT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void decode_kernel(const DecodeParams p) {
+// The units from b on
+template <class OP, int RT, int WAVES, int HINT>
+__device__ __forceinline__ void decode_units(const DecodeParams &p, Walk<OP, WAVES> &walk, Unit b, int at, const Cut &cut, int wg,
+                                             int wave, int lane) {
     constexpr int NT = OP::NT;
     using St = Stage<OP, WAVES>;
-    const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : uniform(threadIdx.x >> 6);
-    const int i = lane & 15, g = lane >> 4, wg = blockIdx.x;
+    const int i = lane & 15, g = lane >> 4;
     const float c2 = p.scale_log2;
-
-    Walk<OP, WAVES> walk(p, wave);
-    Unit b, n1, n2;       // this unit, the next, the one after it
+    Unit n1, n2;       // the next unit, the one after it
     Pages<OP, WAVES> p1, p2;
-    Cut cut;
-    int at;
-    if (!walk.first(p, b, at, wg, cut, wave, lane)) return;
     p1.ask(p, b, wave);
     typename OP::Q q[RT];
     typename OP::K k;
@@ -419,8 +432,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void decode_kernel(const DecodeParam
     Rows<OP, RT> R;
     take_queries<OP, RT>(p, q, b.r, b.hd, i, g);
     St st(p, b, p1, wave);
-    st.load_k(p, k, i, g);
-    st.load_v(p, v, i, g);
+    st.template load_k<HINT>(p, k, i, g);
+    st.template load_v<HINT>(p, v, i, g);
     n1 = b;
     bool more = walk.left > 0;
     if (more) {
@@ -448,12 +461,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void decode_kernel(const DecodeParam
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) OP::scores(k, q[rt], s[rt]);
         __builtin_amdgcn_sched_barrier(0);
-        st.load_k(p, k, i, g);
+        st.template load_k<HINT>(p, k, i, g);
         __builtin_amdgcn_sched_barrier(0);
         softmax_step<OP, RT>(R, s, w, rows, c2, g);
         OP::template outputs<RT>(v, w, R.o);
         __builtin_amdgcn_sched_barrier(0);
-        st.load_v(p, v, i, g);
+        st.template load_v<HINT>(p, v, i, g);
         __builtin_amdgcn_sched_barrier(0);
         const bool seg_end = b.last();
         if (seg_end || !more) {
@@ -542,6 +555,28 @@ __global__ __launch_bounds__(64 * WAVES, 2) void decode_kernel(const DecodeParam
     }
 }
 
+// The non-temporal hint of a buffer load
+constexpr int kStream = 2;
+
+// STREAM: the call may read so much that keys and values go around the caches.  How much it is is
+// known here only; the loop stands twice, as waits for loads are counted in each path by itself.
+template <class OP, int RT, int WAVES, bool STREAM>
+__global__ __launch_bounds__(64 * WAVES, 2) void decode_kernel(const DecodeParams p) {
+    const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : uniform(threadIdx.x >> 6), wg = blockIdx.x;
+    Walk<OP, WAVES> walk(p, wave);
+    Unit b;
+    Cut cut;
+    int at;
+    if (!walk.first(p, b, at, wg, cut, wave, lane)) return;
+    if constexpr (STREAM) {
+        if (cut.total >= p.stream_units) {
+            decode_units<OP, RT, WAVES, kStream>(p, walk, b, at, cut, wg, wave, lane);
+            return;
+        }
+    }
+    decode_units<OP, RT, WAVES, 0>(p, walk, b, at, cut, wg, wave, lane);
+}
+
 // The records of ROWS query rows of a sequence and head, joined in an order that the lengths fix:
 // several ways take a row's records in turn, LANES lanes of four values each, and their sums are joined.
 template <class OP, int ROWS>
@@ -616,13 +651,16 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p)
 template <class OP>
 hipError_t launch_op(const DecodeParams &p, hipStream_t s) {
     const dim3 grid((unsigned)p.grid);
-    auto go = [&](auto waves) {
-        constexpr int W = decltype(waves)::value;
-        if (p.rows > 16) hipLaunchKernelGGL((decode_kernel<OP, 2, W>), grid, dim3(64 * W), 0, s, p);
-        else hipLaunchKernelGGL((decode_kernel<OP, 1, W>), grid, dim3(64 * W), 0, s, p);
-    };
-    if (p.waves == 4) go(std::integral_constant<int, 4>());
-    else go(std::integral_constant<int, 1>());
+    if (p.rows > 16) {
+        if (p.waves == 4) hipLaunchKernelGGL((decode_kernel<OP, 2, 4, false>), grid, dim3(256), 0, s, p);
+        else hipLaunchKernelGGL((decode_kernel<OP, 2, 1, false>), grid, dim3(64), 0, s, p);
+    } else if (p.waves == 1) {
+        hipLaunchKernelGGL((decode_kernel<OP, 1, 1, false>), grid, dim3(64), 0, s, p);
+    } else if (p.stream_units) {
+        hipLaunchKernelGGL((decode_kernel<OP, 1, 4, true>), grid, dim3(256), 0, s, p);
+    } else {
+        hipLaunchKernelGGL((decode_kernel<OP, 1, 4, false>), grid, dim3(256), 0, s, p);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.alone) return e;
     const int segs = p.n * p.n_kv_heads * p.tiles;

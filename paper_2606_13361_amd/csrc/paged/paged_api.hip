@@ -133,9 +133,14 @@ constexpr int64_t kOneWaveStages = 32;
 // Records are joined a query row a workgroup, or four where there are many: 1 and 4, one sequence of 3774
 // rows 9.8 and 11.7, 16 of 100 to 3980 32.1 and 31.8, 32 56.6 and 56.0, 1000 of 10 to 200 134 and 121.
 constexpr int64_t kMergeHeads = 128;
+// Keys and values of a whole call from which they are loaded with the non-temporal hint, in ranges of four
+// waves and up to 16 query rows of a kv head.  Without and with it: 64 sequences of 300 to 32768 rows 752 and
+// 679, 64 of 100 to 4096 (538 MB) 105 and 93, one of 32768 (134 MB) 29.7 and 27.0, 8 of 100 to 3980 (67 MB) 20.4
+// and 19.4; one of 16000 (66 MB) that the caches still hold 16.8 and 16.7, 4 of 100 to 3980 (34 MB) 11.3 and 12.9.
+constexpr int64_t kStreamBytes = 48 << 20;
 
 struct DecodePlan {
-    int64_t tiles, rows, grid;
+    int64_t tiles, rows, grid, stage_bytes, units;
     int waves, merge_rows;
     bool alone;
     size_t ws_bytes;
@@ -151,15 +156,16 @@ bool plan_decode(const kvr_desc *d, int64_t n, int64_t max_len, DecodePlan *out)
     const int64_t heads = n * d->n_kv_heads * s.tiles;
     const int64_t stages = max_len > 0 ? ceil_div(max_len, stage) : 1;
     if (heads > 0 && stages > kMaxRows / heads) return false;
-    const int64_t stage_bytes = stage * d->head_dim * elt_bytes(d) * 2, bytes = stages * stage_bytes;      // of a sequence and head, at most
-    const int64_t waves = kAskedBytes / stage_bytes * kCus;
+    s.stage_bytes = stage * d->head_dim * elt_bytes(d) * 2;
+    const int64_t bytes = stages * s.stage_bytes;      // of a sequence and head, at most
+    const int64_t waves = kAskedBytes / s.stage_bytes * kCus;
     const int64_t by_heads = heads * kAloneByHeads < kAloneMost ? heads * kAloneByHeads : kAloneMost;
     s.alone = bytes <= (by_heads > kAloneBytes ? by_heads : kAloneBytes);
     if (s.alone) s.waves = heads >= kOneWaveHeads && bytes <= kOneWaveBytes ? 1 : 4;
     else s.waves = stages <= kOneWaveStages ? 1 : 4;
     s.merge_rows = heads >= kMergeHeads ? 4 : 1;
-    const int64_t units = ceil_div(stages, s.waves) * heads;
-    s.grid = s.alone ? heads : units < waves / s.waves ? units : waves / s.waves;
+    s.units = ceil_div(stages, s.waves) * heads;      // at most
+    s.grid = s.alone ? heads : s.units < waves / s.waves ? s.units : waves / s.waves;
     // (single waves have more records than workgroups of four: room for what a shorter max_len needs, too)
     const int64_t one = (stages < kOneWaveStages ? stages : kOneWaveStages) * heads, most = one < waves ? one : waves;
     const int64_t sharers = s.grid > most ? s.grid : most;
@@ -285,6 +291,8 @@ int kvr_paged_decode(const kvr_desc *desc, const kvr_pages *pages, const kvr_row
     p.rows = (int32_t)plan.rows;
     p.grid = (int32_t)plan.grid;
     p.waves = plan.waves;
+    const int64_t stream_units = kStreamBytes / (plan.waves * plan.stage_bytes);
+    p.stream_units = !plan.alone && plan.waves == 4 && plan.units >= stream_units ? (int32_t)stream_units : 0;
     p.merge_rows = plan.merge_rows;
     p.alone = plan.alone ? 1 : 0;
     // part / (parts of a page), exact for the parts of 2^31 rows: with 2^b parts or more, ceil(2^(32 + b) / parts)

@@ -50,6 +50,7 @@ struct DecodeParams {
     int32_t tiles;           // of 16 (32) query rows of a kv head
     int32_t rows;            // of a record
     int32_t grid;            // workgroups that share the units
+    int32_t stream_units;    // units from which keys and values are loaded with the non-temporal hint (0: never)
     int32_t waves;           // of a workgroup
     int32_t merge_rows;      // query rows of a workgroup that joins records, 1 or 4
     int32_t alone;           // a workgroup takes one sequence and head, nothing is joined

@@ -194,6 +194,16 @@ def test_each_way(dt, heads, way):
 
 
 @DTYPES
+def test_keys_and_values_around_the_caches(dt):
+    """53 MB of 16-bit keys and values (f32: 105), which are loaded with the non-temporal hint; with a page that
+    is not there and rows behind the lengths."""
+    b = Batch(dt, (8, 2, 128), 64, [30001, 0, 12345, -1, 9000], seed=8, lost=[(0, 17, -1)])
+    t = b.gpu()
+    b.call(t)
+    b.check(t)
+
+
+@DTYPES
 @pytest.mark.parametrize("heads", [(8, 8, 64), (8, 4, 128), (68, 2, 64)], ids=lambda h: "%d_%d_%d" % h)
 def test_a_wave_for_each_of_many_short_ones(dt, heads):
     n = 1024 // heads[1] + 3
