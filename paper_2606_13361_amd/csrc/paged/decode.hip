@@ -430,10 +430,14 @@ __device__ __forceinline__ void decode_units(const DecodeParams &p, Walk<OP, WAV
     typename OP::K k;
     typename OP::V v;
     Rows<OP, RT> R;
+    // in this order, as the loop has it: it waits for the keys only, with the values on their way
     take_queries<OP, RT>(p, q, b.r, b.hd, i, g);
     St st(p, b, p1, wave);
+    __builtin_amdgcn_sched_barrier(0);
     st.template load_k<HINT>(p, k, i, g);
+    __builtin_amdgcn_sched_barrier(0);
     st.template load_v<HINT>(p, v, i, g);
+    __builtin_amdgcn_sched_barrier(0);
     n1 = b;
     bool more = walk.left > 0;
     if (more) {
@@ -544,6 +548,9 @@ __device__ __forceinline__ void decode_units(const DecodeParams &p, Walk<OP, WAV
                 *sharers_of<OP>(p, b.r, b.hd) = make_int2(wg, whole ? wg : cut.range_of(last));
             }
             R.clear();
+            // the queries have landed: otherwise every stage's scores would wait for what was asked for before
+            // these, its values among it
+            wait_vmcnt<0>();
             at += b.u + 1 - seg_u;      // of the next segment's first unit
             seg_u = 0;
         }
