@@ -15,12 +15,14 @@
 // out by a lane each, while the first rows are on their way.
 //
 // HBM bounds it (a 1 GB copy reaches 5.1 TB/s).  bf16, 32 / 8 heads of 128, read and written:
-//   32768 tokens' norms and rotation 127 us, 5.4 TB/s
-//   32 prompts, 32767 tokens, into pages 171 us, 4.7 TB/s; 3774 tokens' keys and values 9.3 us
-// Rows of the next tokens that are not on their way while these are worked out are hidden by
-// other waves: 3 rows a lane (4 waves a SIMD) and 6 (3 waves) took 181 and 198 us for the prompts,
-// 66 and 74 us for 32768 tokens' keys and values.  Written rows bypass the caches as far as
-// a hint does that: 3774 tokens 10.9 us without, the norms 136.
+//   32768 tokens' norms and rotation 123 us, 5.6 TB/s
+//   32 prompts, 32767 tokens, into pages 168 us, 4.8 TB/s; 3774 tokens' keys and values 9.2 us, 3.6 TB/s
+//   one token 3.8 us: launch, length, page, rotation
+// Waits for rows that are not on their way while others are worked out are filled by other waves: 3
+// rows a lane (4 waves a SIMD) and 6 (3 waves) took 181 and 198 us for the prompts, 66 and 74 us for
+// 32768 tokens' keys and values.  Written rows bypass the caches as far as a hint does that: 3774 tokens
+// 10.9 us without, the norms 136.  A wave for the rows of one token instead of a workgroup for a few
+// tokens' (cosines read for each row, places behind a barrier): the prompts 218 -> 170, the norms 196 -> 127.
 #include "attn_common.hpp"
 #include "paged/paged_internal.hpp"
 
