@@ -2,13 +2,12 @@
 //
 //   out[r, h] = softmax_j(scale q[r, h] . k_j) v_j,  j < len[r] + n_new, j's page in the pool
 //
-// The lengths are read on the device, so the work is shared out there too: the keys of a
-// sequence and kv head are units, a stage of 32 (fp32: 16) for each wave of a workgroup,
-// and the units of the whole batch, one sequence and head after the other, are
-// cut into equal ranges, one for each workgroup.  However ragged the batch, every workgroup
-// reads as much.  A sequence and head that lie in one range are finished there; pieces of
-// one that several ranges share are records (m, l, O) of the workspace, which a second
-// launch joins in their order.
+// The lengths are read on the device, so the work is shared out there too: the keys of a sequence and kv
+// head are units, a stage of 32 (fp32: 16) for each wave of a workgroup, and the units of the whole batch, one
+// sequence and head after the other, are cut into equal ranges, one for each workgroup.  However ragged the
+// batch, every workgroup reads as much.  A sequence and head that lie in one range are finished there; pieces
+// of one that several ranges share are records (m, l, O) of the workspace, which a second launch joins in
+// their order.  Short or many sequences: a workgroup, or a wave, takes one and nothing is joined (paged_api.hip).
 //
 // A wave's stages go from memory straight to the registers that the matrix instructions read
 // (attn_direct.hpp); a stage's two halves of 16 rows lie in one page each, and a buffer
@@ -18,7 +17,7 @@
 // ends of sequences too: its pages are looked up another stage ahead, with scalar loads, which
 // do not wait behind the keys and values that are on their way.
 //
-// HBM bounds it: 4 G operations for each byte of 16-bit keys and values, G query heads to a kv head.
+// HBM bounds it: G operations for each byte of 16-bit keys and values, G query heads to a kv head.
 // Measured, a range's kernel and the join, in us (32 / 8 heads of 128 where nothing else is said):
 //   64 sequences of 300 to 32768 rows   618 + 4.6    4.3 GB, 7.0 TB/s
 //   64 of up to 4096, fp16              83.1 + 4.6   538 MB, 6.5 TB/s
@@ -38,7 +37,6 @@ namespace kvr {
 namespace {
 
 using namespace dev;
-
 
 // The two element kinds: a stage's weights as the second product's operand.  16-bit: the weight
 // cut to the element type and what that left over, rounded, as two operands, so that weights

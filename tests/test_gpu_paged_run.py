@@ -94,16 +94,19 @@ def test_conversations_against_the_dense_calls(dt, ps):
 
 
 @DTYPES
-def test_a_captured_step_serves_a_whole_decode(dt):
+@pytest.mark.parametrize("reach", [208, 1600], ids=["one_launch", "shared_out"])
+def test_a_captured_step_serves_a_whole_decode(dt, reach):
     """Append, decode and the lengths' update in one graph, replayed with new tokens, eager work between; an
     eager server does the same steps.  A slot leaves the batch on the way."""
     heads, n = (16, 2, 64), 5
     Hq, Hkv, d = heads
-    a, b = (Server(dt, heads, 16, n, 1600, seed=3) for _ in range(2))
+    a, b = (Server(dt, heads, 16, n, reach, seed=3) for _ in range(2))
+    assert (a.ws.numel() > 0) == (reach == 1600)
     x = draw(a.g, dt, n, Hq + 2 * Hkv, d)
     w = [draw(a.g, dt, d) for _ in range(2)]
     q = torch.empty((n, Hq, d), dtype=dt, device=DEV)
-    start = torch.tensor([1500, 0, 14, 15, 700], dtype=torch.int32, device=DEV)
+    long = reach - 100
+    start = torch.tensor([long, 0, 14, 15, long // 2], dtype=torch.int32, device=DEV)
     for s in (a, b):
         s.pool.normal_(generator=torch.Generator(device=DEV).manual_seed(9))
         s.len.copy_(start)
@@ -134,7 +137,7 @@ def test_a_captured_step_serves_a_whole_decode(dt):
         torch.cuda.synchronize()
         assert same_bits(a.out, b.out) and same_bits(a.pool, b.pool) and torch.equal(a.len, b.len)
         assert i >= 3 or same_bits(q, q2)
-    assert a.len.tolist() == [1506, 6, -1, 21, 706]
+    assert a.len.tolist() == [long + 6, 6, -1, 21, long // 2 + 6]
 
 
 def test_two_streams_at_once():
