@@ -117,12 +117,14 @@ int check_page_pointers(const kvr_pages *g) {
 // 32768 829, 754 and 763; 16 / 2, 64 of 100 to 3900 21.2, 20.8 and 22.0.
 constexpr int64_t kAskedBytes = 64 << 10;
 // A sequence and head of at most this many bytes is one workgroup's of four waves, and nothing is joined:
-// 160 KB, more where there are many of them, as far as one long sequence among short ones does not hold the
-// others up for long.  In one launch and shared out: 1 sequence of 250 rows (128 KB) 5.7 and 6.7, 310 6.4
-// and 6.8, 480 7.8 and 7.0; 8 of 20 to 300 7.5 and 8.1, to 480 (240 KB) 8.9 and 8.5; 31 of 10 to 480 10.2
-// and 13.1, 32 of 10 to 980 (496 KB) 18.5 and 20.3, 64 of 100 to 1500 (752 KB) 47.4 and 46.3; 16 / 2, 64 of 10
-// to 900 (232 KB) 9.8 and 11.0; fp32, 8 of 10 to 150 (160 KB) 9.1 and 8.5, 64 of 10 to 480 (480 KB) 34.2 and 33.9.
-constexpr int64_t kAloneBytes = 160 << 10, kAloneMost = 512 << 10, kAloneByHeads = 2 << 10;
+// 256 KB, more where there are many of them, as far as one long sequence among short ones does not hold the
+// others up for long.  In one launch and shared out, in a graph and (in brackets) issued one by one, where two launches
+// take the host 10: 1 sequence of 310 rows 6.2 and 6.9 (7.4 and 10.4), 480 (240 KB) 7.5 and 7.3 (7.9 and 10.3), 600
+// 8.6 and 7.2 (8.9 and 10.4); 8 of 20 to 480 8.5 and 8.6 (8.2 and 10.1), to 600 9.5 and 9.0 (9.3 and 10.0); 16 / 2, 1 of 900
+// (232 KB) 8.4 and 7.0 (8.7 and 10.3); fp32, 8 of 10 to 250 (256 KB) 10.2 and 8.9 (9.9 and 10.2).  In a graph: 32 of 10 to 980
+// (496 KB) 18.5 and 20.3, 64 of 100 to 1500 (752 KB) 47.4 and 46.3; 16 / 2, 64 of 10 to 900 9.8 and 11.0; fp32, 64 of
+// 10 to 480 (480 KB) 34.2 and 33.9.
+constexpr int64_t kAloneBytes = 256 << 10, kAloneMost = 512 << 10, kAloneByHeads = 2 << 10;
 // One wave instead of four, where many of them are short: 128 sequences of 10 to 200 rows 16.7 instead of 18.1, 256
 // 27.3 instead of 30.1, 256 of 10 to 480 (240 KB) 56.6 and 55.4; 64 of 10 to 250 12.5 and 11.3.
 constexpr int64_t kOneWaveHeads = 1024, kOneWaveBytes = 128 << 10;

@@ -173,14 +173,14 @@ def test_many_sequences(max_pages):
     b.check(t)
 
 
-# max_len of the ways of a call of 6 sequences of at most 150 rows, by the bytes of a sequence and head: one launch
-# of four waves each, ranges of one wave, ranges of four
+# max_len of the ways of a call of 6 sequences of at most 150 rows or so, by the bytes of a sequence and head: one
+# launch of four waves each, ranges of one wave, ranges of four
 WAYS = {"one_launch": 160, "ranges_of_a_wave": 1024, "ranges_of_four": 3200}
+EACH = [(w, h) for w in WAYS for h in ((8, 2, 128), (8, 2, 64), (20, 1, 128), (40, 1, 64)) if w != "ranges_of_a_wave" or h[2] == 128]
 
 
 @DTYPES
-@pytest.mark.parametrize("heads", [(8, 2, 128), (8, 2, 64), (20, 1, 128), (40, 1, 64)], ids=lambda h: "%d_%d_%d" % h)
-@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("way,heads", EACH, ids=lambda x: x if isinstance(x, str) else "%d_%d_%d" % x)
 def test_each_way(dt, heads, way):
     reach = WAYS[way] // (2 if dt == F32 else 1)
     rows = [reach // (7 if way == "one_launch" else 3), 150, 0, -1, 33, 64]

@@ -212,3 +212,43 @@ def test_a_batch_with_norms_against_the_oracle(dt):
     b = bound(dt, want, mass, P._f64(q), np.abs(P._f64(kp)).max((0, 2)), np.maximum(rows, 0))
     err = np.abs(P._f64(s.out) - want)
     assert (err[on] <= b[on]).all()
+
+
+def test_the_binding_refuses_what_does_not_fit_together():
+    s = Server(BF16, (8, 2, 64), 16, 3, 64)
+    q, k = draw(s.g, BF16, 3, 8, 64), draw(s.g, BF16, 3, 2, 64)
+    before = s.pool.clone()
+    kp, vp = s.pool[:, 0], s.pool[:, 1]
+    ints = lambda n: torch.zeros(n, dtype=torch.int32, device=DEV)
+    for f in (lambda: kvr.PagedCache(s.desc, kp, vp, s.table.long()),                       # the table's type
+              lambda: kvr.PagedCache(s.desc, kp, vp, s.table[:, ::2]),                      # not contiguous
+              lambda: kvr.PagedCache(s.desc, kp, vp.contiguous(), s.table),                 # pages another distance apart
+              lambda: kvr.PagedCache(s.desc, kp.transpose(1, 2), vp.transpose(1, 2), s.table),
+              lambda: kvr.PagedCache(s.desc, kp.half(), vp.half(), s.table),
+              lambda: kvr.kvr_paged_append(s.desc, s.cache, k[:2], k, s.len),
+              lambda: kvr.kvr_paged_append(s.desc, s.cache, k.float(), k, s.len),
+              lambda: kvr.kvr_paged_append(s.desc, s.cache, k[..., ::2], k, s.len),
+              lambda: kvr.kvr_paged_append(s.desc, s.cache, k, k, s.len.long()),
+              lambda: kvr.kvr_paged_append(s.desc, s.cache, k, k, s.len[:2]),
+              lambda: kvr.kvr_paged_append(s.desc, s.cache, k, k, s.len, cu_seqlens=ints(3)),
+              lambda: kvr.kvr_paged_append(s.desc, s.cache, k, k, s.len, pos=ints(2)),
+              lambda: kvr.kvr_paged_append(s.desc, s.cache, k, k, s.len, k_norm=k[0]),
+              lambda: kvr.kvr_paged_append(s.desc, s.cache, k, k, s.len, q_out=q),
+              lambda: kvr.kvr_paged_append(kvr.make_desc(8, 4, 64, BF16, 0), s.cache, k, k, s.len),
+              lambda: kvr.kvr_paged_append(s.desc, s.cache, k, k, s.len, rope=kvr.RopeTable(128, 64)),
+              lambda: kvr.kvr_paged_decode(s.desc, s.cache, k, s.len, s.out, s.ws),
+              lambda: kvr.kvr_paged_decode(s.desc, s.cache, q, s.len, s.out[:2], s.ws),
+              lambda: kvr.kvr_paged_decode(s.desc, s.cache, q, s.len, s.out.transpose(0, 1).contiguous().transpose(0, 1), s.ws),
+              lambda: kvr.kvr_qk_norm_rope(s.desc, q, k, k_out=q),
+              lambda: kvr.kvr_qk_norm_rope(s.desc, None, k, q_out=q)):
+        with pytest.raises(ValueError):
+            f()
+    for f, status in ((lambda: kvr.kvr_paged_decode(s.desc, s.cache, q, s.len, s.out, s.ws, max_len=65), kvr.KVR_ERR_CAPACITY),
+                      (lambda: kvr.kvr_paged_append(s.desc, s.cache, k, k, s.len, rope=kvr.RopeTable(64, 63)), kvr.KVR_ERR_POSITION),
+                      (lambda: kvr.kvr_paged_append(s.desc, s.cache, k[:2], k[:2], s.len), kvr.KVR_ERR_SHAPE),
+                      (lambda: kvr.kvr_qk_norm_rope(s.desc, q[:, :1].expand(3, 8, 64), None), kvr.KVR_ERR_SHAPE)):
+        with pytest.raises(kvr.KvrError) as e:
+            f()
+        assert e.value.status == status
+    torch.cuda.synchronize()
+    assert same_bits(s.pool, before)
