@@ -51,8 +51,9 @@ template <class E, int D>
 struct Dec16 : Op16<E, D> {
     using B = Op16<E, D>;
     static constexpr int PARTS = 2;
-    // fp16 weights reach down to 2^-14 before they lose bits: the largest is 2^12
-    static constexpr float LIFT = std::is_same<E, F16>::value ? 12.f : 0.f;
+    // The largest weight is 2^LIFT.  fp16 weights lose bits below 2^-14, so it is 2^12; bf16 and fp32 numbers reach
+    // down to 2^-126, and with 2^-20 a sum of a million of the largest values is finite, as their mean is.
+    static constexpr float LIFT = std::is_same<E, F16>::value ? 12.f : -20.f;
     using W = Weights<B>;
     // part h of a stage
     template <int HINT>
@@ -99,7 +100,7 @@ template <int D>
 struct Dec32 : Op32<D> {
     using B = Op32<D>;
     static constexpr int PARTS = 1;
-    static constexpr float LIFT = 0.f;
+    static constexpr float LIFT = -20.f;
     using W = typename B::P;
     template <int HINT>
     __device__ static __forceinline__ void load_k(typename B::K &k, __amdgpu_buffer_rsrc_t r, int, int i, int g) {

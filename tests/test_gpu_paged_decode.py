@@ -310,19 +310,21 @@ def test_scores_as_large_as_numbers_go():
         assert torch.equal(t["out"][r].cpu(), b.vp[b.table[r, 1], 0, 5].expand(2, 64))
 
 
-def test_largest_numbers():
+@pytest.mark.parametrize("reach", [208, 8192], ids=["one_launch", "shared_out"])
+def test_largest_numbers(reach):
     """A mean of the largest values is finite; an infinity where it has weight shows."""
     for dt, big in ((BF16, 3.3e38), (F16, 65504.0), (F32, 3.4e38)):
-        b = Batch(dt, (4, 1, 64), 16, [200, 200])
+        m = reach - 8
+        b = Batch(dt, (4, 1, 64), 16, [m, m], max_pages=reach // 16)
         b.q.zero_()
-        b.vp[b.table[0, :12].long(), :] = big / 512 if dt != F16 else big
-        b.vp[b.table[0, 12], :, :8] = big / 512 if dt != F16 else big
+        for j in range(reach // 16):
+            b.vp[b.table[0, j], :, :min(16, m - 16 * j)] = big
         b.vp[b.table[1, 7], 0, 3, 5] = float("inf")
         t = b.gpu()
         b.call(t)
         torch.cuda.synchronize()
         got = t["out"].float().cpu()
-        want = torch.tensor(big / 512 if dt != F16 else big, dtype=dt).float()
+        want = torch.tensor(big, dtype=dt).float()
         assert torch.allclose(got[0], want.expand_as(got[0]), rtol=2.0 ** -7, atol=0)
         assert bool((got[1, :, 5] == float("inf")).all())
         assert bool(torch.isfinite(got[1, :, torch.arange(64) != 5]).all())
