@@ -339,7 +339,7 @@ struct Stage {
 template <class OP, int RT>
 struct Rows {
     f32x4 o[RT][OP::NT];
-    float m[RT], l[RT];      // reference (log2 domain); the lane's share of the row's sum
+    float m[RT], l[RT];      // half the largest score; the lane's share of the row's sum
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
@@ -351,7 +351,9 @@ struct Rows {
     }
 };
 
-// Scores become weights 2^(c2 s - m), m the running maximum less LIFT
+// Scores become weights 2^(c2 (s / 2 - m) + LIFT), m half the largest score so far.  The difference comes first: the largest
+// score's is zero, however large it is (less a rounded reference of c2 s it is half a step of that, whole powers of two
+// from scores of 1e7 on).  It is of halves: two finite scores may be an infinity apart.
 template <class OP, int RT>
 __device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][OP::NS], typename OP::W (&w)[RT],
                                              const int (&rows)[OP::PARTS], float c2, int g) {
@@ -370,9 +372,9 @@ __device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][OP:
         float mx = s[rt][0];
 #pragma unroll
         for (int e = 1; e < OP::NS; ++e) mx = fmaxf(mx, s[rt][e]);
-        mx = fmaxf(quad_max(mx) * c2 - OP::LIFT, R.m[rt]);
+        mx = fmaxf(0.5f * quad_max(mx), R.m[rt]);
         if (__ballot(mx > R.m[rt])) {
-            const float a = __builtin_amdgcn_exp2f(R.m[rt] - mx);
+            const float a = __builtin_amdgcn_exp2f((R.m[rt] - mx) * c2);
             R.m[rt] = mx;
             R.l[rt] *= a;
 #pragma unroll
@@ -381,7 +383,7 @@ __device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][OP:
         float p[OP::NS], sum = 0.f;
 #pragma unroll
         for (int e = 0; e < OP::NS; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][e], c2, -R.m[rt]));
+            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(__builtin_fmaf(s[rt][e], 0.5f, -R.m[rt]), c2, OP::LIFT));
             sum += p[e];
         }
         R.l[rt] += sum;
@@ -431,7 +433,7 @@ __device__ __forceinline__ void decode_units(const DecodeParams &p, Walk<OP, WAV
     constexpr int NT = OP::NT;
     using St = Stage<OP, WAVES>;
     const int i = lane & 15, g = lane >> 4;
-    const float c2 = p.scale_log2;
+    const float c2 = p.half_scale_log2;
     Unit n1, n2;       // the next unit, the one after it
     Pages<OP, WAVES> p1, p2;
     p1.ask(p, b, wave);
@@ -541,7 +543,7 @@ __device__ __forceinline__ void decode_units(const DecodeParams &p, Walk<OP, WAV
 #pragma unroll
                         for (int s = 0; s < WAVES; ++s) {
                             const float2 ml = lds.ml[s][lane];
-                            const float a = __builtin_amdgcn_exp2f(ml.x - M);
+                            const float a = __builtin_amdgcn_exp2f((ml.x - M) * c2);
                             L = __builtin_fmaf(a, ml.y, L);
 #pragma unroll
                             for (int t = 0; t < NT / 4; ++t)
@@ -628,13 +630,13 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p)
         }
 #pragma unroll
         for (int s = 0; s < BATCH; ++s) mx = fmaxf(mx, w[s].x);
-        const float a = __builtin_amdgcn_exp2f(M - mx);
+        const float a = __builtin_amdgcn_exp2f((M - mx) * p.half_scale_log2);
         M = mx;
         l *= a;
         acc *= a;
 #pragma unroll
         for (int s = 0; s < BATCH; ++s) {
-            const float f = __builtin_amdgcn_exp2f(w[s].x - M);
+            const float f = __builtin_amdgcn_exp2f((w[s].x - M) * p.half_scale_log2);
             l = __builtin_fmaf(f, w[s].y, l);
 #pragma unroll
             for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(f, x[s][c], acc[c]);
@@ -647,13 +649,13 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p)
     float top = M;
 #pragma unroll
     for (int s = 1; s < WAYS; ++s) top = fmaxf(top, mls[s * ROWS + slot].x);
-    const float a = __builtin_amdgcn_exp2f(M - top);
+    const float a = __builtin_amdgcn_exp2f((M - top) * p.half_scale_log2);
     l *= a;
     acc *= a;
 #pragma unroll
     for (int s = 1; s < WAYS; ++s) {
         const float2 ml = mls[s * ROWS + slot];
-        const float f = __builtin_amdgcn_exp2f(ml.x - top);
+        const float f = __builtin_amdgcn_exp2f((ml.x - top) * p.half_scale_log2);
         l = __builtin_fmaf(f, ml.y, l);
         const f32x4 x = sums[s * ROWS * LANES + threadIdx.x];
 #pragma unroll

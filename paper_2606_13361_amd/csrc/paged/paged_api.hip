@@ -304,7 +304,8 @@ int kvr_paged_decode(const kvr_desc *desc, const kvr_pages *pages, const kvr_row
     while (((uint64_t)1 << bits) < parts) ++bits;
     p.part_shift = 32 + bits;
     p.part_mul = (((uint64_t)1 << p.part_shift) + parts - 1) / parts;
-    p.scale_log2 = eff_scale(desc) * 1.4426950408889634f;
+    // (finite: no difference stays none)
+    p.half_scale_log2 = fminf(eff_scale(desc) * (2.f * 1.4426950408889634f), 3.4028235e38f);
     return to_status(launch_decode(p, desc->head_dim, desc->dtype, (hipStream_t)stream));
 }
 

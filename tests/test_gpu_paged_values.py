@@ -1,0 +1,81 @@
+"""kvr_paged_decode with scores and values of every size.
+
+Queries have one element that is not zero, so that a score is one product: exact in 16-bit types, rounded once in
+fp32.  What each test allows is derived in its docstring."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged as P
+from paper_2606_13361_amd import kvr
+from test_gpu_paged_decode import Batch
+
+pytestmark = pytest.mark.gpu
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+DTYPES = pytest.mark.parametrize("dt", [BF16, F16, F32], ids=["bf16", "fp16", "f32"])
+# table's rows of 16-bit types (f32: half): one launch, ranges of a wave, ranges of four
+REACH = pytest.mark.parametrize("reach", [320, 1024, 6144], ids=["one_launch", "ranges_of_a_wave", "ranges_of_four"])
+HEADS = pytest.mark.parametrize("heads", [(4, 1, 128), (40, 1, 128)], ids=lambda h: "%d_%d_%d" % h)
+
+
+def column(b, pool, r, d, values):
+    """Element d of the rows of sequence r, in every kv head."""
+    for j in range(-(-len(values) // b.ps)):
+        x = values[b.ps * j:b.ps * (j + 1)]
+        pool[b.table[r, j], :, :len(x), d] = x.to(b.dt)
+
+
+def batch(dt, heads, reach, rows, q0, seed=0, **kw):
+    b = Batch(dt, heads, 16, rows, seed=seed, max_pages=reach // 16, **kw)
+    b.q.zero_()
+    b.q[:, :, 0] = q0
+    return b
+
+
+def run(b):
+    t = b.gpu()
+    b.call(t)
+    torch.cuda.synchronize()
+    return t["out"].cpu()
+
+
+def oracle(b):
+    with np.errstate(invalid="ignore", over="ignore"):
+        return P.decode(b.q, b.kp, b.vp, b.table.numpy(), b.rows)
+
+
+# queries' and keys' sizes: scores of 1e7 and more, all finite in fp32
+LARGE = [(F16, 2999.0, 3001.0), (F16, 59000.0, 61000.0), (BF16, 3.3e4, 5.1e4), (BF16, 1.3e9, 7.7e9), (BF16, 1.1e19, 0.9e19),
+         (F32, 5.0e4, 4.9e4), (F32, 3.1e5, 2.9e5), (F32, 7.3e11, 1.9e12), (F32, 3.0 * 2.0 ** 60, 5.0 * 2.0 ** 59)]
+
+
+@pytest.mark.parametrize("dt,q,k", LARGE, ids=lambda x: str(x).replace("torch.", ""))
+@REACH
+@HEADS
+def test_large_finite_scores(dt, q, k, heads, reach):
+    """Scores are apart by 500 units of log2 and more, or the same number: the keys of the largest one have one weight, the
+    others none (2^-500 in 64 bits).  The result is the mean of w values: off by its rounding, and by w + 8 steps of
+    fp32 (two sums, a quotient, products).  Scores rise and fall; queries of odd heads are negative."""
+    reach //= 2 if dt == F32 else 1
+    rows = [reach, reach - 7, 40, 1, 0, -1, reach // 2]
+    b = batch(dt, heads, reach, rows, q, seed=3)
+    b.q[:, 1::2, 0] *= -1.0
+    g = torch.Generator().manual_seed(reach)
+    keys = {}
+    for r, m in enumerate(rows):
+        if m <= 0:
+            continue
+        low = torch.randint(1, 33, (m,), generator=g) / 64.0 if r % 3 else torch.arange(m, 0, -1) / (2.0 * m) + 1.0 / 64.0
+        x = (k * (1.0 - low.double())).to(dt)
+        x[torch.randperm(m, generator=g)[:1 + r % 3]] = k
+        keys[r] = -x if r % 2 else x
+        column(b, b.kp, r, 0, keys[r])
+    got, (out, mass) = P._f64(run(b)), oracle(b)
+    for r, m in enumerate(rows):
+        if m < 0:
+            continue
+        for p in (0, 1):
+            best = 0 if m == 0 else int((keys[r] == (keys[r].min() if p else keys[r].max())).sum())
+            allowed = 1.1 * (torch.finfo(dt).eps / 2 * np.abs(out[r, p::2]) + (best + 8) * 2.0 ** -24 * mass[r, p::2])
+            err = np.nan_to_num(np.abs(got[r, p::2] - out[r, p::2]), nan=np.inf)
+            assert (err <= allowed).all(), "sequence %d: %.3g off, a mean of %d values" % (r, err.max(), best)
