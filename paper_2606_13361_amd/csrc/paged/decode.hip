@@ -51,9 +51,11 @@ template <class E, int D>
 struct Dec16 : Op16<E, D> {
     using B = Op16<E, D>;
     static constexpr int PARTS = 2;
-    // The largest weight is 2^LIFT.  fp16 weights lose bits below 2^-14, so it is 2^12; bf16 and fp32 numbers reach
-    // down to 2^-126, and with 2^-20 a sum of a million of the largest values is finite, as their mean is.
-    static constexpr float LIFT = std::is_same<E, F16>::value ? 12.f : -20.f;
+    // Weights enter the second product times LIFT, the largest one 1.  fp16 numbers lose bits below 2^-14, so it is 2^12;
+    // bf16 and fp32 numbers reach down to 2^-126, and with 2^-20 a sum of a million of the largest values is finite, as
+    // their mean is.  A factor is exact; as an addend of the weight's exponent it would cost fp32 weights up to
+    // four bits (9 sequences of up to 945 rows off by 1.5e-7 instead of 7.9e-8).
+    static constexpr float LIFT = std::is_same<E, F16>::value ? 0x1p12f : 0x1p-20f;
     using W = Weights<B>;
     // part h of a stage
     template <int HINT>
@@ -74,12 +76,12 @@ struct Dec16 : Op16<E, D> {
     __device__ static __forceinline__ void pack(W &w, const float (&p)[B::NS]) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float a = p[2 * j] * (1.f - 0x1p-20f), b = p[2 * j + 1] * (1.f - 0x1p-20f);
+            const float a = p[2 * j] * (LIFT * (1.f - 0x1p-20f)), b = p[2 * j + 1] * (LIFT * (1.f - 0x1p-20f));
             uint32_t x;
             if constexpr (std::is_same<E, F16>::value) x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
             else x = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
             w.hi.f[j] = x;
-            w.lo.f[j] = E::pack2(p[2 * j] - E::lo(x), p[2 * j + 1] - E::hi(x));
+            w.lo.f[j] = E::pack2(__builtin_fmaf(p[2 * j], LIFT, -E::lo(x)), __builtin_fmaf(p[2 * j + 1], LIFT, -E::hi(x)));
         }
     }
     template <int RT>
@@ -100,7 +102,7 @@ template <int D>
 struct Dec32 : Op32<D> {
     using B = Op32<D>;
     static constexpr int PARTS = 1;
-    static constexpr float LIFT = -20.f;
+    static constexpr float LIFT = 0x1p-20f;
     using W = typename B::P;
     template <int HINT>
     __device__ static __forceinline__ void load_k(typename B::K &k, __amdgpu_buffer_rsrc_t r, int, int i, int g) {
@@ -118,7 +120,10 @@ struct Dec32 : Op32<D> {
     __device__ static __forceinline__ f32x4 load(__amdgpu_buffer_rsrc_t r, int off) {
         return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, HINT));
     }
-    __device__ static __forceinline__ void pack(W &w, const float (&p)[B::NS]) { B::weights(w, p); }
+    __device__ static __forceinline__ void pack(W &w, const float (&p)[B::NS]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w.f[e] = p[e] * LIFT;
+    }
     template <int RT>
     __device__ static __forceinline__ void outputs(const typename B::V &v, const W (&w)[RT], f32x4 (&o)[RT][B::NT]) {
         B::template accumulate<RT>(v, w, o);
@@ -351,7 +356,7 @@ struct Rows {
     }
 };
 
-// Scores become weights 2^(c2 (s / 2 - m) + LIFT), m half the largest score so far.  The difference comes first: the largest
+// Scores become weights 2^(c2 (s / 2 - m)), m half the largest score so far.  The difference comes first: the largest
 // score's is zero, however large it is (less a rounded reference of c2 s it is half a step of that, whole powers of two
 // from scores of 1e7 on).  It is of halves: two finite scores may be an infinity apart.
 template <class OP, int RT>
@@ -383,7 +388,7 @@ __device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][OP:
         float p[OP::NS], sum = 0.f;
 #pragma unroll
         for (int e = 0; e < OP::NS; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(__builtin_fmaf(s[rt][e], 0.5f, -R.m[rt]), c2, OP::LIFT));
+            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][e], 0.5f, -R.m[rt]) * c2);
             sum += p[e];
         }
         R.l[rt] += sum;
@@ -499,7 +504,7 @@ __device__ __forceinline__ void decode_units(const DecodeParams &p, Walk<OP, WAV
                 auto put = [&](int c, const f32x4 (&acc)[NT / 4], float M, float L) {
                     const int d = NT * (4 * g + c);
                     if (whole) {
-                        const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;      // no keys: zeros
+                        const float inv = L > 0.f ? 1.f / L * (1.f / OP::LIFT) : L == 0.f ? 0.f : L;      // no keys: zeros
                         unsigned char *out = (unsigned char *)p.out + ((int64_t)b.r * p.n_q_heads + kh * p.group + row) * OP::ROWB;
 #pragma unroll
                         for (int t = 0; t < NT / 4; ++t)
@@ -661,7 +666,7 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p)
 #pragma unroll
         for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(f, x[c], acc[c]);
     }
-    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+    const float inv = l > 0.f ? 1.f / l * (1.f / OP::LIFT) : l == 0.f ? 0.f : l;
     const int64_t to = (int64_t)r * p.n_q_heads + kh * p.group + row0 + row;
     OP::put4((unsigned char *)p.out + to * OP::ROWB, d, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
 }

@@ -79,3 +79,20 @@ def test_large_finite_scores(dt, q, k, heads, reach):
             allowed = 1.1 * (torch.finfo(dt).eps / 2 * np.abs(out[r, p::2]) + (best + 8) * 2.0 ** -24 * mass[r, p::2])
             err = np.nan_to_num(np.abs(got[r, p::2] - out[r, p::2]), nan=np.inf)
             assert (err <= allowed).all(), "sequence %d: %.3g off, a mean of %d values" % (r, err.max(), best)
+
+
+def test_weights_of_fp32_keep_their_bits():
+    """Two keys, the values 1 and 0: out = w / (1 + w) for one, 1 / (1 + w) for the other order, w = 2^-x, 0 <= x < 0.19.
+    Steps of 2^-24: x has the rounding of the scores' difference, of the scale (two) and of the product, 3 x: 0.6, of w 0.4;
+    2^x of one place, 1 (its steps are half as large below 1); out changes by at most 0.53 of w's; the sum 1,
+    the quotient 1, the product 1.  In all 3.8, a tenth more."""
+    n = 400
+    b = batch(F32, (4, 2, 64), 16, [2] * n, 8.0)
+    g = torch.Generator().manual_seed(5)
+    for r in range(n):
+        column(b, b.kp, r, 0, torch.rand(2, generator=g) * 0.125)
+        b.vp[b.table[r, 0], :, 0] = 1.0
+        b.vp[b.table[r, 0], :, 1] = 0.0
+    got, (out, _) = P._f64(run(b)), oracle(b)
+    rel = np.abs(got - out) / out
+    assert (rel <= 1.1 * 3.8 * 2.0 ** -24).all(), "%.3g steps" % (rel.max() * 2.0 ** 24)
