@@ -42,7 +42,8 @@ using namespace dev;
 // cut to the element type and what that left over, rounded, as two operands, so that weights
 // keep 16 bits (fp16: 22) and outputs are off by little more than their own rounding; the
 // products are matrix instructions that wait for memory anyway.  The cut is of a little less
-// than the weight: then the rest is positive where the weight is, and an infinite value stays one.
+// than the weight: then both are positive, and an infinite value stays one, down to weights of 2^-36 (fp16:
+// the rest, too, is at least the smallest number) or 2^-85 (bf16) of the largest.  Below, it is no number.
 template <class OP>
 struct Weights {
     typename OP::P hi, lo;
@@ -51,11 +52,13 @@ template <class E, int D>
 struct Dec16 : Op16<E, D> {
     using B = Op16<E, D>;
     static constexpr int PARTS = 2;
-    // Weights enter the second product times LIFT, the largest one 1.  fp16 numbers lose bits below 2^-14, so it is 2^12;
+    // Weights enter the second product times LIFT, the largest one 1.  fp16 numbers end at 2^-24 and below 2^16: it is 2^15;
     // bf16 and fp32 numbers reach down to 2^-126, and with 2^-20 a sum of a million of the largest values is finite, as
     // their mean is.  A factor is exact; as an addend of the weight's exponent it would cost fp32 weights up to
     // four bits (9 sequences of up to 945 rows off by 1.5e-7 instead of 7.9e-8).
-    static constexpr float LIFT = std::is_same<E, F16>::value ? 0x1p12f : 0x1p-20f;
+    static constexpr float LIFT = std::is_same<E, F16>::value ? 0x1p15f : 0x1p-20f;
+    // of the rest: it rounds to the smallest fp16 number (and less than that: a weight of zero is not cut to minus it)
+    static constexpr float LEAST = std::is_same<E, F16>::value ? 0x1.fffp-25f : 0.f;
     using W = Weights<B>;
     // part h of a stage
     template <int HINT>
@@ -76,7 +79,8 @@ struct Dec16 : Op16<E, D> {
     __device__ static __forceinline__ void pack(W &w, const float (&p)[B::NS]) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float a = p[2 * j] * (LIFT * (1.f - 0x1p-20f)), b = p[2 * j + 1] * (LIFT * (1.f - 0x1p-20f));
+            const float a = __builtin_fmaf(p[2 * j], LIFT * (1.f - 0x1p-20f), -LEAST);
+            const float b = __builtin_fmaf(p[2 * j + 1], LIFT * (1.f - 0x1p-20f), -LEAST);
             uint32_t x;
             if constexpr (std::is_same<E, F16>::value) x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
             else x = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);

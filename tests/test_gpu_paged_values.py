@@ -96,3 +96,33 @@ def test_weights_of_fp32_keep_their_bits():
     got, (out, _) = P._f64(run(b)), oracle(b)
     rel = np.abs(got - out) / out
     assert (rel <= 1.1 * 3.8 * 2.0 ** -24).all(), "%.3g steps" % (rel.max() * 2.0 ** 24)
+
+
+# weights that an infinite value is seen with, in log2 below the largest
+SEEN = {F16: 36.0, BF16: 60.0, F32: 100.0}
+
+
+@DTYPES
+@REACH
+def test_an_infinite_value_shows_at_small_weights(dt, reach):
+    """One key of each sequence has some weight down to 2^-36 (fp16), 2^-60, 2^-100 of the largest, and infinities among its values; the other
+    keys' are finite."""
+    reach //= 2 if dt == F32 else 1
+    n = 48
+    rows = [reach] + [min(17 + 5 * r, reach) for r in range(1, n)]
+    b = batch(dt, (4, 2, 128), reach, rows, 1.0, seed=7)
+    g = torch.Generator().manual_seed(9)
+    unit = np.sqrt(128.0) * np.log(2.0)                    # of a score: a factor of 2
+    for r, m in enumerate(rows):
+        x = torch.zeros(m)
+        j = int(torch.randint(0, m, (1,), generator=g))
+        x[j] = -unit * SEEN[dt] * (r + torch.rand(1, generator=g).item()) / n * 0.98
+        column(b, b.kp, r, 0, x)
+        page = b.table[r, j // 16]
+        b.vp[page, :, j % 16, 5] = float("inf")
+        b.vp[page, :, j % 16, 100] = -float("inf")
+    got = run(b).float()
+    assert bool((got[:, :, 5] == float("inf")).all()), (got[:, 0, 5] != float("inf")).nonzero().flatten().tolist()
+    assert bool((got[:, :, 100] == -float("inf")).all())
+    rest = [i for i in range(128) if i not in (5, 100)]
+    assert bool(torch.isfinite(got[:, :, rest]).all())
