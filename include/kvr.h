@@ -545,7 +545,8 @@ int kvr_paged_append(const kvr_desc *desc, const kvr_pages *pages, const kvr_rop
  *   captured graphs) that may run at once need one each.
  * A sequence with len[r] < 0, or more than max_len rows, takes no part: its rows of out stay
  * as they were.  Rows in no page of the pool get no weight, whatever the others hold; a
- * sequence without any other rows, or with no row at all, gets zeros.
+ * sequence without any other rows, or with no row at all, gets zeros (one whose scores are
+ * all -infinity: NaN).
  * Scores, weights and sums in fp32; 16-bit weights enter the second product as two operands,
  * a cut weight and what the cut left over.  An infinite value gives an infinite mean where its
  * weight is at least 2^-36 (fp16), 2^-85 (bf16) or 2^-100 (fp32) of the largest, NaN below that.

@@ -345,6 +345,14 @@ struct Stage {
     }
 };
 
+// The sum of no weights.  Sums of it alone keep its sign, one with a weight of zero does not: keys whose scores
+// are all -infinity leave +0, and their softmax is no number; no keys leave this, and give zeros.
+constexpr float kNoKeys = -0.f;
+// What makes a row's products its output
+__device__ __forceinline__ float reciprocal(float l) {
+    return l > 0.f ? 1.f / l : __float_as_uint(l) == __float_as_uint(kNoKeys) ? 0.f : __builtin_nanf("");
+}
+
 template <class OP, int RT>
 struct Rows {
     f32x4 o[RT][OP::NT];
@@ -465,6 +473,7 @@ __device__ __forceinline__ void decode_units(const DecodeParams &p, Walk<OP, WAV
         p1.ask(p, n1, wave);
     }
     int seg_u = b.u;      // the segment's first unit here
+    int seen = 0;         // whether the wave has had any keys of it
     R.clear();
 
     for (;;) {
@@ -472,7 +481,7 @@ __device__ __forceinline__ void decode_units(const DecodeParams &p, Walk<OP, WAV
         typename OP::W w[RT];
         int rows[OP::PARTS];
 #pragma unroll
-        for (int h = 0; h < OP::PARTS; ++h) rows[h] = st.rows[h];
+        for (int h = 0; h < OP::PARTS; ++h) seen |= rows[h] = st.rows[h];
         if (more) st = St(p, n1, p1, wave);
         else st = St();
         n2 = n1;
@@ -503,12 +512,12 @@ __device__ __forceinline__ void decode_units(const DecodeParams &p, Walk<OP, WAV
             for (int rt = 0; rt < RT; ++rt) {
                 const int row = row0 + 16 * rt + i;
                 const bool on = row < p.group;
-                const float l = quad_sum(R.l[rt]);
+                const float l = seen ? quad_sum(R.l[rt]) : kNoKeys;
                 // c: the component of the lane's four, head-dim indices NT (4 g + c) ..
                 auto put = [&](int c, const f32x4 (&acc)[NT / 4], float M, float L) {
                     const int d = NT * (4 * g + c);
                     if (whole) {
-                        const float inv = L > 0.f ? 1.f / L * (1.f / OP::LIFT) : L == 0.f ? 0.f : L;      // no keys: zeros
+                        const float inv = reciprocal(L) * (1.f / OP::LIFT);
                         unsigned char *out = (unsigned char *)p.out + ((int64_t)b.r * p.n_q_heads + kh * p.group + row) * OP::ROWB;
 #pragma unroll
                         for (int t = 0; t < NT / 4; ++t)
@@ -543,7 +552,7 @@ __device__ __forceinline__ void decode_units(const DecodeParams &p, Walk<OP, WAV
                     }
                     __syncthreads();
                     if (on && wave < 4) {
-                        float M = -FLT_MAX, L = 0.f;
+                        float M = -FLT_MAX, L = kNoKeys;
                         f32x4 acc[NT / 4];
 #pragma unroll
                         for (int t = 0; t < NT / 4; ++t) acc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -572,7 +581,7 @@ __device__ __forceinline__ void decode_units(const DecodeParams &p, Walk<OP, WAV
             // these, its values among it
             wait_vmcnt<0>();
             at += b.u + 1 - seg_u;      // of the next segment's first unit
-            seg_u = 0;
+            seg_u = seen = 0;
         }
         if (!more) break;
         b = n1;
@@ -620,7 +629,7 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p)
     const int slot = threadIdx.x / LANES, way = slot / ROWS, d = threadIdx.x % LANES * 4;
     const int kh = hd / p.tiles, row0 = (hd - kh * p.tiles) * p.rows, rows = min(p.rows, p.group - row0);
     const int at = (blockIdx.x - seg * groups) * ROWS + slot % ROWS, row = min(at, rows - 1);
-    float M = -FLT_MAX, l = 0.f;
+    float M = -FLT_MAX, l = kNoKeys;
     f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
     for (int s0 = wgs.x + way; s0 <= wgs.y; s0 += WAYS * BATCH) {
         f32x4 x[BATCH];
@@ -629,7 +638,7 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p)
 #pragma unroll
         for (int s = 0; s < BATCH; ++s) {
             const int wg = s0 + s * WAYS;
-            w[s] = make_float2(-FLT_MAX, 0.f);
+            w[s] = make_float2(-FLT_MAX, kNoKeys);
             x[s] = (f32x4){0.f, 0.f, 0.f, 0.f};
             if (wg <= wgs.y) {
                 const int64_t rec = 2 * (int64_t)wg + (wg == wgs.x ? 1 : 0);
@@ -670,7 +679,7 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p)
 #pragma unroll
         for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(f, x[c], acc[c]);
     }
-    const float inv = l > 0.f ? 1.f / l * (1.f / OP::LIFT) : l == 0.f ? 0.f : l;
+    const float inv = reciprocal(l) * (1.f / OP::LIFT);
     const int64_t to = (int64_t)r * p.n_q_heads + kh * p.group + row0 + row;
     OP::put4((unsigned char *)p.out + to * OP::ROWB, d, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
 }

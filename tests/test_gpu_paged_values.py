@@ -126,3 +126,31 @@ def test_an_infinite_value_shows_at_small_weights(dt, reach):
     assert bool((got[:, :, 100] == -float("inf")).all())
     rest = [i for i in range(128) if i not in (5, 100)]
     assert bool(torch.isfinite(got[:, :, rest]).all())
+
+
+@DTYPES
+@REACH
+def test_scores_that_are_all_minus_infinity(dt, reach):
+    """Their softmax is no number, as in 64 bits; a sequence without rows in pages has zeros, and one finite score all
+    the weight."""
+    reach //= 2 if dt == F32 else 1
+    rows = [reach, 1, 40, 0, 40, reach, reach, 33]
+    lost = [(4, j, -1) for j in range(3)] + [(5, j, -1) for j in range(0, reach // 16, 2)]
+    b = batch(dt, (4, 2, 64) if reach != 1024 else (4, 2, 128), reach, rows, 1.0, seed=11, lost=lost)
+    for r, m in enumerate(rows):
+        if r not in (3, 4):
+            at = {j: int(b.table[r, j]) for j in range(-(-m // 16))}
+            for j, page in at.items():
+                if page >= 0:
+                    b.kp[page, :, :min(16, m - 16 * j), 0] = -float("inf")
+    last = rows[6] - 1
+    b.kp[b.table[6, last // 16], :, last % 16, 0] = -3.0
+    b.kp[b.table[7, 0], :, 2, 0] = 0.0
+    got = run(b)
+    for r in (0, 1, 2, 5):
+        assert bool(torch.isnan(got[r]).all()), r
+    for r in (3, 4):
+        assert bool((got[r] == 0).all()), r
+    for r, j in ((6, last), (7, 2)):
+        want = b.vp[b.table[r, j // 16], :, j % 16].repeat_interleave(2, 0)
+        assert torch.equal(got[r], want), r
