@@ -537,8 +537,9 @@ int kvr_paged_append(const kvr_desc *desc, const kvr_pages *pages, const kvr_rop
  *   sequence r, query head h reading kv head h / G.
  *   q: n_q_heads rows for each of n tokens (rotated already, as kvr_paged_append leaves
  *   them); out [n][n_q_heads][head_dim].
- *   len: DEVICE int32 [n], read when the work runs; n_new >= 0 is added to each: 1 where the
- *   step's token has been appended and len not yet advanced.
+ *   len: DEVICE int32 [n], read when the work runs (while it runs len must not change: results
+ *   are undefined then); n_new >= 0 is added to each: 1 where the step's token has been appended
+ *   and len not yet advanced.
  *   max_len: no sequence has more rows; at most max_pages * page_size (KVR_ERR_CAPACITY).
  *   It decides how the work is shared out and the workspace's size, not how much is read.
  *   ws: kvr_workspace_bytes_paged(desc, n, max_len) bytes, NULL when that is 0; calls (and
