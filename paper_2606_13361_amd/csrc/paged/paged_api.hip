@@ -162,14 +162,17 @@ bool plan_decode(const kvr_desc *d, int64_t n, int64_t max_len, DecodePlan *out)
     const int64_t bytes = stages * s.stage_bytes;      // of a sequence and head, at most
     const int64_t waves = kAskedBytes / s.stage_bytes * kCus;
     const int64_t by_heads = heads * kAloneByHeads < kAloneMost ? heads * kAloneByHeads : kAloneMost;
-    s.alone = bytes <= (by_heads > kAloneBytes ? by_heads : kAloneBytes);
+    const int64_t alone_bytes = by_heads > kAloneBytes ? by_heads : kAloneBytes;
+    s.alone = bytes <= alone_bytes;
     if (s.alone) s.waves = heads >= kOneWaveHeads && bytes <= kOneWaveBytes ? 1 : 4;
     else s.waves = stages <= kOneWaveStages ? 1 : 4;
     s.merge_rows = heads >= kMergeHeads ? 4 : 1;
     s.units = ceil_div(stages, s.waves) * heads;      // at most
     s.grid = s.alone ? heads : s.units < waves / s.waves ? s.units : waves / s.waves;
-    // (single waves have more records than workgroups of four: room for what a shorter max_len needs, too)
-    const int64_t one = (stages < kOneWaveStages ? stages : kOneWaveStages) * heads, most = one < waves ? one : waves;
+    // (single waves have more records than workgroups of four: room for what a shorter max_len needs, too, where one
+    // that is not one launch has single waves)
+    const int64_t one = kOneWaveStages * s.stage_bytes > alone_bytes ? (stages < kOneWaveStages ? stages : kOneWaveStages) * heads : 0;
+    const int64_t most = one < waves ? one : waves;
     const int64_t sharers = s.grid > most ? s.grid : most;
     if (!s.alone) s.ws_bytes = (size_t)(2 * sharers * s.rows * (d->head_dim + 2)) * sizeof(float) + (size_t)heads * 8;
     *out = s;
