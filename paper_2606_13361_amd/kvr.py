@@ -646,6 +646,14 @@ def kvr_cache_evict(desc, kcache, vcache, L, weight, n_keep, kout, vout, n_first
 
 
 # ---------------------------------------------------------------- paged caches
+def _fits(x, name, bits=32):
+    """x as an integer of the C call's type: ctypes would drop what is above it"""
+    x = int(x)
+    if not -(1 << (bits - 1)) <= x < 1 << (bits - 1):
+        raise ValueError("%s is %d, beyond %d bits" % (name, x, bits))
+    return x
+
+
 class PagedCache:
     """Sequences in the pages of a pool: k, v [n_pages, n_kv_heads, page_size, head_dim] and a
     page table, int32 [n, max_pages], all on one GPU.  A page is contiguous; pages may be any
@@ -672,6 +680,8 @@ class PagedCache:
             raise ValueError("pages of k are %d elements apart, those of v %d" % tuple(stride))
         if not isinstance(table, torch.Tensor) or table.dim() != 2:
             raise ValueError("table must be an int32 tensor [n, max_pages]")
+        for size, what in ((n_pages, "pages"), (ps, "rows of a page"), (table.shape[0], "rows of table"), (table.shape[1], "columns of table")):
+            _fits(size, "the number of " + what)
         tp = _at(table, "table", torch.int32, table.shape, dev)
         self.k, self.v, self.table = k, v, table
         self.device, self.n, self.reach = dev, table.shape[0], table.shape[1] * ps
@@ -758,8 +768,8 @@ def kvr_qk_norm_rope(desc, q, k, q_out=None, k_out=None, rope=None, q_norm=None,
     elif k_out is not None:
         raise ValueError("k_out without k")
     qn, kn = _vector(q_norm, "q_norm", dt, d, dev), _vector(k_norm, "k_norm", dt, d, dev)
-    at, rp = _vector(pos, "pos", torch.int32, n, dev), _rope_at(rope, desc, dev)
-    _launch(lambda s: load().kvr_qk_norm_rope(_byref(desc), rp, qi, ki, qn, kn, eps, n, at, int(pos0), qo, ko, s),
+    at, rp, p0 = _vector(pos, "pos", torch.int32, n, dev), _rope_at(rope, desc, dev), _fits(pos0, "pos0", 64)
+    _launch(lambda s: load().kvr_qk_norm_rope(_byref(desc), rp, qi, ki, qn, kn, eps, n, at, p0, qo, ko, s),
             "kvr_qk_norm_rope", stream, dev)
 
 
@@ -794,7 +804,7 @@ def kvr_paged_append(desc, cache, k, v, length, rope=None, cu_seqlens=None, pos=
 
 
 def kvr_workspace_bytes_paged(desc, n, max_len):
-    return _bytes(load().kvr_workspace_bytes_paged(ctypes.byref(desc), int(n), int(max_len)))
+    return _bytes(load().kvr_workspace_bytes_paged(ctypes.byref(desc), _fits(n, "n"), _fits(max_len, "max_len", 64)))
 
 
 def workspace_for_paged(desc, n, max_len, device="cuda"):
@@ -813,6 +823,6 @@ def kvr_paged_decode(desc, cache, q, length, out, ws=None, n_new=0, max_len=None
     qi, o = _rows(q, "q", dt, shape, dev), _at(out, "out", dt, shape, dev)
     ln = _at(length, "length", torch.int32, (n,), dev)
     wp, wn = _scratch(ws, dev)
-    most = cache.reach if max_len is None else int(max_len)
-    _launch(lambda s: load().kvr_paged_decode(_byref(desc), pages, qi, n, ln, int(n_new), most, o, wp, wn, s),
+    most, new = cache.reach if max_len is None else _fits(max_len, "max_len", 64), _fits(n_new, "n_new")
+    _launch(lambda s: load().kvr_paged_decode(_byref(desc), pages, qi, n, ln, new, most, o, wp, wn, s),
             "kvr_paged_decode", stream, dev)
