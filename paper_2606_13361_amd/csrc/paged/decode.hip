@@ -44,7 +44,7 @@ using namespace dev;
 // keep 16 bits (fp16: 22) and outputs are off by little more than their own rounding; the
 // products are matrix instructions that wait for memory anyway.  The cut is of a little less
 // than the weight: then both are positive, and an infinite value stays one, down to weights of 2^-36 (fp16:
-// the rest, too, is at least the smallest number) or 2^-85 (bf16) of the largest.  Below, it is no number.
+// the rest, too, is at least the smallest number) or 2^-75 (bf16) of the largest.  Below, it is no number.
 template <class OP>
 struct Weights {
     typename OP::P hi, lo;
@@ -53,11 +53,6 @@ template <class E, int D>
 struct Dec16 : Op16<E, D> {
     using B = Op16<E, D>;
     static constexpr int PARTS = 2;
-    // Weights enter the second product times LIFT, the largest one 1.  fp16 numbers end at 2^-24 and below 2^16: it is 2^15;
-    // bf16 and fp32 numbers reach down to 2^-126, and with 2^-20 a sum of a million of the largest values is finite, as
-    // their mean is.  A factor is exact; as an addend of the weight's exponent it would cost fp32 weights up to
-    // four bits (9 sequences of up to 945 rows off by 1.5e-7 instead of 7.9e-8).
-    static constexpr float LIFT = std::is_same<E, F16>::value ? 0x1p15f : 0x1p-20f;
     // of the rest: it rounds to the smallest fp16 number (and less than that: a weight of zero is not cut to minus it)
     static constexpr float LEAST = std::is_same<E, F16>::value ? 0x1.fffp-25f : 0.f;
     using W = Weights<B>;
@@ -77,16 +72,16 @@ struct Dec16 : Op16<E, D> {
             else v.r[4 * h + e] = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, HINT);
         }
     }
-    __device__ static __forceinline__ void pack(W &w, const float (&p)[B::NS]) {
+    __device__ static __forceinline__ void pack(W &w, const float (&p)[B::NS], float lift) {
+        const float cut = lift * (1.f - 0x1p-20f);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float a = __builtin_fmaf(p[2 * j], LIFT * (1.f - 0x1p-20f), -LEAST);
-            const float b = __builtin_fmaf(p[2 * j + 1], LIFT * (1.f - 0x1p-20f), -LEAST);
+            const float a = __builtin_fmaf(p[2 * j], cut, -LEAST), b = __builtin_fmaf(p[2 * j + 1], cut, -LEAST);
             uint32_t x;
             if constexpr (std::is_same<E, F16>::value) x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
             else x = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
             w.hi.f[j] = x;
-            w.lo.f[j] = E::pack2(__builtin_fmaf(p[2 * j], LIFT, -E::lo(x)), __builtin_fmaf(p[2 * j + 1], LIFT, -E::hi(x)));
+            w.lo.f[j] = E::pack2(__builtin_fmaf(p[2 * j], lift, -E::lo(x)), __builtin_fmaf(p[2 * j + 1], lift, -E::hi(x)));
         }
     }
     template <int RT>
@@ -107,7 +102,6 @@ template <int D>
 struct Dec32 : Op32<D> {
     using B = Op32<D>;
     static constexpr int PARTS = 1;
-    static constexpr float LIFT = 0x1p-20f;
     using W = typename B::P;
     template <int HINT>
     __device__ static __forceinline__ void load_k(typename B::K &k, __amdgpu_buffer_rsrc_t r, int, int i, int g) {
@@ -125,9 +119,9 @@ struct Dec32 : Op32<D> {
     __device__ static __forceinline__ f32x4 load(__amdgpu_buffer_rsrc_t r, int off) {
         return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, HINT));
     }
-    __device__ static __forceinline__ void pack(W &w, const float (&p)[B::NS]) {
+    __device__ static __forceinline__ void pack(W &w, const float (&p)[B::NS], float lift) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w.f[e] = p[e] * LIFT;
+        for (int e = 0; e < 4; ++e) w.f[e] = p[e] * lift;
     }
     template <int RT>
     __device__ static __forceinline__ void outputs(const typename B::V &v, const W (&w)[RT], f32x4 (&o)[RT][B::NT]) {
@@ -215,7 +209,7 @@ struct Rows {
 // from scores of 1e7 on).  It is of halves: two finite scores may be an infinity apart.
 template <class OP, int RT>
 __device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][OP::NS], typename OP::W (&w)[RT],
-                                             const int (&rows)[OP::PARTS], float c2, int g) {
+                                             const int (&rows)[OP::PARTS], float c2, float lift, int g) {
     int all = rows[0];
 #pragma unroll
     for (int h = 1; h < OP::PARTS; ++h) all += rows[h];
@@ -246,7 +240,7 @@ __device__ __forceinline__ void softmax_step(Rows<OP, RT> &R, float (&s)[RT][OP:
             sum += p[e];
         }
         R.l[rt] += sum;
-        OP::pack(w[rt], p);
+        OP::pack(w[rt], p, lift);
     }
 }
 
@@ -292,7 +286,7 @@ __device__ __forceinline__ void decode_units(const DecodeParams &p, Walk<OP, WAV
     constexpr int NT = OP::NT;
     using St = Stage<OP, WAVES>;
     const int i = lane & 15, g = lane >> 4;
-    const float c2 = p.half_scale_log2;
+    const float c2 = p.half_scale_log2, lift = p.lift;
     Unit n1, n2;       // the next unit, the one after it
     Pages<OP, WAVES> p1, p2;
     p1.ask(p, b, wave);
@@ -332,7 +326,7 @@ __device__ __forceinline__ void decode_units(const DecodeParams &p, Walk<OP, WAV
         __builtin_amdgcn_sched_barrier(0);
         st.template load_k<HINT>(p, k, i, g);
         __builtin_amdgcn_sched_barrier(0);
-        softmax_step<OP, RT>(R, s, w, rows, c2, g);
+        softmax_step<OP, RT>(R, s, w, rows, c2, lift, g);
         OP::template outputs<RT>(v, w, R.o);
         __builtin_amdgcn_sched_barrier(0);
         st.template load_v<HINT>(p, v, i, g);
@@ -353,7 +347,7 @@ __device__ __forceinline__ void decode_units(const DecodeParams &p, Walk<OP, WAV
                 auto put = [&](int c, const f32x4 (&acc)[NT / 4], float M, float L) {
                     const int d = NT * (4 * g + c);
                     if (whole) {
-                        const float inv = reciprocal(L) * (1.f / OP::LIFT);
+                        const float inv = reciprocal(L) * p.unlift;
                         unsigned char *out = (unsigned char *)p.out + ((int64_t)b.r * p.n_q_heads + kh * p.group + row) * OP::ROWB;
 #pragma unroll
                         for (int t = 0; t < NT / 4; ++t)
@@ -515,7 +509,7 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(const DecodeParams p)
 #pragma unroll
         for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(f, x[c], acc[c]);
     }
-    const float inv = reciprocal(l) * (1.f / OP::LIFT);
+    const float inv = reciprocal(l) * p.unlift;
     const int64_t to = (int64_t)r * p.n_q_heads + kh * p.group + row0 + row;
     OP::put4((unsigned char *)p.out + to * OP::ROWB, d, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
 }

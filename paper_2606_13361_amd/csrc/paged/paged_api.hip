@@ -307,6 +307,15 @@ int kvr_paged_decode(const kvr_desc *desc, const kvr_pages *pages, const kvr_row
     while (((uint64_t)1 << bits) < parts) ++bits;
     p.part_shift = 32 + bits;
     p.part_mul = (((uint64_t)1 << p.part_shift) + parts - 1) / parts;
+    // Weights enter the second product times this, the largest one 1.  fp16 numbers end at 2^-24 and below 2^16: 2^15;
+    // bf16 and fp32 numbers reach down to 2^-126, and a sum over max_len rows of the largest values is finite, as their
+    // mean is, with 1 / max_len (a half of that: sums are rounded).  A factor is exact; as an addend of the weight's
+    // exponent it would cost fp32 weights up to four bits (9 sequences of up to 945 rows off by 1.5e-7 instead of 7.9e-8).
+    int lift = 15;
+    if (desc->dtype != KVR_F16)
+        for (lift = -1; ((int64_t)1 << (-1 - lift)) < max_len;) --lift;
+    p.lift = ldexpf(1.f, lift);
+    p.unlift = ldexpf(1.f, -lift);
     // (finite: no difference stays none)
     p.half_scale_log2 = fminf(eff_scale(desc) * (2.f * 1.4426950408889634f), 3.4028235e38f);
     return to_status(launch_decode(p, desc->head_dim, desc->dtype, (hipStream_t)stream));

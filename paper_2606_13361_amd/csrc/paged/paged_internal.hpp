@@ -57,6 +57,7 @@ struct DecodeParams {
     uint32_t part_shift;     // 16-row parts of a page, as a divisor: (part * part_mul) >> part_shift
     uint64_t part_mul;
     float half_scale_log2;   // the scale in log2, of half a score: twice as large
+    float lift, unlift;      // factor of the weights in the second product, a power of two, and 1 / lift
 };
 // keys of a wave's stage: a unit of work is one for each of the workgroup's 1 or 4 waves
 constexpr int kStageKeys = 32, kStageKeysF32 = 16;

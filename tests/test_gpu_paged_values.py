@@ -154,3 +154,35 @@ def test_scores_that_are_all_minus_infinity(dt, reach):
     for r, j in ((6, last), (7, 2)):
         want = b.vp[b.table[r, j // 16], :, j % 16].repeat_interleave(2, 0)
         assert torch.equal(got[r], want), r
+
+
+@pytest.mark.parametrize("dt,big", [(BF16, 3.3e38), (F32, 3.3e38), (F16, 65504.0)], ids=["bf16", "f32", "fp16"])
+def test_a_mean_of_many_of_the_largest_values_is_finite(dt, big):
+    """2^25 rows, one page over and over, all of one value and one weight: 2^14 rows to each of 2048 waves, 2^12 products at
+    most, each off by 2^-24 of the sum, and up to 2^9 records joined: 2^-11 in all."""
+    b = Batch(dt, (4, 1, 64), 4096, [4096], spare=0)
+    b.q.zero_()
+    page = int(b.table[0, 0])
+    b.vp[page] = big
+    b.table = torch.full((1, 8192), page, dtype=torch.int32)
+    t = b.gpu()
+    t["len"].fill_(8192 * 4096)
+    b.call(t)
+    torch.cuda.synchronize()
+    want = float(torch.tensor(big, dtype=dt))
+    err = (t["out"].double().cpu() - want).abs().max().item()
+    assert err <= 1.1 * want * (2.0 ** -11 + torch.finfo(dt).eps / 2), err
+
+
+def test_small_values_of_short_sequences():
+    """Weights are lifted by 1 / max_len (32 rows: 2^-6) and no more: values of 3e-36 stay normal numbers.  32 sums and a
+    few more steps."""
+    b = Batch(F32, (4, 1, 64), 16, [32, 32, 16])
+    b.q.zero_()
+    g = torch.Generator().manual_seed(2)
+    want = (2.9e-36 * (1.0 + torch.rand(64, generator=g))).float()
+    for r in range(3):
+        for j in range(b.rows[r] // 16):
+            b.vp[b.table[r, j]] = want
+    err = (run(b).double() / want.double() - 1.0).abs().max().item()
+    assert err <= 1.1 * 38 * 2.0 ** -24, err
