@@ -548,9 +548,9 @@ int kvr_paged_append(const kvr_desc *desc, const kvr_pages *pages, const kvr_rop
  * as they were.  Rows in no page of the pool get no weight, whatever the others hold; a
  * sequence without any other rows, or with no row at all, gets zeros (one whose scores are
  * all -infinity: NaN).
- * Scores, weights and sums in fp32; 16-bit weights enter the second product as two operands,
- * a cut weight and what the cut left over.  An infinite value gives an infinite mean where its
- * weight is at least 2^-36 (fp16), 2^-75 (bf16) or 2^-90 (fp32) of the largest, NaN below that.
+ * Scores, weights and sums in fp32; weights enter the second product with 22 bits (fp16) or 24
+ * (as two or three operands).  An infinite value gives an infinite mean where its weight is at
+ * least 2^-36 (fp16), 2^-60 (bf16) or 2^-90 (fp32) of the largest, NaN below that.
  * Results are the same bit for bit for the same lengths of the whole batch.
  * out must not overlap the other arguments.
  * Limits: max_len at most 2^30; n n_q_heads below 2^24 and n n_q_heads max_len below 2^35 are

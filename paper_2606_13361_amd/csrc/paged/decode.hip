@@ -24,7 +24,7 @@
 //   one of 32768                        23.6 + 4.0   134 MB, 5.7 TB/s: four stages a wave
 //   one of 3774                         6.8 + 3.4    latency: lengths, page, keys, records, the second launch
 //   9 of up to 945, 16 / 2 heads of 64, fp32   5.4 + 3.6   latency
-// A stage of 32 keys and 128 dimensions is 16 loads, 24 matrix and 127 vector instructions, one wave on a SIMD.
+// A stage of 32 bf16 keys of 128 dimensions is 16 loads, 32 matrix and 161 vector instructions, one wave on a SIMD.
 // What it took, in a graph: records joined a query row a workgroup, one of 32768 38 -> 31.7 us; pages by scalar loads
 // (vector loads wait behind the keys on their way), 32 of 10 to 480 rows shared out 17 -> 14.4 and fewer registers,
 // 64 of up to 32768 768 -> 720; scores that wait for the keys only, 64 of 100 to 480 20.0 -> 19.5.
@@ -39,15 +39,18 @@ namespace {
 
 using namespace dev;
 
-// The two element kinds: a stage's weights as the second product's operand.  16-bit: the weight
-// cut to the element type and what that left over, rounded, as two operands, so that weights
-// keep 16 bits (fp16: 22) and outputs are off by little more than their own rounding; the
-// products are matrix instructions that wait for memory anyway.  The cut is of a little less
-// than the weight: then both are positive, and an infinite value stays one, down to weights of 2^-36 (fp16:
-// the rest, too, is at least the smallest number) or 2^-75 (bf16) of the largest.  Below, it is no number.
-template <class OP>
+// The two element kinds: a stage's weights as the second product's operands.  16-bit: the weight
+// cut to the element type, and what that left over, rounded (fp16: 22 bits) or, in bf16, cut and rounded once more
+// (24), so that outputs are off by their own rounding alone; the products are matrix instructions that wait for
+// memory anyway.  With two operands in bf16 (16 bits) 0.39 % of the outputs of 64 sequences of 300 to 32768 rows are
+// another bf16 number than the exact ones rounded, with three 0.06 %, and 32-bit arithmetic of weights rounded once has
+// 0.1 %; in a graph 632 and 635 us, one sequence of 300 rows 6.3 and 6.6, of 32768 27.1 and 27.5.
+// A cut is of a little less than its number: then all operands are positive, and an infinite value stays one, down to
+// weights of 2^-36 (fp16: the rest, too, is at least the smallest number) or 2^-60 (bf16) of the largest.  Below, it is
+// no number.
+template <class OP, int N>
 struct Weights {
-    typename OP::P hi, lo;
+    typename OP::P part[N];      // the largest first
 };
 template <class E, int D>
 struct Dec16 : Op16<E, D> {
@@ -55,7 +58,8 @@ struct Dec16 : Op16<E, D> {
     static constexpr int PARTS = 2;
     // of the rest: it rounds to the smallest fp16 number (and less than that: a weight of zero is not cut to minus it)
     static constexpr float LEAST = std::is_same<E, F16>::value ? 0x1.fffp-25f : 0.f;
-    using W = Weights<B>;
+    static constexpr int WEIGHTS = std::is_same<E, F16>::value ? 2 : 3;
+    using W = Weights<B, WEIGHTS>;
     // part h of a stage
     template <int HINT>
     __device__ static __forceinline__ void load_k(typename B::K &k, __amdgpu_buffer_rsrc_t r, int h, int i, int g) {
@@ -72,16 +76,25 @@ struct Dec16 : Op16<E, D> {
             else v.r[4 * h + e] = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, HINT);
         }
     }
+    __device__ static __forceinline__ uint32_t cut2(float a, float b) {
+        if constexpr (std::is_same<E, F16>::value) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
+        else return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+    }
     __device__ static __forceinline__ void pack(W &w, const float (&p)[B::NS], float lift) {
         const float cut = lift * (1.f - 0x1p-20f);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float a = __builtin_fmaf(p[2 * j], cut, -LEAST), b = __builtin_fmaf(p[2 * j + 1], cut, -LEAST);
-            uint32_t x;
-            if constexpr (std::is_same<E, F16>::value) x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
-            else x = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
-            w.hi.f[j] = x;
-            w.lo.f[j] = E::pack2(__builtin_fmaf(p[2 * j], lift, -E::lo(x)), __builtin_fmaf(p[2 * j + 1], lift, -E::hi(x)));
+            uint32_t x = cut2(a, b);
+            w.part[0].f[j] = x;
+            float r = __builtin_fmaf(p[2 * j], lift, -E::lo(x)), s = __builtin_fmaf(p[2 * j + 1], lift, -E::hi(x));
+            if constexpr (WEIGHTS == 3) {
+                x = cut2(r * (1.f - 0x1p-12f), s * (1.f - 0x1p-12f));
+                w.part[1].f[j] = x;
+                r -= E::lo(x);
+                s -= E::hi(x);
+            }
+            w.part[WEIGHTS - 1].f[j] = E::pack2(r, s);
         }
     }
     template <int RT>
@@ -90,10 +103,9 @@ struct Dec16 : Op16<E, D> {
         for (int t = 0; t < B::NT; ++t) {
             const u32x4 a = B::column(v, t);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                o[rt][t] = B::mfma(a, w[rt].lo.f, o[rt][t]);
-                o[rt][t] = B::mfma(a, w[rt].hi.f, o[rt][t]);
-            }
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int n = WEIGHTS - 1; n >= 0; --n) o[rt][t] = B::mfma(a, w[rt].part[n].f, o[rt][t]);
             if (RT > 1 && t % 2) __builtin_amdgcn_sched_barrier(0);      // operands of two at a time
         }
     }

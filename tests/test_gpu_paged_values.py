@@ -98,6 +98,25 @@ def test_weights_of_fp32_keep_their_bits():
     assert (rel <= 1.1 * 3.8 * 2.0 ** -24).all(), "%.3g steps" % (rel.max() * 2.0 ** 24)
 
 
+@DTYPES
+def test_weights_keep_their_bits_where_values_cancel(dt):
+    """Two keys, the values 1 and -1: out = (1 - w) / (1 + w), w = 2^-x, 0 <= x < 0.003, up to 0.001: the weights' errors are not
+    hidden by its rounding.  Steps of 2^-24: a weight's 1.2 (x has three roundings, 2^x is off by one place), the sum 1, the quotient 1,
+    the products 1, twice; and what a weight loses as operands: nothing (fp32), a third cut's rest of 2^-14, rounded: 2
+    (bf16), a rest of 2^-10 2^-11: 8 and a little (fp16)."""
+    n = 400
+    b = batch(dt, (4, 2, 64), 16, [2] * n, 0.125)
+    g = torch.Generator().manual_seed(6)
+    for r in range(n):
+        column(b, b.kp, r, 0, torch.rand(2, generator=g) * 0.125)
+        b.vp[b.table[r, 0], :, 0] = 1.0
+        b.vp[b.table[r, 0], :, 1] = -1.0
+    got, (out, _) = P._f64(run(b)), oracle(b)
+    steps = 8.4 + {F32: 0, BF16: 2, F16: 8.8}[dt]
+    err, allowed = np.abs(got - out), 1.1 * (torch.finfo(dt).eps / 2 * np.abs(out) + steps * 2.0 ** -24)
+    assert (err <= allowed).all(), "%.3g of what is allowed" % (err / allowed).max()
+
+
 # weights that an infinite value is seen with, in log2 below the largest
 SEEN = {F16: 36.0, BF16: 60.0, F32: 100.0}
 
