@@ -551,7 +551,7 @@ int kvr_paged_append(const kvr_desc *desc, const kvr_pages *pages, const kvr_rop
  * Scores, weights and sums in fp32; weights enter the second product with 22 bits (fp16) or 24
  * (as two or three operands).  An infinite value gives an infinite mean where its weight is at
  * least 2^-36 (fp16), 2^-60 (bf16) or 2^-90 (fp32) of the largest, NaN below that.
- * Results are the same bit for bit for the same lengths of the whole batch.
+ * Results are the same bit for bit for the same lengths of the whole batch and max_len.
  * out must not overlap the other arguments.
  * Limits: max_len at most 2^30; n n_q_heads below 2^24 and n n_q_heads max_len below 2^35 are
  * served (KVR_ERR_SHAPE).

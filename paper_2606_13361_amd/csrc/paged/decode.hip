@@ -19,11 +19,12 @@
 //
 // HBM bounds it: G operations for each byte of 16-bit keys and values, G query heads to a kv head.
 // Measured, a range's kernel and the join, in us (32 / 8 heads of 128 where nothing else is said):
-//   64 sequences of 300 to 32768 rows   618 + 4.6    4.3 GB, 7.0 TB/s
-//   64 of up to 4096, fp16              83.1 + 4.6   538 MB, 6.5 TB/s
-//   one of 32768                        23.6 + 4.0   134 MB, 5.7 TB/s: four stages a wave
-//   one of 3774                         6.8 + 3.4    latency: lengths, page, keys, records, the second launch
+//   64 sequences of 300 to 32768 rows   619 + 4.6    4.3 GB, 7.0 TB/s, what a launch that only reads reaches
+//   64 of up to 4096, fp16              83.4 + 4.7   538 MB, 6.5 TB/s (reading: 6.7)
+//   one of 32768                        23.9 + 4.5   134 MB, 5.6 TB/s (reading: 6.3): four stages a wave
+//   one of 3774                         7.0 + 3.5    latency: lengths, page, keys, records, the second launch
 //   9 of up to 945, 16 / 2 heads of 64, fp32   5.4 + 3.6   latency
+//   64 of 100 to 16000, fp32            740 in all   4.2 GB, 5.7 TB/s; 32 / 1 heads 124: 530 MB, 4.3 TB/s
 // A stage of 32 bf16 keys of 128 dimensions is 16 loads, 32 matrix and 161 vector instructions, one wave on a SIMD.
 // What it took, in a graph: records joined a query row a workgroup, one of 32768 38 -> 31.7 us; pages by scalar loads
 // (vector loads wait behind the keys on their way), 32 of 10 to 480 rows shared out 17 -> 14.4 and fewer registers,

@@ -113,32 +113,35 @@ int check_page_pointers(const kvr_pages *g) {
 // heads of 64); a stage is a wave's 16 KB of keys and values (8 KB at 64).
 //
 // Waves that share the units out: as many as ask for this much at once on a compute unit.  32, 64 and
-// 128 KB: one sequence of 32768 rows 33.5, 29.7 and 30.8, 64 of 100 to 4096 125, 105 and 107, of 300 to
-// 32768 829, 754 and 763; 16 / 2, 64 of 100 to 3900 21.2, 20.8 and 22.0.
+// 128 KB: one sequence of 32768 rows 38.0, 27.4 and 29.0, 64 of 100 to 4096 143, 99 and 98, in fp16 153, 95 and 106, of
+// 300 to 32768 1116, 682 and 683; 16 / 2, 64 of 100 to 3900 19.1, 19.7 and 21.2.
 constexpr int64_t kAskedBytes = 64 << 10;
 // A sequence and head of at most this many bytes is one workgroup's of four waves, and nothing is joined:
 // 256 KB, more where there are many of them, as far as one long sequence among short ones does not hold the
 // others up for long.  In one launch and shared out, in a graph and (in brackets) issued one by one, where two launches
-// take the host 10: 1 sequence of 310 rows 6.2 and 6.9 (7.4 and 10.4), 480 (240 KB) 7.5 and 7.3 (7.9 and 10.3), 600
-// 8.6 and 7.2 (8.9 and 10.4); 8 of 20 to 480 8.5 and 8.6 (8.2 and 10.1), to 600 9.5 and 9.0 (9.3 and 10.0); 16 / 2, 1 of 900
-// (232 KB) 8.4 and 7.0 (8.7 and 10.3); fp32, 8 of 10 to 250 (256 KB) 10.2 and 8.9 (9.9 and 10.2).  In a graph: 32 of 10 to 980
-// (496 KB) 18.5 and 20.3, 64 of 100 to 1500 (752 KB) 47.4 and 46.3; 16 / 2, 64 of 10 to 900 9.8 and 11.0; fp32, 64 of
-// 10 to 480 (480 KB) 34.2 and 33.9.
+// take the host 10: 1 sequence of 310 rows 6.6 and 7.0 (7.5 and 10.5), 480 (240 KB) 7.7 and 7.0 (8.1 and 10.3), 600
+// 8.7 and 7.3 (9.0 and 10.3); 8 of 20 to 480 8.6 and 8.7 (8.3 and 10.1), to 600 9.7 and 9.0 (9.6 and 9.9); 16 / 2, 1 of 900
+// (232 KB) 9.2 and 6.9 (9.5 and 9.8); fp32, 8 of 10 to 250 (256 KB) 10.2 and 8.9 (10.1 and 9.9).  In a graph: 32 of 10 to 980
+// (496 KB) 18.4 and 20.1, 64 of 100 to 1500 (752 KB) 47.7 and 45.7; 16 / 2, 64 of 10 to 900 10.1 and 10.9; fp32, 64 of
+// 10 to 480 (480 KB) 33.7 and 37.2.
 constexpr int64_t kAloneBytes = 256 << 10, kAloneMost = 512 << 10, kAloneByHeads = 2 << 10;
-// One wave instead of four, where many of them are short: 128 sequences of 10 to 200 rows 16.7 instead of 18.1, 256
-// 27.3 instead of 30.1, 256 of 10 to 480 (240 KB) 56.6 and 55.4; 64 of 10 to 250 12.5 and 11.3.
+// One wave instead of four, where many of them are short: 128 sequences of 10 to 200 rows 16.6 instead of 18.4, 256
+// 27.3 instead of 29.8, 256 of 10 to 480 (240 KB) 56.9 and 55.6; 64 of 10 to 250 12.0 and 11.2.
 constexpr int64_t kOneWaveHeads = 1024, kOneWaveBytes = 128 << 10;
 // Shared out, ranges of one wave up to this many stages of a sequence, of four beyond (records of which
-// there are fewer): 1 sequence of 480 rows 7.0 and 7.9, 980 (31 stages) 7.6 and 8.6, 1500 8.7 and 8.8, 3774
-// 11.6 and 9.8; 8 of 100 to 980 11.0 and 11.2.
+// there are fewer): 1 sequence of 480 rows 7.0 and 8.1, 980 (31 stages) 7.9 and 8.6, 1500 8.9 and 9.0, 3774
+// 11.6 and 9.9; 8 of 100 to 980 11.2 and 11.6.
 constexpr int64_t kOneWaveStages = 32;
 // Records are joined a query row a workgroup, or four where there are many: 1 and 4, one sequence of 3774
-// rows 9.8 and 11.7, 16 of 100 to 3980 32.1 and 31.8, 32 56.6 and 56.0, 1000 of 10 to 200 134 and 121.
+// rows 9.8 and 11.6, of 32768 27.1 and 29.0, 16 of 100 to 3980 31.3 and 31.2, 32 53.4 and 52.5, 64 of up to 4096 in fp16 95.5 and 93.8.
 constexpr int64_t kMergeHeads = 128;
 // Keys and values of a whole call from which they are loaded with the non-temporal hint, in ranges of four
-// waves and up to 16 query rows of a kv head.  Without and with it: 64 sequences of 300 to 32768 rows 752 and
-// 679, 64 of 100 to 4096 (538 MB) 105 and 93, one of 32768 (134 MB) 29.7 and 27.0, 8 of 100 to 3980 (67 MB) 20.4
-// and 19.4; one of 16000 (66 MB) that the caches still hold 16.8 and 16.7, 4 of 100 to 3980 (34 MB) 11.3 and 12.9.
+// waves and up to 16 query rows of a kv head.  Without and with it: 64 sequences of 300 to 32768 rows 767 and
+// 678, 64 of 100 to 4096 (538 MB) 105 and 94, one of 32768 (134 MB) 29.6 and 26.9, 8 of 100 to 3980 (67 MB) 20.3
+// and 19.4; one of 16000 (66 MB) 19.2 and 18.1, that the caches still hold 16.9 and 16.8, 4 of 100 to 3980 (34 MB) 14.4 and
+// 14.7, held 11.1 and 12.6; fp32, 64 of 100 to 16000 756 and 747.  What is read is counted, not what is
+// distinct: pages that sequences share come from the caches more slowly with the hint, 64 sequences with 256 rows each
+// behind one prefix of 4096 rows 93 and 107, of 32768 573 and 752.
 constexpr int64_t kStreamBytes = 48 << 20;
 
 struct DecodePlan {
